@@ -423,6 +423,67 @@ comfuse_status_t comfuse_gemm_spec(const comfuse_fusion_spec_t* spec, const comf
                                    void* const* row_out, int32_t fused, void* workspace, size_t workspace_bytes,
                                    void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * 8-bit integer layers (the paper has no counterpart: its precision is not stated).
+ *
+ * A linear layer in 8 bits multiplies int8 activations, one scale per row (token), by int8 weights, one scale per row of the
+ * weight (output channel); the sums are exact integers and the scales come behind them:
+ *   comfuse_quantize_rows   turns rows into int8 and a scale each, alone or behind a residual addition and an RMSNorm;
+ *   comfuse_gemm_q8         multiplies them by a quantised weight, with bias, activation and residual behind the scales.
+ * Inference only, like the rest of the library (rounding to 8 bits has no gradient).
+ * Conventions as above, except: tensors that are not 8-bit and not scales have the one type that the description names;
+ * scales are fp32 vectors and 4-byte aligned; a leading dimension is a multiple of 16 BYTES, a row length is any number. */
+typedef enum {
+  COMFUSE_DTYPE_BF16 = 0,
+  COMFUSE_DTYPE_F16 = 1,
+  COMFUSE_DTYPE_F32 = 2
+} comfuse_dtype_t;
+
+typedef enum {
+  COMFUSE_QUANTIZE_PLAIN = 0,  /* y = x                                                                             */
+  COMFUSE_QUANTIZE_RMSNORM = 1 /* h = x + residual;  y = h * rsqrt(mean(h^2) + eps) * gamma, over the row of N      */
+} comfuse_quantize_kind_t;
+
+typedef struct {
+  int32_t kind;               /* comfuse_quantize_kind_t */
+  int32_t dtype;              /* comfuse_dtype_t of x, residual, gamma and h */
+  int32_t rows, N;            /* rows >= 1, 1 <= N <= 65536 */
+  int64_t ldx, ldr, ldh;      /* elements; ldr / ldh matter where residual / h are given */
+  int64_t ldq, ldv;           /* elements of q (int8) and values (bf16; matters where given) */
+  float eps;                  /* RMSNORM kind: > 0 and finite; PLAIN kind: 0 */
+  int32_t reserved;           /* must be 0 */
+} comfuse_quantize_desc_t;
+
+/* scale[i] = max_j |y[i, j]| / 127,  q[i, j] = y[i, j] / scale[i] rounded to the nearest whole number (ties to even), so q lies in
+ * [-127, 127] and q * scale is within half a scale of y.  All arithmetic is fp32; y is not rounded to `dtype` in between, nor is
+ * h.  (y / scale is computed as 127 * h * gamma / max|h * gamma|, in which the norm cancels: within 2^-21 of its value, so a y that close to
+ * the middle of two codes may take either.)  A row of zeros has scale 0 and q 0.  A row with an infinity or a NaN in h * gamma (in x for the PLAIN
+ * kind) has scale NaN and q 0: everything computed from it is NaN.
+ * RMSNORM kind: residual may be NULL (h = x), gamma may be NULL (1); h, if not NULL, receives x + residual rounded to `dtype` and may
+ * be the residual or x itself (same pointer and leading dimension).  PLAIN kind: residual, gamma and h must be NULL.
+ * values, if not NULL, receives q * scale as bf16: what the 8 bits stand for, for this library's bf16 GEMMs (a model's accuracy
+ * before all its layers have 8-bit weights).  Columns between N and a leading dimension are neither read nor written. */
+comfuse_status_t comfuse_quantize_rows(const comfuse_quantize_desc_t* desc, const void* x, const void* residual, const void* gamma, void* h, int8_t* q,
+                                       float* scale, void* values, void* cuda_stream);
+
+typedef struct {
+  int32_t batch;              /* >= 1; A, B, residual, Y and the scales are batched, bias is shared */
+  int32_t M, N, K;            /* A int8 [M, K], B int8 [N, K] (one output channel per row), residual and Y [M, N]; N <= 65536, K <= 131071 */
+  int64_t lda, ldb, ldr, ldy; /* elements; ldr matters where residual is given */
+  int64_t batch_stride_a, batch_stride_b, batch_stride_r, batch_stride_y; /* elements, multiples of 16 bytes; matter for batch > 1 */
+  int32_t dtype;              /* comfuse_dtype_t of bias, residual and Y */
+  int32_t activation;         /* 0 = none, or COMFUSE_OP_RELU, COMFUSE_OP_GELU_TANH, COMFUSE_OP_TANH, COMFUSE_OP_SIGMOID */
+  uint32_t flags;             /* must be 0 */
+  int32_t reserved;           /* must be 0 */
+} comfuse_gemm_q8_desc_t;
+
+/* Y[i, j] = act(scale_a[i] * scale_b[j] * sum_k A[i, k] B[j, k] + bias[j]) + residual[i, j].  The sums are exact (int32: 131071 products
+ * of -128 * -128 fit), everything behind them is fp32, rounded once to `dtype` at the store.  scale_a: [batch, M], scale_b: [batch, N],
+ * dense; bias ([N]) and residual may be NULL.  Y may be the residual itself (same pointer and strides).  No workspace: calls of few
+ * rows split the contraction over a cluster and add its integer shares over distributed shared memory, in any order the same. */
+comfuse_status_t comfuse_gemm_q8(const comfuse_gemm_q8_desc_t* desc, const int8_t* A, const float* scale_a, const int8_t* B, const float* scale_b,
+                                 const void* bias, const void* residual, void* Y, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

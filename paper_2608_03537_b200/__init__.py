@@ -11,6 +11,8 @@ Functions mirror the C entry points:
     gemm_epilogue_host(...) -> comfuse_gemm_epilogue_host (per-step tensors in host memory, staged through a device buffer)
     b2b_gemm_host(...)      -> comfuse_b2b_gemm_host
     b2b_gemm(...)           -> comfuse_b2b_gemm           (GEMM -> F -> GEMM -> post-norm tail, Sec. 4)
+    quantize_rows(...), rmsnorm_quantize_rows(...) -> comfuse_quantize_rows (rows to int8 with a scale each, alone or behind a norm)
+    gemm_q8(...)            -> comfuse_gemm_q8            (int8 product with a scale for each token and channel)
     workspace_size(...)     -> comfuse_workspace_size
     b2b_workspace_size(...) -> comfuse_b2b_workspace_size
     last_device_status()    -> comfuse_last_device_status
@@ -52,6 +54,8 @@ EXPORTED_SYMBOLS = (
     "comfuse_gemm_spec",
     "comfuse_gemm_spec_prepare",
     "comfuse_program_compiler_status",
+    "comfuse_quantize_rows",
+    "comfuse_gemm_q8",
     "comfuse_selftest_bounds_predicate",
     "comfuse_last_device_status",
     "comfuse_launch_count",
@@ -81,6 +85,23 @@ class EpilogueArgs(Structure):
 class B2bDesc(Structure):
     _fields_ = [("M", c_int32), ("K", c_int32), ("N1", c_int32), ("N2", c_int32), ("eps", c_float), ("fused", c_int32),
                 ("kind", c_int32), ("batch", c_int32), ("alpha", c_float), ("flags", c_int32)]
+
+
+# 8-bit integer layers
+DTYPE_BF16, DTYPE_F16, DTYPE_F32 = 0, 1, 2
+QUANTIZE_PLAIN, QUANTIZE_RMSNORM = 0, 1
+
+
+class QuantizeDesc(Structure):
+    _fields_ = [("kind", c_int32), ("dtype", c_int32), ("rows", c_int32), ("N", c_int32), ("ldx", c_int64), ("ldr", c_int64), ("ldh", c_int64),
+                ("ldq", c_int64), ("ldv", c_int64), ("eps", c_float), ("reserved", c_int32)]
+
+
+class GemmQ8Desc(Structure):
+    _fields_ = [("batch", c_int32), ("M", c_int32), ("N", c_int32), ("K", c_int32),
+                ("lda", c_int64), ("ldb", c_int64), ("ldr", c_int64), ("ldy", c_int64),
+                ("batch_stride_a", c_int64), ("batch_stride_b", c_int64), ("batch_stride_r", c_int64), ("batch_stride_y", c_int64),
+                ("dtype", c_int32), ("activation", c_int32), ("flags", ctypes.c_uint32), ("reserved", c_int32)]
 
 
 # Epilogue programs as data: the node vocabulary (comfuse_op_t), by name
@@ -170,6 +191,10 @@ def lib() -> ctypes.CDLL:
         L.comfuse_gemm_spec_prepare.restype = c_int32
         L.comfuse_program_compiler_status.argtypes = [POINTER(ctypes.c_char_p)]
         L.comfuse_program_compiler_status.restype = c_int32
+        L.comfuse_quantize_rows.argtypes = [POINTER(QuantizeDesc)] + [c_void_p] * 8
+        L.comfuse_quantize_rows.restype = c_int32
+        L.comfuse_gemm_q8.argtypes = [POINTER(GemmQ8Desc)] + [c_void_p] * 8
+        L.comfuse_gemm_q8.restype = c_int32
         L.comfuse_last_device_status.argtypes = [c_void_p]
         L.comfuse_last_device_status.restype = c_int32
         L.comfuse_selftest_bounded_wait.argtypes = [ctypes.c_uint32, c_void_p, POINTER(ctypes.c_uint32)]
@@ -479,6 +504,73 @@ def gemm_spec(A, B, Y, spec: FusionSpec, *, params=(), row_out=(), fused=True, w
                                           _current_stream if stream is None else stream)
     if st != OK:
         raise ComfuseError(st, "comfuse_gemm_spec")
+    return Y
+
+
+ACTIVATIONS = {None: 0, "none": 0, "relu": OPS["relu"], "gelu_tanh": OPS["gelu_tanh"], "tanh": OPS["tanh"], "sigmoid": OPS["sigmoid"]}   # of gemm_q8
+_q8 = None   # the marshalling extension, once the 8-bit entry points are in it
+
+
+def _bound_q8():
+    global _q8, _current_device
+    if _q8 is None:
+        import torch
+        b = _bound()
+        b.bind_q8(*(ctypes.cast(f, c_void_p).value for f in (lib().comfuse_quantize_rows, lib().comfuse_gemm_q8)),
+                  torch.bfloat16, torch.float16, torch.float32, torch.int8)
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _q8 = b
+    return _q8
+
+
+def _current_device() -> int:   # (replaced by the bare call once the entry points are bound)
+    raise RuntimeError("no call has bound the 8-bit entry points yet")
+
+
+def _device_of(stream, q8) -> int:
+    """The device that a call's tensors have to be on: the current one, which the given stream has to belong to."""
+    if stream is None:
+        _current_stream()   # (sets the device up on first use)
+        return _current_device()
+    device = _current_device()
+    if getattr(stream, "device_index", device) != device:
+        raise AssertionError("the stream does not belong to the current device")
+    return device
+
+
+def quantize_rows(x, q, scale, *, values=None, stream=None):
+    """Enqueue q, scale = x as int8 codes with one scale per row: scale[i] = max|x[i]| / 127, q = x / scale rounded to nearest.  ``x`` [M, N]
+    bf16, fp16 or fp32, ``q`` [M, N] int8, ``scale`` [M] fp32; ``values`` [M, N] bf16, if given, receives q * scale.  Rows start on 16-byte
+    boundaries (allocate a leading dimension that is a multiple of 16 bytes).  A row with an infinity or NaN has scale NaN."""
+    b = _q8 or _bound_q8()
+    st = b.quantize_rows(QUANTIZE_PLAIN, x, None, None, None, q, scale, values, 0.0, _device_of(stream, b), _current_stream if stream is None else stream)
+    if st != OK:
+        raise ComfuseError(st, "comfuse_quantize_rows")
+    return q, scale
+
+
+def rmsnorm_quantize_rows(x, q, scale, *, residual=None, gamma=None, h=None, values=None, eps=1e-5, stream=None):
+    """Enqueue q, scale = int8 codes of y = t * rsqrt(mean(t^2) + eps) * gamma, t = x + residual, with one scale per row.  ``h``, if given,
+    receives t (it may be ``residual`` or ``x`` itself: the residual stream updated in place).  x, residual, h [M, N] and gamma [N] have one
+    type (bf16, fp16 or fp32); q, scale, values as in quantize_rows."""
+    b = _q8 or _bound_q8()
+    st = b.quantize_rows(QUANTIZE_RMSNORM, x, residual, gamma, h, q, scale, values, eps, _device_of(stream, b), _current_stream if stream is None else stream)
+    if st != OK:
+        raise ComfuseError(st, "comfuse_quantize_rows")
+    return q, scale
+
+
+def gemm_q8(A, scale_a, B, scale_b, Y, *, bias=None, residual=None, activation=None, stream=None):
+    """Enqueue Y = act(scale_a[i] * scale_b[j] * (A.B^T)[i, j] + bias[j]) + residual[i, j].  ``A`` int8 [M, K] (a token per row), ``B`` int8 [N, K]
+    (a linear layer's weight, an output channel per row), scales fp32 [M] and [N]; Y, bias and residual bf16, fp16 or fp32, one type.
+    With a leading batch dimension everywhere (bias excepted): a product per batch.  ``activation``: None, "relu", "gelu_tanh", "tanh" or
+    "sigmoid".  Rows start on 16-byte boundaries; ``residual`` may be ``Y`` itself."""
+    b = _q8 or _bound_q8()
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation: one of {list(ACTIVATIONS)} is expected, got {activation!r}")
+    st = b.gemm_q8(A, scale_a, B, scale_b, Y, bias, residual, ACTIVATIONS[activation], _device_of(stream, b), _current_stream if stream is None else stream)
+    if st != OK:
+        raise ComfuseError(st, "comfuse_gemm_q8")
     return Y
 
 

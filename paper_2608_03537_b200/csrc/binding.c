@@ -17,6 +17,12 @@ typedef comfuse_status_t (*b2b_gemm_fn)(const comfuse_b2b_desc_t*, const void*, 
                                         const void*, void*, void*, size_t, void*);
 typedef comfuse_status_t (*gemm_spec_fn)(const comfuse_fusion_spec_t*, const comfuse_gemm_shape_t*, const void*, const void*, void*, const void* const*,
                                          const int64_t*, void* const*, int32_t, void*, size_t, void*);
+typedef comfuse_status_t (*quantize_rows_fn)(const comfuse_quantize_desc_t*, const void*, const void*, const void*, void*, int8_t*, float*, void*, void*);
+typedef comfuse_status_t (*gemm_q8_fn)(const comfuse_gemm_q8_desc_t*, const int8_t*, const float*, const int8_t*, const float*, const void*, const void*, void*,
+                                       void*);
+static quantize_rows_fn f_quantize_rows;
+static gemm_q8_fn f_gemm_q8;
+static PyObject *t_bf16, *t_f16, *t_f32, *t_i8, *s_dtype, *s_get_device;  // the tensor library's element types (bind_q8)
 static gemm_epilogue_fn f_gemm_epilogue;
 static b2b_gemm_fn f_b2b_gemm;
 static gemm_spec_fn f_gemm_spec;
@@ -333,6 +339,153 @@ static PyObject* py_gemm_spec(PyObject* self, PyObject* const* a, Py_ssize_t n) 
   return ok ? PyLong_FromLong((long)st) : NULL;
 }
 
+// ---- the 8-bit integer layers.  Their tensors have more than one element type, so types, shapes and devices are looked at one by one.
+
+// The type of a tensor: `want`, or where that is NULL one of bf16, fp16 and fp32, as a comfuse_dtype_t (0 for a `want` that it is); -1 = refused.
+static int type_of(PyObject* t, PyObject* want, const char* what) {
+  PyObject* d = PyObject_GetAttr(t, s_dtype);
+  if (!d) return -1;
+  Py_DECREF(d);  // (a tensor's type outlives it)
+  if (want ? d == want : (d == t_bf16 || d == t_f16 || d == t_f32)) return want || d == t_bf16 ? COMFUSE_DTYPE_BF16 : d == t_f16 ? COMFUSE_DTYPE_F16 : COMFUSE_DTYPE_F32;
+  PyErr_Format(PyExc_AssertionError, "%s has another element type than the call takes", what);
+  return -1;
+}
+// A matrix (or a batch of them) of the given type and, where they are given (>= 0), sizes, with a dense last dimension, on `device`.
+static int matrix(PyObject* t, PyObject* type, int64_t device, int64_t batch, int64_t rows, int64_t cols, const char* what, Geometry* g, const void** p) {
+  int64_t at = 0;
+  if (type_of(t, type, what) < 0 || !geometry(t, g) || !method_i64(t, s_get_device, &at) || !pointer(t, p)) return 0;
+  if (g->n > 3 || (g->n == 3) != (batch >= 0) || (batch >= 0 && g->size[0] != batch) || (rows >= 0 && g->size[g->n - 2] != rows) ||
+      (cols >= 0 && g->size[g->n - 1] != cols)) {
+    PyErr_Format(PyExc_AssertionError, "%s has a shape that does not match the call", what);
+    return 0;
+  }
+  if (g->stride[g->n - 1] != 1 && g->size[g->n - 1] != 1) {
+    PyErr_Format(PyExc_AssertionError, "the last dimension of %s must be dense", what);
+    return 0;
+  }
+  if (at != device) {
+    PyErr_Format(PyExc_AssertionError, "%s is not on the current device", what);
+    return 0;
+  }
+  if (g->size[g->n - 2] == 1) g->stride[g->n - 2] = (g->size[g->n - 1] + 15) / 16 * 16;  // (one row: nothing is addressed by its stride)
+  return 1;
+}
+// A dense vector (or [batch, n]) of the given type with n elements; None: a null pointer.
+static int vector(PyObject* t, PyObject* type, int64_t device, int64_t batch, int64_t n, const char* what, const void** p) {
+  Geometry g;
+  int64_t at = 0;
+  *p = NULL;
+  if (t == Py_None) return 1;
+  if (type_of(t, type, what) < 0 || !shape_of(t, &g) || !method_i64(t, s_get_device, &at) || !pointer(t, p)) return 0;
+  if (g.n != (batch >= 0 ? 2 : 1) || (batch >= 0 && g.size[0] != batch) || g.size[g.n - 1] != n) {
+    PyErr_Format(PyExc_AssertionError, "%s has a shape that does not match the call", what);
+    return 0;
+  }
+  if (at != device) {
+    PyErr_Format(PyExc_AssertionError, "%s is not on the current device", what);
+    return 0;
+  }
+  return contiguous(t);
+}
+static PyObject* type_object(int dtype) { return dtype == COMFUSE_DTYPE_BF16 ? t_bf16 : dtype == COMFUSE_DTYPE_F16 ? t_f16 : t_f32; }
+
+// quantize_rows(kind, x, residual, gamma, h, q, scale, values, eps, device, stream) -> status
+static PyObject* py_quantize_rows(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  comfuse_quantize_desc_t d;
+  Geometry X, R = {0}, H = {0}, Q, V = {0};
+  const void *x, *r = NULL, *gamma, *h = NULL, *q, *scale, *v = NULL;
+  int64_t kind, device;
+  double eps;
+  void* stream;
+  if (!fixed_args(n, 11, "quantize_rows") || !to_i64(a[0], &kind) || !to_i64(a[9], &device) || !to_f64(a[8], &eps)) return NULL;
+  const int dtype = type_of(a[1], NULL, "x");
+  if (dtype < 0) return NULL;
+  PyObject* type = type_object(dtype);
+  if (!matrix(a[1], type, device, -1, -1, -1, "x", &X, &x)) return NULL;
+  const int64_t M = X.size[0], N = X.size[1];
+  if ((a[2] != Py_None && !matrix(a[2], type, device, -1, M, N, "residual", &R, &r)) || !vector(a[3], type, device, -1, N, "gamma", &gamma) ||
+      (a[4] != Py_None && !matrix(a[4], type, device, -1, M, N, "h", &H, &h)) || !matrix(a[5], t_i8, device, -1, M, N, "q", &Q, &q) ||
+      !vector(a[6], t_f32, device, -1, M, "scale", &scale) || (a[7] != Py_None && !matrix(a[7], t_bf16, device, -1, M, N, "values", &V, &v)) ||
+      !stream_of(a[10], &stream))
+    return NULL;
+  if (!require(M <= INT32_MAX && N <= INT32_MAX, "sizes are 32-bit numbers")) return NULL;
+  memset(&d, 0, sizeof(d));
+  d.kind = (int32_t)kind;
+  d.dtype = dtype;
+  d.rows = (int32_t)M;
+  d.N = (int32_t)N;
+  d.ldx = X.stride[0];
+  d.ldr = r ? R.stride[0] : 0;
+  d.ldh = h ? H.stride[0] : 0;
+  d.ldq = Q.stride[0];
+  d.ldv = v ? V.stride[0] : 0;
+  d.eps = (float)eps;
+  comfuse_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_quantize_rows(&d, x, r, gamma, (void*)h, (int8_t*)q, (float*)scale, (void*)v, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong((long)st);
+}
+
+// gemm_q8(A, scale_a, B, scale_b, Y, bias, residual, activation, device, stream) -> status
+static PyObject* py_gemm_q8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  comfuse_gemm_q8_desc_t d;
+  Geometry A, B, Y, R = {0};
+  const void *pA, *pB, *pY, *sa, *sb, *bias, *r = NULL;
+  int64_t activation, device;
+  void* stream;
+  if (!fixed_args(n, 10, "gemm_q8") || !to_i64(a[7], &activation) || !to_i64(a[8], &device)) return NULL;
+  const int dtype = type_of(a[4], NULL, "Y");
+  if (dtype < 0 || !shape_of(a[0], &A)) return NULL;
+  PyObject* type = type_object(dtype);
+  const int64_t batch = A.n == 3 ? A.size[0] : -1;
+  if (!matrix(a[0], t_i8, device, batch, -1, -1, "A", &A, &pA)) return NULL;
+  const int64_t M = A.size[A.n - 2], K = A.size[A.n - 1];
+  if (!matrix(a[2], t_i8, device, batch, -1, K, "B", &B, &pB)) return NULL;
+  const int64_t N = B.size[B.n - 2];
+  if (!vector(a[1], t_f32, device, batch, M, "scale_a", &sa) || !vector(a[3], t_f32, device, batch, N, "scale_b", &sb) ||
+      !matrix(a[4], type, device, batch, M, N, "Y", &Y, &pY) || !vector(a[5], type, device, -1, N, "bias", &bias) ||
+      (a[6] != Py_None && !matrix(a[6], type, device, batch, M, N, "residual", &R, &r)) || !stream_of(a[9], &stream))
+    return NULL;
+  if (!require(batch <= INT32_MAX && M <= INT32_MAX && N <= INT32_MAX && K <= INT32_MAX, "sizes are 32-bit numbers")) return NULL;
+  memset(&d, 0, sizeof(d));
+  d.batch = (int32_t)(batch < 0 ? 1 : batch);
+  d.M = (int32_t)M;
+  d.N = (int32_t)N;
+  d.K = (int32_t)K;
+  d.lda = A.stride[A.n - 2];
+  d.ldb = B.stride[B.n - 2];
+  d.ldy = Y.stride[Y.n - 2];
+  d.ldr = r ? R.stride[R.n - 2] : 0;
+  if (batch >= 0) {
+    d.batch_stride_a = A.stride[0];
+    d.batch_stride_b = B.stride[0];
+    d.batch_stride_y = Y.stride[0];
+    d.batch_stride_r = r ? R.stride[0] : 0;
+  }
+  d.dtype = dtype;
+  d.activation = (int32_t)activation;
+  comfuse_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_gemm_q8(&d, (const int8_t*)pA, (const float*)sa, (const int8_t*)pB, (const float*)sb, bias, r, (void*)pY, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong((long)st);
+}
+
+// bind_q8(address of comfuse_quantize_rows, of comfuse_gemm_q8, the tensor library's bf16, fp16, fp32 and int8 types)
+static PyObject* py_bind_q8(PyObject* self, PyObject* args) {
+  unsigned long long r, g;
+  PyObject* t[4];
+  if (!PyArg_ParseTuple(args, "KKOOOO", &r, &g, t, t + 1, t + 2, t + 3)) return NULL;
+  f_quantize_rows = (quantize_rows_fn)(uintptr_t)r;
+  f_gemm_q8 = (gemm_q8_fn)(uintptr_t)g;
+  t_bf16 = Py_NewRef(t[0]);
+  t_f16 = Py_NewRef(t[1]);
+  t_f32 = Py_NewRef(t[2]);
+  t_i8 = Py_NewRef(t[3]);
+  Py_RETURN_NONE;
+}
+
 // bind(address of comfuse_gemm_epilogue, of comfuse_b2b_gemm, of comfuse_gemm_spec): the loaded library's entry points
 static PyObject* py_bind(PyObject* self, PyObject* args) {
   unsigned long long e, b, s;
@@ -349,6 +502,9 @@ static PyMethodDef methods[] = {
     {"gemm_epilogue", (PyCFunction)(void (*)(void))py_gemm_epilogue, METH_FASTCALL, NULL},
     {"b2b", (PyCFunction)(void (*)(void))py_b2b, METH_FASTCALL, NULL},
     {"gemm_spec", (PyCFunction)(void (*)(void))py_gemm_spec, METH_FASTCALL, NULL},
+    {"bind_q8", py_bind_q8, METH_VARARGS, NULL},
+    {"quantize_rows", (PyCFunction)(void (*)(void))py_quantize_rows, METH_FASTCALL, NULL},
+    {"gemm_q8", (PyCFunction)(void (*)(void))py_gemm_q8, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
@@ -361,5 +517,7 @@ PyMODINIT_FUNC PyInit__binding(void) {
   s_numel = PyUnicode_InternFromString("numel");
   s_element_size = PyUnicode_InternFromString("element_size");
   s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+  s_dtype = PyUnicode_InternFromString("dtype");
+  s_get_device = PyUnicode_InternFromString("get_device");
   return PyModule_Create(&module);
 }

@@ -42,6 +42,11 @@ EncodeFn get_encode_fn() {
   return g_encode;
 }
 
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool mult8(long long v) { return (v & 7) == 0; }
+
+}  // namespace
+
 unsigned long long timeout_ns() {
   static unsigned long long v = [] {
     const char* e = std::getenv("COMFUSE_TIMEOUT_MS");
@@ -51,11 +56,6 @@ unsigned long long timeout_ns() {
   }();
   return v;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool mult8(long long v) { return (v & 7) == 0; }
-
-}  // namespace
 
 int ResidentClusters::of(const void* kernel, int threads, int smem_bytes, int size, const DeviceInfo& dev) {
   std::atomic<int>& slot = known_[dev.device < kMaxDev ? dev.device : kMaxDev - 1][size];
@@ -104,7 +104,7 @@ bool programmatic_launch_enabled() {
 
 // COMFUSE_FEW_ROWS=0 keeps calls of few rows on the kernels that calls of many rows take (few_rows.cu and few_rows_mlp.cu off): for
 // comparisons, and for testing those kernels' edges at small sizes.
-static bool few_rows_enabled() {
+bool few_rows_enabled() {
   static const bool on = [] {
     const char* e = std::getenv("COMFUSE_FEW_ROWS");
     return !(e && e[0] == '0');
@@ -183,6 +183,14 @@ const DeviceInfo* current_device_info() {
   return &g_dev[d];
 }
 
+comfuse_status_t check_device(const DeviceInfo** out) {
+  const DeviceInfo* dev = current_device_info();
+  if (!dev) return COMFUSE_ERR_CUDA;
+  if (dev->cc_major != 10) return COMFUSE_ERR_ARCH;
+  *out = dev;
+  return COMFUSE_OK;
+}
+
 bool encode_tmap_bf16_3d(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1_bytes,
                          uint64_t stride2_bytes, uint32_t box_rows) {
   EncodeFn enc = get_encode_fn();
@@ -194,6 +202,18 @@ bool encode_tmap_bf16_3d(CUtensorMap* out, const void* base, uint64_t d0, uint64
   return enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool encode_tmap_u8_3d(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1_bytes, uint64_t stride2_bytes,
+                       uint32_t box_rows) {
+  EncodeFn enc = get_encode_fn();
+  if (!enc) return false;
+  cuuint64_t dims[3] = {d0, d1, d2};
+  cuuint64_t strides[2] = {stride1_bytes, stride2_bytes};
+  cuuint32_t box[3] = {128, box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 namespace {
@@ -215,14 +235,6 @@ bool make_gemm_maps(GemmMaps* maps, const void* A, const void* B, const void* R,
   if (!encode_tmap_bf16_3d(&maps->Y, Y, N, M, batch, static_cast<uint64_t>(ldy) * 2, bs(bsy, M, ldy), 32)) return false;
   if (R && !encode_tmap_bf16_3d(&maps->R, R, N, M, batch, static_cast<uint64_t>(ldr) * 2, bs(bsr, M, ldr), 128)) return false;
   return true;
-}
-
-comfuse_status_t check_device(const DeviceInfo** out) {
-  const DeviceInfo* dev = current_device_info();
-  if (!dev) return COMFUSE_ERR_CUDA;
-  if (dev->cc_major != 10) return COMFUSE_ERR_ARCH;
-  *out = dev;
-  return COMFUSE_OK;
 }
 
 int kind_to_epi(int kind) {

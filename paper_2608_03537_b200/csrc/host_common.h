@@ -47,6 +47,15 @@ bool leader_reduce_enabled();
 bool encode_tmap_bf16_3d(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1_bytes,
                          uint64_t stride2_bytes, uint32_t box_rows);
 
+// The same for bytes: box = {128, box_rows, 1}, columns and rows outside the tensor read as zeros.
+bool encode_tmap_u8_3d(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1_bytes, uint64_t stride2_bytes,
+                       uint32_t box_rows);
+
+// COMFUSE_OK with the current device's facts, ERR_CUDA without a device, ERR_ARCH on one that is not compute capability 10.x.
+comfuse_status_t check_device(const DeviceInfo** out);
+unsigned long long timeout_ns();  // limit of every bounded wait (COMFUSE_TIMEOUT_MS)
+bool few_rows_enabled();          // COMFUSE_FEW_ROWS
+
 // Tensor maps of one GEMM -> subgraph call: operands A [batch, M, K] and B [batch, K, N], residual R and output Y
 // [batch, M, N]; all bf16, 128-byte swizzle, boxes of 64 elements by 128 rows (A, R), 64 rows (B) or 32 rows (Y: one
 // epilogue warp's box).

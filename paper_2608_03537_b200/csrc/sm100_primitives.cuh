@@ -345,6 +345,36 @@ __host__ __device__ constexpr uint32_t make_idesc_bf16(int m, int n, bool a_mn_m
          (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
 
+// The 8-bit integer kind: int8 operands, int32 accumulators, 32 elements of the contraction an instruction.  Instruction descriptor:
+//   [4,6) D format (2 = s32)  [7,10) A format (1 = signed 8 bits)  [10,13) B format  [15], [16] majors (0 = K)  [17,23) N >> 3  [24,29) M >> 4
+__host__ __device__ constexpr uint32_t make_idesc_i8(int m, int n) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+__device__ __forceinline__ void umma_i8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_i8_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Frees tensor memory, for the kernels of CTA pairs (kPair) and of single CTAs.
+template <bool kPair>
+__device__ __forceinline__ void tmem_release(uint32_t taddr, uint32_t ncols) {
+  if constexpr (kPair)
+    tmem_dealloc_pair(taddr, ncols);
+  else
+    tmem_dealloc(taddr, ncols);
+}
+
 // Shared-memory matrix descriptor, 128-byte swizzle.
 //   [0,14) start address >> 4   [16,30) leading byte offset >> 4   [32,46) stride byte offset >> 4
 //   [46,48) descriptor version (1 on sm_100)   [61,64) layout (2 = 128-byte swizzle)
