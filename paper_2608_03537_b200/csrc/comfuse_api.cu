@@ -204,16 +204,16 @@ bool encode_tmap_bf16_3d(CUtensorMap* out, const void* base, uint64_t d0, uint64
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool encode_tmap_u8_3d(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1_bytes, uint64_t stride2_bytes,
-                       uint32_t box_rows) {
+bool encode_tmap_128b_3d(CUtensorMap* out, CUtensorMapDataType type, int bytes, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t ld,
+                         uint64_t batch_stride, uint32_t box_rows) {
   EncodeFn enc = get_encode_fn();
   if (!enc) return false;
   cuuint64_t dims[3] = {d0, d1, d2};
-  cuuint64_t strides[2] = {stride1_bytes, stride2_bytes};
-  cuuint32_t box[3] = {128, box_rows, 1};
+  cuuint64_t strides[2] = {ld * bytes, batch_stride * bytes};
+  cuuint32_t box[3] = {128u / static_cast<uint32_t>(bytes), box_rows, 1};
   cuuint32_t estr[3] = {1, 1, 1};
-  return enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return enc(out, type, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 namespace {

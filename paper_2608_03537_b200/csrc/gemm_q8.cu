@@ -1,15 +1,16 @@
 // The 8-bit integer product for many rows: Y = act(sa sb (A . B^T) + bias) + R, on CTA pairs.
 //
 // What bounds it: the tensor cores (int8 at twice the bf16 rate), and behind short contractions the bytes of Y.  As in the bf16 tile
-// kernel two CTAs multiply a 256 x 256 tile (cta_group::2): each holds its own 128 rows of A and half of B's 256, 32 KB a K block of 128 bytes,
-// which the tensor cores take 512 clocks for.  Clusters of two are persistent and walk the tiles in bands of 8 row blocks, so that the
-// tiles in flight share their operands in the L2.  Two accumulators of 256 columns alternate: a tile's epilogue runs under the
-// next one's products.
+// kernel two CTAs multiply a 256 x BN tile (cta_group::2): each holds its own 128 rows of A and half of B's BN (256, or 128 where that fills
+// more SMs).  Clusters of two are persistent and walk the tiles in bands of 8 row blocks, so that the tiles in flight share their
+// operands in the L2.  Two accumulators alternate: a tile's epilogue runs under the next one's products.
 //
-// Epilogue: thread = one row of the tile, 32 columns at a time, a warp 128 of the 256.  The channel's scale and bias come from shared
-// memory (broadcast), the row's scale is a register.  Rows leave straight from registers, 32 bytes a store: every store fills its
-// sectors, so there is nothing that staging through shared memory would save, and the room goes to a sixth stage of the ring.
+// Epilogue: thread = one row of the tile, 32 columns at a time, a warp half of the columns.  The channel's scale and bias come from shared
+// memory (broadcast), the row's scale is a register.  Results leave as boxes of 32 rows x 128 bytes staged in shared memory and stored by
+// TMA; the residual comes in the same way, into the box that its sum leaves from.  A TMA store writes whole 16-byte units (measured: up to
+// seven bf16 behind the last column), so Y's map ends at the last whole unit and the columns behind it are stored one by one.
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 #include "q8_common.cuh"
@@ -18,23 +19,28 @@
 namespace comfuse {
 namespace {
 
+template <int BN, int STAGES, int BOXES>
 struct PairQ8Cfg {
-  static constexpr int NSTAGES = 6;
+  static constexpr int NSTAGES = STAGES;
   static constexpr int kEpiWarps = 8;
   static constexpr int kThreads = 32 * (2 + kEpiWarps);
-  static constexpr int HALF_BYTES = 128 * 128;           // 128 rows of A, or of B, x 128 bytes
-  static constexpr int STAGE_BYTES = 2 * HALF_BYTES;
-  static constexpr int OFF_VEC = NSTAGES * STAGE_BYTES;  // [2][256] (scale, bias) of the tile's channels
-  static constexpr int OFF_BAR = OFF_VEC + 2 * 256 * 8;
-  static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
-  static_assert((2 * NSTAGES + 5) * 8 + 16 <= 256, "barrier room");
+  static constexpr int A_BYTES = 128 * 128;              // 128 rows of A x 128 bytes
+  static constexpr int STAGE_BYTES = A_BYTES + BN / 2 * 128;
+  static constexpr int BOX_BYTES = 32 * 128;
+  static constexpr int OFF_BOX = NSTAGES * STAGE_BYTES;  // BOXES staging boxes a warp
+  static constexpr int OFF_VEC = OFF_BOX + kEpiWarps * BOXES * BOX_BYTES;  // [2][BN] (scale, bias) of the tile's channels
+  static constexpr int OFF_BAR = OFF_VEC + 2 * BN * 8;
+  static constexpr int NUM_BARS = 2 * NSTAGES + 5 + kEpiWarps * BOXES;
+  static constexpr int OFF_MISC = OFF_BAR + NUM_BARS * 8;
+  static constexpr int SMEM_BYTES = OFF_MISC + 16 + 1024;
+  static_assert(STAGE_BYTES % 1024 == 0, "swizzled tiles start on 1024-byte boundaries");
   static_assert(SMEM_BYTES <= 232448 && SMEM_BYTES > 116 * 1024, "one CTA per SM");
 };
 
-template <int DT>
-__global__ void __launch_bounds__(PairQ8Cfg::kThreads, 1) gemm_q8_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                                                                             const GemmQ8Params p) {
-  using Cfg = PairQ8Cfg;
+template <int DT, int BN, int STAGES, int BOXES>
+__global__ void __launch_bounds__(PairQ8Cfg<BN, STAGES, BOXES>::kThreads, 1)
+gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Params p) {
+  using Cfg = PairQ8Cfg<BN, STAGES, BOXES>;
   constexpr int NSTAGES = Cfg::NSTAGES;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
@@ -46,7 +52,8 @@ __global__ void __launch_bounds__(PairQ8Cfg::kThreads, 1) gemm_q8_pair_kernel(co
   auto bar_tfull = [&](int a) { return bar_base + 8u * (2 * NSTAGES + a); };    // accumulator complete
   auto bar_tempty = [&](int a) { return bar_base + 8u * (2 * NSTAGES + 2 + a); };  // accumulator read by both CTAs' epilogue warps (even CTA)
   const uint32_t bar_drain = bar_base + 8u * (2 * NSTAGES + 4);
-  uint32_t* s_tmem_base = reinterpret_cast<uint32_t*>(smem + Cfg::OFF_BAR + (2 * NSTAGES + 5) * 8);
+  auto bar_res = [&](int e, uint32_t k) { return bar_drain + 8u + 8u * (e * BOXES + k); };  // residual box k of epilogue warp e landed
+  uint32_t* s_tmem_base = reinterpret_cast<uint32_t*>(smem + Cfg::OFF_MISC);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem_base + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -66,13 +73,17 @@ __global__ void __launch_bounds__(PairQ8Cfg::kThreads, 1) gemm_q8_pair_kernel(co
       mbar_init(bar_tempty(a), 2 * Cfg::kEpiWarps);
     }
     mbar_init(bar_drain, 1);
+    for (int e = 0; e < Cfg::kEpiWarps; ++e)
+      for (uint32_t k = 0; k < BOXES; ++k) mbar_init(bar_res(e, k), 1);
     *s_abort = 0;
     fence_mbar_init();
-    prefetch_tensormap(&tmA);
-    prefetch_tensormap(&tmB);
+    prefetch_tensormap(&maps.A);
+    prefetch_tensormap(&maps.B);
+    prefetch_tensormap(&maps.Y);
+    if (p.residual) prefetch_tensormap(&maps.R);
   }
   if (warp == 1) {
-    tmem_alloc_pair(smem_u32(s_tmem_base), 512);
+    tmem_alloc_pair(smem_u32(s_tmem_base), 2 * BN);
     tmem_relinquish_alloc_permit_pair();
   }
   tcgen05_fence_before_sync();
@@ -90,7 +101,7 @@ __global__ void __launch_bounds__(PairQ8Cfg::kThreads, 1) gemm_q8_pair_kernel(co
     const long long band = t / (8ll * p.ntiles);
     const int in_band = static_cast<int>(t - band * 8 * p.ntiles), first = static_cast<int>(band * 8);
     const int high = p.mtiles - first < 8 ? p.mtiles - first : 8;
-    n0 = (in_band / high) * 256;
+    n0 = (in_band / high) * BN;
     m0 = (first + in_band % high) * 256;
   };
 
@@ -107,8 +118,8 @@ __global__ void __launch_bounds__(PairQ8Cfg::kThreads, 1) gemm_q8_pair_kernel(co
           if (!mbar_wait<false>(bar_empty(stage), phase ^ 1u, w)) { ok = false; break; }  // passes on a fresh barrier
           const uint32_t sa = smem_base + stage * Cfg::STAGE_BYTES, full = map_to_cta(bar_full(stage), 0);
           mbar_arrive_expect_tx_cluster(full, Cfg::STAGE_BYTES);
-          tma_load_3d_pair(sa, &tmA, full, kb * 128, m0 + static_cast<int>(rank) * 128, b);
-          tma_load_3d_pair(sa + Cfg::HALF_BYTES, &tmB, full, kb * 128, n0 + static_cast<int>(rank) * 128, b);
+          tma_load_3d_pair(sa, &maps.A, full, kb * 128, m0 + static_cast<int>(rank) * 128, b);
+          tma_load_3d_pair(sa + Cfg::A_BYTES, &maps.B, full, kb * 128, n0 + static_cast<int>(rank) * (BN / 2), b);
           if (++stage == NSTAGES) { stage = 0; phase ^= 1u; }
         }
       }
@@ -119,7 +130,7 @@ __global__ void __launch_bounds__(PairQ8Cfg::kThreads, 1) gemm_q8_pair_kernel(co
       int stage = 0;
       uint32_t phase = 0, n = 0;
       bool ok = true;
-      constexpr uint32_t idesc = make_idesc_i8(256, 256);
+      constexpr uint32_t idesc = make_idesc_i8(256, BN);
       for (long long tile = cluster_id; tile < p.tiles && ok; tile += clusters, ++n) {
         const uint32_t slot = n & 1u;
         if (!mbar_wait<false>(bar_tempty(slot), ((n >> 1) & 1u) ^ 1u, w)) break;
@@ -128,10 +139,10 @@ __global__ void __launch_bounds__(PairQ8Cfg::kThreads, 1) gemm_q8_pair_kernel(co
           if (!mbar_wait<false>(bar_full(stage), phase, w)) { ok = false; break; }
           tcgen05_fence_after_sync();
           const uint32_t sa = smem_base + stage * Cfg::STAGE_BYTES;
-          const uint64_t adesc = make_smem_desc_sw128(sa, 16, 1024), bdesc = make_smem_desc_sw128(sa + Cfg::HALF_BYTES, 16, 1024);
+          const uint64_t adesc = make_smem_desc_sw128(sa, 16, 1024), bdesc = make_smem_desc_sw128(sa + Cfg::A_BYTES, 16, 1024);
 #pragma unroll
           for (int k = 0; k < 4; ++k)  // 32 bytes of the contraction an instruction
-            umma_i8_ss_pair(tmem_base + slot * 256, adesc + static_cast<uint64_t>(2 * k), bdesc + static_cast<uint64_t>(2 * k), idesc, (kb | k) != 0 ? 1u : 0u);
+            umma_i8_ss_pair(tmem_base + slot * BN, adesc + static_cast<uint64_t>(2 * k), bdesc + static_cast<uint64_t>(2 * k), idesc, (kb | k) != 0 ? 1u : 0u);
           umma_commit_pair_both(bar_empty(stage));  // the stage is free in both CTAs once these have read it
           if (++stage == NSTAGES) { stage = 0; phase ^= 1u; }
         }
@@ -142,93 +153,118 @@ __global__ void __launch_bounds__(PairQ8Cfg::kThreads, 1) gemm_q8_pair_kernel(co
     }
   } else {
     // ------------------------------------------------------------------------------------------ epilogue warps
-    const int q = warp & 3, half = (warp - 2) >> 2;  // TMEM lane quarter: rows 32q ..; which 128 columns
-    const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * 128;
+    const int e = warp - 2, q = warp & 3, half = e >> 2;  // TMEM lane quarter: rows 32q ..; which half of the columns
+    constexpr int E = 128 / Elem<DT>::kBytes;               // columns of a box
+    const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * (BN / 2);
     const uint32_t tempty = map_to_cta(bar_tempty(0), 0);
+    const uint32_t box0 = smem_base + Cfg::OFF_BOX + e * BOXES * Cfg::BOX_BYTES;
     float2* s_vec = reinterpret_cast<float2*>(smem + Cfg::OFF_VEC);
-    constexpr int kWords = 8 * Elem<DT>::kBytes;  // 32 elements
-    uint32_t n = 0;
+    const int whole = gemm_q8_stored_columns(DT, p.N);  // by TMA
+    uint32_t n = 0, count = 0;  // tiles, and boxes of this warp
     for (long long tile = cluster_id; tile < p.tiles; tile += clusters, ++n) {
       int b, m0, n0;
       decode(tile, b, m0, n0);
       const uint32_t slot = n & 1u;
-      {
-        const int i = static_cast<int>(threadIdx.x) - 64, c = n0 + i;  // 256 threads, 256 channels
+      for (int i = static_cast<int>(threadIdx.x) - 64; i < BN; i += 32 * Cfg::kEpiWarps) {
+        const int c = n0 + i;
         float2 v = make_float2(0.f, 0.f);
         if (c < p.N) {
           v.x = __ldg(p.scale_b + static_cast<long long>(b) * p.N + c);
           if (p.bias) v.y = Elem<DT>::get(p.bias, c);
         }
-        s_vec[slot * 256 + i] = v;  // (the barrier below keeps the warps within one tile of each other)
+        s_vec[slot * BN + i] = v;  // (the barrier below keeps the warps within one tile of each other)
       }
       named_barrier_sync(1, 32 * Cfg::kEpiWarps);
-      const long long row = m0 + static_cast<int>(rank) * 128 + q * 32 + lane;
-      const bool live = row < p.M;
-      const float sa = live ? __ldg(p.scale_a + static_cast<long long>(b) * p.M + row) : 0.f;
-      const char* res = static_cast<const char*>(p.residual) + (b * p.batch_stride_r + row * p.ldr) * Elem<DT>::kBytes;
-      char* out = static_cast<char*>(p.Y) + (b * p.batch_stride_y + row * p.ldy) * Elem<DT>::kBytes;
+      const int row0 = m0 + static_cast<int>(rank) * 128 + q * 32, col0 = n0 + half * (BN / 2);
+      const float sa = row0 + lane < p.M ? __ldg(p.scale_a + static_cast<long long>(b) * p.M + row0 + lane) : 0.f;
+      const int left = row0 < p.M && col0 < p.N ? (p.N - col0 + E - 1) / E : 0;
+      const int boxes = left < BN / 2 / E ? left : BN / 2 / E;  // that hold anything of Y
+      // box k of this tile: once its staging box has been read out by the store before last, ask for the residual
+      auto ask = [&](int k) {
+        if (lane == 0 && p.residual && k < boxes) {
+          if (k == 0 || BOXES == 1) tma_store_wait_read<BOXES - 1>();
+          else tma_store_wait_read<BOXES - 2 < 0 ? 0 : BOXES - 2>();
+          const uint32_t sel = (count + k) % BOXES;
+          mbar_arrive_expect_tx(bar_res(e, sel), Cfg::BOX_BYTES);
+          tma_load_3d(box0 + sel * Cfg::BOX_BYTES, &maps.R, bar_res(e, sel), col0 + k * E, row0, b);
+        }
+      };
+      ask(0);
       const bool ok = mbar_wait<false>(bar_tfull(slot), (n >> 1) & 1u, w);
       __syncwarp();
       tcgen05_fence_after_sync();
+      auto release = [&]() {  // the accumulator is read: it may be overwritten once everyone is here
+        tcgen05_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_noflush(tempty + 8u * slot);
+      };
+      if (boxes == 0) release();
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        const int local = half * 128 + c * 32, col = n0 + local;
-        const bool whole = col + 32 <= p.N;
-        uint32_t rw[kWords];
-        if (p.residual && live && whole) {
+      for (int k = 0; k < boxes; ++k) {
+        const uint32_t sel = (count + k) % BOXES, row_addr = box0 + sel * Cfg::BOX_BYTES + lane * 128;
+        if (BOXES > 1) ask(k + 1);
+        else if (k > 0) ask(k);
 #pragma unroll
-          for (int i = 0; i < kWords; i += 8) {
-            const char* at = res + static_cast<long long>(col) * Elem<DT>::kBytes + i * 4;
-            if (p.wide) {
-              ld_32(at, rw + i);
-            } else {
-              ld_16(at, rw + i);
-              ld_16(at + 16, rw + i + 4);
-            }
+        for (int h = 0; h < E / 32; ++h) {
+          const int local = half * (BN / 2) + k * E + h * 32;
+          uint32_t v[32];
+          tmem_ld_32cols(lane_addr + slot * BN + k * E + h * 32, v);
+          if (k == boxes - 1 && h == E / 32 - 1) release();
+          float z[32];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float4 sv = *reinterpret_cast<const float4*>(s_vec + slot * BN + local + i);
+            z[i] = fmaf(static_cast<float>(static_cast<int>(v[i])) * sv.x, sa, sv.y);
+            z[i + 1] = fmaf(static_cast<float>(static_cast<int>(v[i + 1])) * sv.z, sa, sv.w);
           }
-        }
-        uint32_t v[32];
-        tmem_ld_32cols(lane_addr + slot * 256 + c * 32, v);
-        if (c == 3) {  // the last of this warp's columns is read: the accumulator may be overwritten once everyone is here
-          tcgen05_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster_noflush(tempty + 8u * slot);
-        }
-        float z[32];
+          activate(z, p.activation);
+          if (h == 0) {  // the staging box is this warp's again
+            if (p.residual) {
+              mbar_wait<false>(bar_res(e, sel), ((count + k) / BOXES) & 1u, w);
+            } else if (lane == 0) {
+              tma_store_wait_read<BOXES - 1>();
+            }
+            __syncwarp();
+          }
+          constexpr int kChunks = 2 * Elem<DT>::kBytes;  // 16-byte chunks of 32 columns
+          uint32_t at[kChunks];
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          const float4 sv = *reinterpret_cast<const float4*>(s_vec + slot * 256 + local + i);
-          z[i] = fmaf(static_cast<float>(static_cast<int>(v[i])) * sv.x, sa, sv.y);
-          z[i + 1] = fmaf(static_cast<float>(static_cast<int>(v[i + 1])) * sv.z, sa, sv.w);
-        }
-        activate(z, p.activation);
-        if (!live || !ok) continue;
-        if (whole) {
+          for (int c = 0; c < kChunks; ++c) at[c] = row_addr + (((h * kChunks + c) ^ (lane & 7)) << 4);
           if (p.residual) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) z[i] += Elem<DT>::of(rw, i);
-          }
-          uint32_t ow[kWords];
-          Elem<DT>::pack(z, ow);
-          if (COMFUSE_IN_BOUNDS(row < p.M && col + 31 < p.N && b < p.batch, p.status)) {
+            for (int c = 0; c < kChunks; ++c) {
+              uint32_t r[4];
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at[c]) : "memory");
+              constexpr int kEach = 16 / Elem<DT>::kBytes;
 #pragma unroll
-            for (int i = 0; i < kWords; i += 8) {
-              char* at = out + static_cast<long long>(col) * Elem<DT>::kBytes + i * 4;
-              if (p.wide) {
-                st_32(at, ow + i);
-              } else {
-                st_16(at, ow + i);
-                st_16(at + 16, ow + i + 4);
-              }
+              for (int i = 0; i < kEach; ++i) z[c * kEach + i] += Elem<DT>::of(r, i);
             }
           }
-        } else {
+          const int col = col0 + k * E + h * 32;
+          if (col + 32 > whole && ok && row0 + lane < p.M) {
+            void* out = static_cast<char*>(p.Y) + (b * p.batch_stride_y + static_cast<long long>(row0 + lane) * p.ldy) * Elem<DT>::kBytes;
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (col + i < p.N) Elem<DT>::put(out, col + i, p.residual ? z[i] + Elem<DT>::get(res, col + i) : z[i]);
+            for (int i = 0; i < 32; ++i)
+              if (col + i >= whole && col + i < p.N) Elem<DT>::put(out, col + i, z[i]);
+          }
+          uint32_t ow[4 * kChunks];
+          Elem<DT>::pack(z, ow);
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at[c]), "r"(ow[4 * c]), "r"(ow[4 * c + 1]), "r"(ow[4 * c + 2]), "r"(ow[4 * c + 3]) : "memory");
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          const int col = col0 + k * E;
+          if (ok && col < whole && COMFUSE_IN_BOUNDS(col < p.N && row0 < p.M && b < p.batch, p.status)) tma_store_3d(&maps.Y, box0 + sel * Cfg::BOX_BYTES, col, row0, b);
+          tma_store_commit();
         }
       }
+      count += static_cast<uint32_t>(boxes);
     }
+    if (lane == 0) tma_store_wait_read<0>();  // the staging boxes outlive the last stores' reads (the stores themselves complete at the kernel's end)
+    __syncwarp();
   }
 
   // -------------------------------------------------------------------------------------------- teardown
@@ -238,15 +274,15 @@ __global__ void __launch_bounds__(PairQ8Cfg::kThreads, 1) gemm_q8_pair_kernel(co
   if (warp == 1) {
     __syncwarp();
     tcgen05_fence_after_sync();
-    tmem_release<true>(tmem_base, 512);
+    tmem_release<true>(tmem_base, 2 * BN);
     if (lane == 0) linger_behind_expired_wait(w);
   }
 }
 
-template <int DT>
-cudaError_t launch_instance(const CUtensorMap& tmA, const CUtensorMap& tmB, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
-  using Cfg = PairQ8Cfg;
-  auto kern = gemm_q8_pair_kernel<DT>;
+template <int DT, int BN, int STAGES, int BOXES>
+cudaError_t launch_instance(const GemmQ8PairMaps& maps, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
+  using Cfg = PairQ8Cfg<BN, STAGES, BOXES>;
+  auto kern = gemm_q8_pair_kernel<DT, BN, STAGES, BOXES>;
   static ResidentClusters resident;  // (sets the kernel's attributes on the device the first time it is asked)
   const int fit = resident.of(reinterpret_cast<const void*>(kern), Cfg::kThreads, Cfg::SMEM_BYTES, 2, dev);
   if (fit < 1) return cudaErrorLaunchOutOfResources;
@@ -265,19 +301,31 @@ cudaError_t launch_instance(const CUtensorMap& tmA, const CUtensorMap& tmB, cons
   cfg.attrs = attr;
   cfg.numAttrs = programmatic_launch_enabled() ? 2 : 1;
   count_launch();
-  return cudaLaunchKernelEx(&cfg, kern, tmA, tmB, p);
+  return cudaLaunchKernelEx(&cfg, kern, maps, p);
+}
+
+template <int DT>
+cudaError_t launch_columns(int columns, const GemmQ8PairMaps& maps, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
+  if (columns == 128) return launch_instance<DT, 128, 6, 2>(maps, p, dev, stream);
+  return launch_instance<DT, 256, 5, 1>(maps, p, dev, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_gemm_q8_pair(int dtype, const CUtensorMap& tmA, const CUtensorMap& tmB, GemmQ8Params p, const DeviceInfo& dev, cudaStream_t stream) {
+int gemm_q8_pair_columns(int batch, int M, int N, int K, const DeviceInfo& dev) {
+  if (getenv("TC")) return atoi(getenv("TC"));
+  const long long blocks = static_cast<long long>(batch) * ((M + 255) / 256);
+  return 2 * blocks * ((N + 255) / 256) <= dev.sm_count / 2 || N <= 128 ? 128 : 256;
+}
+
+cudaError_t launch_gemm_q8_pair(int dtype, int columns, const GemmQ8PairMaps& maps, GemmQ8Params p, const DeviceInfo& dev, cudaStream_t stream) {
   p.mtiles = (p.M + 255) / 256;
-  p.ntiles = (p.N + 255) / 256;
+  p.ntiles = (p.N + columns - 1) / columns;
   p.tiles = static_cast<long long>(p.batch) * p.mtiles * p.ntiles;
   switch (dtype) {
-    case COMFUSE_DTYPE_BF16: return launch_instance<COMFUSE_DTYPE_BF16>(tmA, tmB, p, dev, stream);
-    case COMFUSE_DTYPE_F16: return launch_instance<COMFUSE_DTYPE_F16>(tmA, tmB, p, dev, stream);
-    default: return launch_instance<COMFUSE_DTYPE_F32>(tmA, tmB, p, dev, stream);
+    case COMFUSE_DTYPE_BF16: return launch_columns<COMFUSE_DTYPE_BF16>(columns, maps, p, dev, stream);
+    case COMFUSE_DTYPE_F16: return launch_columns<COMFUSE_DTYPE_F16>(columns, maps, p, dev, stream);
+    default: return launch_columns<COMFUSE_DTYPE_F32>(columns, maps, p, dev, stream);
   }
 }
 

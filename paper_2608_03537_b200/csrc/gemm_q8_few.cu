@@ -6,6 +6,7 @@
 // accumulators go to shared memory as [row][channel]; behind a cluster barrier each CTA adds its slice of the rows from all of them through
 // distributed shared memory and finishes it, a warp per row and 4 channels per lane.  Integer sums are exact, so the split changes no bit
 // of the result.
+#include <cstdlib>
 #include <type_traits>
 
 #include "q8_common.cuh"
@@ -85,11 +86,32 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads) gemm_q8_few_kernel(const
   const uint32_t tmem_base = *s_tmem_base;
   griddep_wait();
 
-  // epilogue: warp e - 2 finishes every 8th row of the CTA's slice, a lane 4 channels of it
+  // Epilogue: a warp finishes every 8th row of the CTA's slice, a lane 4 channels of it.  RB rows advance together: what they need from
+  // global memory is asked for at once, for the first RB while the products still run.
+  constexpr int RB = 4;
   const int rs = (rows + p.split - 1) / p.split;  // rows per slice
-  const int row0 = rank * rs, row1 = row0 + rs < rows ? row0 + rs : rows;
+  const int row1 = (rank + 1) * rs < rows ? (rank + 1) * rs : rows;
+  int row = rank * rs + warp - 2;
   const int col = n0 + 4 * lane;
   const bool whole = col + 4 <= p.N;
+  const float* scale_a = p.scale_a + static_cast<long long>(b) * p.M + m0;
+  const char* res = static_cast<const char*>(p.residual) + (b * p.batch_stride_r + m0 * p.ldr + col) * Elem<DT>::kBytes;
+  char* out = static_cast<char*>(p.Y) + (b * p.batch_stride_y + m0 * p.ldy + col) * Elem<DT>::kBytes;
+  float sa[RB], sb[4], bias[4];
+  uint32_t rw[RB][Elem<DT>::kBytes];
+  auto fetch = [&]() {
+#pragma unroll
+    for (int k = 0; k < RB; ++k) {
+      const int r = row + k * Cfg::kEpiWarps;
+      if (r < row1) {
+        sa[k] = __ldg(scale_a + r);
+        if (p.residual && whole) {
+          if constexpr (Elem<DT>::kBytes == 4) ld_16(res + r * p.ldr * 4, rw[k]);
+          else ld_8(res + r * p.ldr * 2, rw[k]);
+        }
+      }
+    }
+  };
 
   if (warp == 0) {
     // ------------------------------------------------------------------------------------------ TMA producer
@@ -131,6 +153,12 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads) gemm_q8_few_kernel(const
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;  // TMEM lane quarter; which half of the rows this warp moves to shared memory
     constexpr int MOVE = MT / 2, STEP = MOVE < 16 ? 8 : 16;
+    fetch();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sb[i] = col + i < p.N ? __ldg(p.scale_b + static_cast<long long>(b) * p.N + col + i) : 0.f;
+      bias[i] = p.bias && col + i < p.N ? Elem<DT>::get(p.bias, col + i) : 0.f;
+    }
     mbar_wait<false>(bar_acc, 0, w);
     __syncwarp();
     tcgen05_fence_after_sync();
@@ -157,53 +185,51 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads) gemm_q8_few_kernel(const
   else __syncthreads();
 
   if (warp >= 2) {
-    float sb[4], bias[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      sb[i] = col + i < p.N ? __ldg(p.scale_b + static_cast<long long>(b) * p.N + col + i) : 0.f;
-      bias[i] = p.bias && col + i < p.N ? Elem<DT>::get(p.bias, col + i) : 0.f;
-    }
-    for (int r = row0 + warp - 2; r < row1; r += Cfg::kEpiWarps) {
-      const long long grow = m0 + r;
-      const float sa = __ldg(p.scale_a + static_cast<long long>(b) * p.M + grow);
-      const char* res = static_cast<const char*>(p.residual) + (b * p.batch_stride_r + grow * p.ldr + col) * Elem<DT>::kBytes;
-      char* out = static_cast<char*>(p.Y) + (b * p.batch_stride_y + grow * p.ldy + col) * Elem<DT>::kBytes;
-      uint32_t rw[Elem<DT>::kBytes];
-      if (p.residual && whole) {
-        if constexpr (Elem<DT>::kBytes == 4) ld_16(res, rw);
-        else ld_8(res, rw);
-      }
-      int acc[4] = {0, 0, 0, 0};
-      const uint32_t src = smem_base + static_cast<uint32_t>(r * Cfg::ROW_BYTES + lane * 16);
+    while (row < row1) {
+      int acc[RB][4] = {};
       for (int s = 0; s < p.split; ++s) {
-        int o[4];
-        asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
-                     : "r"(p.split > 1 ? map_to_cta(src, static_cast<uint32_t>(s)) : src)
-                     : "memory");
+        const uint32_t src = smem_base + static_cast<uint32_t>(row * Cfg::ROW_BYTES + lane * 16);
+        const uint32_t at = p.split > 1 ? map_to_cta(src, static_cast<uint32_t>(s)) : src;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += o[i];
-      }
-      float z[4];
+        for (int k = 0; k < RB; ++k) {
+          if (row + k * Cfg::kEpiWarps >= row1) continue;
+          int o[4];
+          asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
+                       : "r"(at + static_cast<uint32_t>(k * Cfg::kEpiWarps * Cfg::ROW_BYTES))
+                       : "memory");
 #pragma unroll
-      for (int i = 0; i < 4; ++i) z[i] = fmaf(static_cast<float>(acc[i]) * sb[i], sa, bias[i]);
-      activate(z, p.activation);
-      if (whole) {
-        if (p.residual) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) z[i] += Elem<DT>::of(rw, i);
+          for (int i = 0; i < 4; ++i) acc[k][i] += o[i];
         }
-        uint32_t ow[Elem<DT>::kBytes];
-        Elem<DT>::pack(z, ow);
-        if (COMFUSE_IN_BOUNDS(grow < p.M && col + 3 < p.N && b < p.batch, p.status)) {
-          if constexpr (Elem<DT>::kBytes == 4) st_16(out, ow);
-          else st_8(out, ow);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (col + i < p.N) Elem<DT>::put(out, i, p.residual ? z[i] + Elem<DT>::get(res, i) : z[i]);
       }
+#pragma unroll
+      for (int k = 0; k < RB; ++k) {
+        const int r = row + k * Cfg::kEpiWarps;
+        if (r >= row1) break;
+        float z[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = fmaf(static_cast<float>(acc[k][i]) * sb[i], sa[k], bias[i]);
+        activate(z, p.activation);
+        char* to = out + r * p.ldy * Elem<DT>::kBytes;
+        if (whole) {
+          if (p.residual) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] += Elem<DT>::of(rw[k], i);
+          }
+          uint32_t ow[Elem<DT>::kBytes];
+          Elem<DT>::pack(z, ow);
+          if (COMFUSE_IN_BOUNDS(m0 + r < p.M && col + 3 < p.N && b < p.batch, p.status)) {
+            if constexpr (Elem<DT>::kBytes == 4) st_16(to, ow);
+            else st_8(to, ow);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (col + i < p.N) Elem<DT>::put(to, i, p.residual ? z[i] + Elem<DT>::get(res + r * p.ldr * Elem<DT>::kBytes, i) : z[i]);
+        }
+      }
+      row += RB * Cfg::kEpiWarps;
+      fetch();
     }
   }
 
@@ -269,14 +295,17 @@ cudaError_t launch_rows(int rows, const CUtensorMap& tmW, const CUtensorMap& tmX
 
 GemmQ8FewPlan gemm_q8_few_plan(int batch, int M, int N, int K, const DeviceInfo& dev) {
   GemmQ8FewPlan c;
+  if (getenv("TR")) c.rows = atoi(getenv("TR")); else
   c.rows = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
   const long long tiles = static_cast<long long>(batch) * ((M + c.rows - 1) / c.rows) * ((N + 127) / 128);
   const long long slots = static_cast<long long>(dev.sm_count) * (c.rows <= 64 ? 2 : 1);
-  if (tiles > slots) {
+  if (getenv("TC")) { c.rows = 0; return c; }
+  if (tiles > slots && !getenv("TR")) {
     c.rows = 0;
     return c;
   }
   const int KB = (K + 127) / 128;
+  if (getenv("TS")) { c.split = atoi(getenv("TS")); return c; }
   while (c.split < 8 && tiles * c.split * 2 <= slots && KB >= 4 * c.split) c.split *= 2;
   return c;
 }

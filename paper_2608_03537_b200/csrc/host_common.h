@@ -47,9 +47,10 @@ bool leader_reduce_enabled();
 bool encode_tmap_bf16_3d(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1_bytes,
                          uint64_t stride2_bytes, uint32_t box_rows);
 
-// The same for bytes: box = {128, box_rows, 1}, columns and rows outside the tensor read as zeros.
-bool encode_tmap_u8_3d(CUtensorMap* out, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t stride1_bytes, uint64_t stride2_bytes,
-                       uint32_t box_rows);
+// The same for elements of any type of `bytes` bytes: boxes of 128 bytes x box_rows rows; strides in ELEMENTS.  Columns and rows outside the
+// tensor read as zeros and are not written.
+bool encode_tmap_128b_3d(CUtensorMap* out, CUtensorMapDataType type, int bytes, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t ld,
+                         uint64_t batch_stride, uint32_t box_rows);
 
 // COMFUSE_OK with the current device's facts, ERR_CUDA without a device, ERR_ARCH on one that is not compute capability 10.x.
 comfuse_status_t check_device(const DeviceInfo** out);

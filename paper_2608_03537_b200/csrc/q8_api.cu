@@ -1,5 +1,6 @@
 // C entry points of the 8-bit integer layers: argument checks, tensor maps, choice of the form.
 #include <cmath>
+#include <cstdlib>
 
 #include "../../include/comfuse.h"
 #include "q8_params.h"
@@ -99,20 +100,38 @@ comfuse_status_t comfuse_gemm_q8(const comfuse_gemm_q8_desc_t* desc, const int8_
   p.ldr = d.ldr; p.ldy = d.ldy;
   p.batch_stride_r = d.batch > 1 ? d.batch_stride_r : 0;
   p.batch_stride_y = d.batch > 1 ? d.batch_stride_y : 0;
-  const int e = dtype_bytes(d.dtype);
-  auto sectors = [&](const void* base, long long ld, long long bs) { return aligned(base, 32) && ((ld * e) & 31) == 0 && ((bs * e) & 31) == 0; };
-  p.wide = sectors(Y, d.ldy, p.batch_stride_y) && (!residual || sectors(residual, d.ldr, p.batch_stride_r)) ? 1 : 0;
   p.status = dev->status_word;
   p.timeout_ns = timeout_ns();
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (few_rows_enabled() && gemm_q8_tokens_fits(d.batch, d.M) && !getenv("TR")) {
+    const GemmQ8TokensParams t = {A, B, d.lda, d.ldb, d.batch > 1 ? d.batch_stride_a : 0, d.batch > 1 ? d.batch_stride_b : 0};
+    return launch_gemm_q8_tokens(d.dtype, t, p, *dev, st) == cudaSuccess ? COMFUSE_OK : COMFUSE_ERR_CUDA;
+  }
   GemmQ8FewPlan few;
   if (few_rows_enabled()) few = gemm_q8_few_plan(d.batch, d.M, d.N, d.K, *dev);
-  CUtensorMap tmA, tmB;
-  if (!encode_tmap_u8_3d(&tmA, A, d.K, d.M, d.batch, d.lda, stride(d.batch_stride_a, d.M, d.lda), few.rows ? few.rows : 128) ||
-      !encode_tmap_u8_3d(&tmB, B, d.K, d.N, d.batch, d.ldb, stride(d.batch_stride_b, d.N, d.ldb), 128))
+  constexpr CUtensorMapDataType kCodes = CU_TENSOR_MAP_DATA_TYPE_UINT8;
+  const uint64_t bsa = stride(d.batch_stride_a, d.M, d.lda), bsb = stride(d.batch_stride_b, d.N, d.ldb);
+  if (few.rows) {
+    CUtensorMap tmW, tmX;
+    if (!encode_tmap_128b_3d(&tmX, kCodes, 1, A, d.K, d.M, d.batch, d.lda, bsa, few.rows) ||
+        !encode_tmap_128b_3d(&tmW, kCodes, 1, B, d.K, d.N, d.batch, d.ldb, bsb, 128))
+      return COMFUSE_ERR_CUDA;
+    return launch_gemm_q8_few(d.dtype, few, tmW, tmX, p, st) == cudaSuccess ? COMFUSE_OK : COMFUSE_ERR_CUDA;
+  }
+  const CUtensorMapDataType type = d.dtype == COMFUSE_DTYPE_BF16  ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                   : d.dtype == COMFUSE_DTYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                                  : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+  const int columns = gemm_q8_pair_columns(d.batch, d.M, d.N, d.K, *dev), e = dtype_bytes(d.dtype);
+  const int stored = gemm_q8_stored_columns(d.dtype, d.N);  // (0: no store goes through the map)
+  GemmQ8PairMaps maps;
+  if (!encode_tmap_128b_3d(&maps.A, kCodes, 1, A, d.K, d.M, d.batch, d.lda, bsa, 128) ||
+      !encode_tmap_128b_3d(&maps.B, kCodes, 1, B, d.K, d.N, d.batch, d.ldb, bsb, columns / 2) ||
+      !encode_tmap_128b_3d(&maps.Y, type, e, Y, stored ? stored : d.N, d.M, d.batch, d.ldy, stride(d.batch_stride_y, d.M, d.ldy), 32))
     return COMFUSE_ERR_CUDA;
-  const cudaError_t err = few.rows ? launch_gemm_q8_few(d.dtype, few, tmB, tmA, p, st) : launch_gemm_q8_pair(d.dtype, tmA, tmB, p, *dev, st);
-  return err == cudaSuccess ? COMFUSE_OK : COMFUSE_ERR_CUDA;
+  maps.R = maps.Y;
+  if (residual && !encode_tmap_128b_3d(&maps.R, type, e, residual, d.N, d.M, d.batch, d.ldr, stride(d.batch_stride_r, d.M, d.ldr), 32))
+    return COMFUSE_ERR_CUDA;
+  return launch_gemm_q8_pair(d.dtype, columns, maps, p, *dev, st) == cudaSuccess ? COMFUSE_OK : COMFUSE_ERR_CUDA;
 }
 
 }  // extern "C"
