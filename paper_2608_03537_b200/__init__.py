@@ -517,7 +517,7 @@ def _bound_q8():
         import torch
         b = _bound()
         b.bind_q8(*(ctypes.cast(f, c_void_p).value for f in (lib().comfuse_quantize_rows, lib().comfuse_gemm_q8)),
-                  torch.bfloat16, torch.float16, torch.float32, torch.int8)
+                  torch.bfloat16, torch.float16, torch.float32, torch.int8, torch.Tensor, getattr(torch.Tensor, "__dlpack_c_exchange_api__", None))
         _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _q8 = b
     return _q8

@@ -340,89 +340,142 @@ static PyObject* py_gemm_spec(PyObject* self, PyObject* const* a, Py_ssize_t n) 
 }
 
 // ---- the 8-bit integer layers.  Their tensors have more than one element type, so types, shapes and devices are looked at one by one.
+//
+// Asking a tensor for these through its Python interface takes 0.5 us a tensor, 3.5 of the 7 us that a norm of one token cost its caller.
+// Where the tensor's class offers the DLPack exchange interface (a public, versioned C structure behind a capsule), one call fills in all of
+// them; the Python interface remains for whatever does not.
+typedef struct { uint32_t major, minor; } DlVersion;
+typedef struct {
+  void* data;
+  struct { int32_t type, id; } device;  // type: 1 = host, 2 = CUDA
+  int32_t ndim;
+  struct { uint8_t code, bits; uint16_t lanes; } dtype;  // code: 0 = int, 2 = IEEE float, 4 = bfloat
+  int64_t* shape;
+  int64_t* strides;  // elements; NULL = dense
+  uint64_t byte_offset;
+} DlTensor;
+typedef struct {
+  DlVersion version;
+  void* previous;
+  void *allocate, *managed_from_object, *managed_to_object;
+  int (*tensor_from_object)(void* object, DlTensor* out);  // a view for the length of the call; 0 = filled in, -1 = a Python error is set
+} DlExchange;
+static const DlExchange* dl_exchange;
+static PyTypeObject* dl_type;  // the class whose tensors it takes
 
-// The type of a tensor: `want`, or where that is NULL one of bf16, fp16 and fp32, as a comfuse_dtype_t (0 for a `want` that it is); -1 = refused.
-static int type_of(PyObject* t, PyObject* want, const char* what) {
-  PyObject* d = PyObject_GetAttr(t, s_dtype);
-  if (!d) return -1;
-  Py_DECREF(d);  // (a tensor's type outlives it)
-  if (want ? d == want : (d == t_bf16 || d == t_f16 || d == t_f32)) return want || d == t_bf16 ? COMFUSE_DTYPE_BF16 : d == t_f16 ? COMFUSE_DTYPE_F16 : COMFUSE_DTYPE_F32;
-  PyErr_Format(PyExc_AssertionError, "%s has another element type than the call takes", what);
-  return -1;
+enum { TYPE_BF16 = COMFUSE_DTYPE_BF16, TYPE_F16 = COMFUSE_DTYPE_F16, TYPE_F32 = COMFUSE_DTYPE_F32, TYPE_I8 = 3, TYPE_OTHER = -1 };
+typedef struct {
+  Geometry g;
+  int type;
+  int64_t device;  // -1 = host
+  const void* p;
+} Described;
+
+static int describe(PyObject* t, Described* d) {
+  if (dl_exchange && PyObject_TypeCheck(t, dl_type)) {
+    DlTensor v;
+    if (dl_exchange->tensor_from_object(t, &v) == 0 && v.ndim <= MAX_DIMS) {
+      d->g.n = v.ndim;
+      int64_t dense = 1;
+      for (int i = v.ndim - 1; i >= 0; --i) {
+        d->g.size[i] = v.shape[i];
+        d->g.stride[i] = v.strides ? v.strides[i] : dense;
+        dense *= v.shape[i];
+      }
+      const int code = v.dtype.code, bits = v.dtype.bits;
+      d->type = v.dtype.lanes != 1 ? TYPE_OTHER
+                : code == 4 && bits == 16 ? TYPE_BF16
+                : code == 2 && bits == 16 ? TYPE_F16
+                : code == 2 && bits == 32 ? TYPE_F32
+                : code == 0 && bits == 8  ? TYPE_I8
+                                          : TYPE_OTHER;
+      d->device = v.device.type == 2 ? v.device.id : v.device.type == 1 ? -1 : -2;
+      d->p = (const char*)v.data + v.byte_offset;
+      return 1;
+    }
+    PyErr_Clear();
+  }
+  int n = 0;
+  PyObject* type = PyObject_GetAttr(t, s_dtype);
+  if (!type) return 0;
+  Py_DECREF(type);  // (a tensor's type outlives it)
+  d->type = type == t_bf16 ? TYPE_BF16 : type == t_f16 ? TYPE_F16 : type == t_f32 ? TYPE_F32 : type == t_i8 ? TYPE_I8 : TYPE_OTHER;
+  return shape_of(t, &d->g) && tuple_i64(PyObject_CallMethodNoArgs(t, s_stride), d->g.stride, &n) && method_i64(t, s_get_device, &d->device) && pointer(t, &d->p);
 }
-// A matrix (or a batch of them) of the given type and, where they are given (>= 0), sizes, with a dense last dimension, on `device`.
-static int matrix(PyObject* t, PyObject* type, int64_t device, int64_t batch, int64_t rows, int64_t cols, const char* what, Geometry* g, const void** p) {
-  int64_t at = 0;
-  if (type_of(t, type, what) < 0 || !geometry(t, g) || !method_i64(t, s_get_device, &at) || !pointer(t, p)) return 0;
-  if (g->n > 3 || (g->n == 3) != (batch >= 0) || (batch >= 0 && g->size[0] != batch) || (rows >= 0 && g->size[g->n - 2] != rows) ||
-      (cols >= 0 && g->size[g->n - 1] != cols)) {
-    PyErr_Format(PyExc_AssertionError, "%s has a shape that does not match the call", what);
-    return 0;
-  }
-  if (g->stride[g->n - 1] != 1 && g->size[g->n - 1] != 1) {
-    PyErr_Format(PyExc_AssertionError, "the last dimension of %s must be dense", what);
-    return 0;
-  }
-  if (at != device) {
-    PyErr_Format(PyExc_AssertionError, "%s is not on the current device", what);
-    return 0;
-  }
+static int refuse(const char* what, const char* why) {
+  PyErr_Format(PyExc_AssertionError, "%s %s", what, why);
+  return 0;
+}
+static int fits(const Described* d, int type, int64_t device, int64_t dims, int64_t batch, int64_t rows, int64_t cols, const char* what) {
+  if (d->type != type) return refuse(what, "has another element type than the call takes");
+  if (d->g.n != dims || (batch >= 0 && d->g.size[0] != batch) || (rows >= 0 && d->g.size[d->g.n - 2] != rows) || (cols >= 0 && d->g.size[d->g.n - 1] != cols))
+    return refuse(what, "has a shape that does not match the call");
+  if (d->device != device) return refuse(what, "is not on the current device");
+  return 1;
+}
+// A matrix, or a batch of them (batch >= 0), with the given element type and, where they are given (>= 0), sizes, and a dense last dimension.
+// None, where that may be: a null pointer.
+static int matrix(PyObject* t, int type, int64_t device, int64_t batch, int64_t rows, int64_t cols, const char* what, Described* d) {
+  if (!describe(t, d) || !fits(d, type, device, batch >= 0 ? 3 : 2, batch, rows, cols, what)) return 0;
+  Geometry* g = &d->g;
+  if (g->stride[g->n - 1] != 1 && g->size[g->n - 1] != 1) return refuse(what, "must be dense in its last dimension");
   if (g->size[g->n - 2] == 1) g->stride[g->n - 2] = (g->size[g->n - 1] + 15) / 16 * 16;  // (one row: nothing is addressed by its stride)
   return 1;
 }
-// A dense vector (or [batch, n]) of the given type with n elements; None: a null pointer.
-static int vector(PyObject* t, PyObject* type, int64_t device, int64_t batch, int64_t n, const char* what, const void** p) {
-  Geometry g;
-  int64_t at = 0;
+static int optional_matrix(PyObject* t, int type, int64_t device, int64_t batch, int64_t rows, int64_t cols, const char* what, Described* d) {
+  if (t != Py_None) return matrix(t, type, device, batch, rows, cols, what, d);
+  memset(d->g.stride, 0, 3 * sizeof(int64_t));
+  d->g.n = 3;
+  d->p = NULL;
+  return 1;
+}
+// A dense vector of n elements (or [batch, n]).  None: a null pointer.
+static int vector(PyObject* t, int type, int64_t device, int64_t batch, int64_t n, const char* what, const void** p) {
+  Described d;
   *p = NULL;
   if (t == Py_None) return 1;
-  if (type_of(t, type, what) < 0 || !shape_of(t, &g) || !method_i64(t, s_get_device, &at) || !pointer(t, p)) return 0;
-  if (g.n != (batch >= 0 ? 2 : 1) || (batch >= 0 && g.size[0] != batch) || g.size[g.n - 1] != n) {
-    PyErr_Format(PyExc_AssertionError, "%s has a shape that does not match the call", what);
-    return 0;
-  }
-  if (at != device) {
-    PyErr_Format(PyExc_AssertionError, "%s is not on the current device", what);
-    return 0;
-  }
-  return contiguous(t);
+  if (!describe(t, &d) || !fits(&d, type, device, batch >= 0 ? 2 : 1, batch, -1, n, what)) return 0;
+  if ((d.g.stride[d.g.n - 1] != 1 && n != 1) || (batch > 1 && d.g.stride[0] != n)) return refuse(what, "must be dense");
+  *p = d.p;
+  return 1;
 }
-static PyObject* type_object(int dtype) { return dtype == COMFUSE_DTYPE_BF16 ? t_bf16 : dtype == COMFUSE_DTYPE_F16 ? t_f16 : t_f32; }
+// The element type of an operand that may have several, looked at first.
+static int float_type(const Described* d, const char* what, int* type) {
+  *type = d->type;
+  return d->type == TYPE_BF16 || d->type == TYPE_F16 || d->type == TYPE_F32 ? 1 : refuse(what, "has another element type than the call takes");
+}
 
 // quantize_rows(kind, x, residual, gamma, h, q, scale, values, eps, device, stream) -> status
 static PyObject* py_quantize_rows(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   comfuse_quantize_desc_t d;
-  Geometry X, R = {0}, H = {0}, Q, V = {0};
-  const void *x, *r = NULL, *gamma, *h = NULL, *q, *scale, *v = NULL;
+  Described x, r, h, q, v;
+  const void *gamma, *scale;
   int64_t kind, device;
   double eps;
   void* stream;
+  int type;
   if (!fixed_args(n, 11, "quantize_rows") || !to_i64(a[0], &kind) || !to_i64(a[9], &device) || !to_f64(a[8], &eps)) return NULL;
-  const int dtype = type_of(a[1], NULL, "x");
-  if (dtype < 0) return NULL;
-  PyObject* type = type_object(dtype);
-  if (!matrix(a[1], type, device, -1, -1, -1, "x", &X, &x)) return NULL;
-  const int64_t M = X.size[0], N = X.size[1];
-  if ((a[2] != Py_None && !matrix(a[2], type, device, -1, M, N, "residual", &R, &r)) || !vector(a[3], type, device, -1, N, "gamma", &gamma) ||
-      (a[4] != Py_None && !matrix(a[4], type, device, -1, M, N, "h", &H, &h)) || !matrix(a[5], t_i8, device, -1, M, N, "q", &Q, &q) ||
-      !vector(a[6], t_f32, device, -1, M, "scale", &scale) || (a[7] != Py_None && !matrix(a[7], t_bf16, device, -1, M, N, "values", &V, &v)) ||
-      !stream_of(a[10], &stream))
+  if (!describe(a[1], &x) || !float_type(&x, "x", &type) || !matrix(a[1], type, device, -1, -1, -1, "x", &x)) return NULL;
+  const int64_t M = x.g.size[0], N = x.g.size[1];
+  if (!optional_matrix(a[2], type, device, -1, M, N, "residual", &r) || !vector(a[3], type, device, -1, N, "gamma", &gamma) ||
+      !optional_matrix(a[4], type, device, -1, M, N, "h", &h) || !matrix(a[5], TYPE_I8, device, -1, M, N, "q", &q) ||
+      !vector(a[6], TYPE_F32, device, -1, M, "scale", &scale) || !optional_matrix(a[7], TYPE_BF16, device, -1, M, N, "values", &v) || !stream_of(a[10], &stream))
     return NULL;
   if (!require(M <= INT32_MAX && N <= INT32_MAX, "sizes are 32-bit numbers")) return NULL;
   memset(&d, 0, sizeof(d));
   d.kind = (int32_t)kind;
-  d.dtype = dtype;
+  d.dtype = type;
   d.rows = (int32_t)M;
   d.N = (int32_t)N;
-  d.ldx = X.stride[0];
-  d.ldr = r ? R.stride[0] : 0;
-  d.ldh = h ? H.stride[0] : 0;
-  d.ldq = Q.stride[0];
-  d.ldv = v ? V.stride[0] : 0;
+  d.ldx = x.g.stride[0];
+  d.ldr = r.g.stride[0];
+  d.ldh = h.g.stride[0];
+  d.ldq = q.g.stride[0];
+  d.ldv = v.g.stride[0];
   d.eps = (float)eps;
   comfuse_status_t st;
   Py_BEGIN_ALLOW_THREADS
-  st = f_quantize_rows(&d, x, r, gamma, (void*)h, (int8_t*)q, (float*)scale, (void*)v, stream);
+  st = f_quantize_rows(&d, x.p, r.p, gamma, (void*)h.p, (int8_t*)q.p, (float*)scale, (void*)v.p, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong((long)st);
 }
@@ -430,22 +483,21 @@ static PyObject* py_quantize_rows(PyObject* self, PyObject* const* a, Py_ssize_t
 // gemm_q8(A, scale_a, B, scale_b, Y, bias, residual, activation, device, stream) -> status
 static PyObject* py_gemm_q8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   comfuse_gemm_q8_desc_t d;
-  Geometry A, B, Y, R = {0};
-  const void *pA, *pB, *pY, *sa, *sb, *bias, *r = NULL;
+  Described A, B, Y, r;
+  const void *sa, *sb, *bias;
   int64_t activation, device;
   void* stream;
+  int type;
   if (!fixed_args(n, 10, "gemm_q8") || !to_i64(a[7], &activation) || !to_i64(a[8], &device)) return NULL;
-  const int dtype = type_of(a[4], NULL, "Y");
-  if (dtype < 0 || !shape_of(a[0], &A)) return NULL;
-  PyObject* type = type_object(dtype);
-  const int64_t batch = A.n == 3 ? A.size[0] : -1;
-  if (!matrix(a[0], t_i8, device, batch, -1, -1, "A", &A, &pA)) return NULL;
-  const int64_t M = A.size[A.n - 2], K = A.size[A.n - 1];
-  if (!matrix(a[2], t_i8, device, batch, -1, K, "B", &B, &pB)) return NULL;
-  const int64_t N = B.size[B.n - 2];
-  if (!vector(a[1], t_f32, device, batch, M, "scale_a", &sa) || !vector(a[3], t_f32, device, batch, N, "scale_b", &sb) ||
-      !matrix(a[4], type, device, batch, M, N, "Y", &Y, &pY) || !vector(a[5], type, device, -1, N, "bias", &bias) ||
-      (a[6] != Py_None && !matrix(a[6], type, device, batch, M, N, "residual", &R, &r)) || !stream_of(a[9], &stream))
+  if (!describe(a[0], &A) || !describe(a[4], &Y) || !float_type(&Y, "Y", &type)) return NULL;
+  const int64_t batch = A.g.n == 3 ? A.g.size[0] : -1;
+  if (!matrix(a[0], TYPE_I8, device, batch, -1, -1, "A", &A)) return NULL;
+  const int64_t M = A.g.size[A.g.n - 2], K = A.g.size[A.g.n - 1];
+  if (!matrix(a[2], TYPE_I8, device, batch, -1, K, "B", &B)) return NULL;
+  const int64_t N = B.g.size[B.g.n - 2];
+  if (!vector(a[1], TYPE_F32, device, batch, M, "scale_a", &sa) || !vector(a[3], TYPE_F32, device, batch, N, "scale_b", &sb) ||
+      !matrix(a[4], type, device, batch, M, N, "Y", &Y) || !vector(a[5], type, device, -1, N, "bias", &bias) ||
+      !optional_matrix(a[6], type, device, batch, M, N, "residual", &r) || !stream_of(a[9], &stream))
     return NULL;
   if (!require(batch <= INT32_MAX && M <= INT32_MAX && N <= INT32_MAX && K <= INT32_MAX, "sizes are 32-bit numbers")) return NULL;
   memset(&d, 0, sizeof(d));
@@ -453,36 +505,58 @@ static PyObject* py_gemm_q8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   d.M = (int32_t)M;
   d.N = (int32_t)N;
   d.K = (int32_t)K;
-  d.lda = A.stride[A.n - 2];
-  d.ldb = B.stride[B.n - 2];
-  d.ldy = Y.stride[Y.n - 2];
-  d.ldr = r ? R.stride[R.n - 2] : 0;
+  d.lda = A.g.stride[A.g.n - 2];
+  d.ldb = B.g.stride[B.g.n - 2];
+  d.ldy = Y.g.stride[Y.g.n - 2];
+  d.ldr = r.g.stride[r.g.n - 2];
   if (batch >= 0) {
-    d.batch_stride_a = A.stride[0];
-    d.batch_stride_b = B.stride[0];
-    d.batch_stride_y = Y.stride[0];
-    d.batch_stride_r = r ? R.stride[0] : 0;
+    d.batch_stride_a = A.g.stride[0];
+    d.batch_stride_b = B.g.stride[0];
+    d.batch_stride_y = Y.g.stride[0];
+    d.batch_stride_r = r.g.stride[0];
   }
-  d.dtype = dtype;
+  d.dtype = type;
   d.activation = (int32_t)activation;
   comfuse_status_t st;
   Py_BEGIN_ALLOW_THREADS
-  st = f_gemm_q8(&d, (const int8_t*)pA, (const float*)sa, (const int8_t*)pB, (const float*)sb, bias, r, (void*)pY, stream);
+  st = f_gemm_q8(&d, (const int8_t*)A.p, (const float*)sa, (const int8_t*)B.p, (const float*)sb, bias, r.p, (void*)Y.p, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong((long)st);
 }
 
-// bind_q8(address of comfuse_quantize_rows, of comfuse_gemm_q8, the tensor library's bf16, fp16, fp32 and int8 types)
+// describe(tensor) -> (element type, device, address, shape, strides), as the 8-bit entry points see it
+static PyObject* py_describe(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Described d;
+  if (!fixed_args(n, 1, "describe") || !describe(a[0], &d)) return NULL;
+  PyObject *size = PyTuple_New(d.g.n), *stride = PyTuple_New(d.g.n);
+  for (int i = 0; size && stride && i < d.g.n; ++i) {
+    PyTuple_SET_ITEM(size, i, PyLong_FromLongLong(d.g.size[i]));
+    PyTuple_SET_ITEM(stride, i, PyLong_FromLongLong(d.g.stride[i]));
+  }
+  return Py_BuildValue("iLKNN", d.type, (long long)d.device, (unsigned long long)(uintptr_t)d.p, size, stride);
+}
+
+// bind_q8(address of comfuse_quantize_rows, of comfuse_gemm_q8, the tensor library's bf16, fp16, fp32 and int8 types, its tensor class, the class's
+// DLPack exchange capsule or None)
 static PyObject* py_bind_q8(PyObject* self, PyObject* args) {
   unsigned long long r, g;
-  PyObject* t[4];
-  if (!PyArg_ParseTuple(args, "KKOOOO", &r, &g, t, t + 1, t + 2, t + 3)) return NULL;
+  PyObject *t[4], *type, *capsule;
+  if (!PyArg_ParseTuple(args, "KKOOOOO!O", &r, &g, t, t + 1, t + 2, t + 3, &PyType_Type, &type, &capsule)) return NULL;
   f_quantize_rows = (quantize_rows_fn)(uintptr_t)r;
   f_gemm_q8 = (gemm_q8_fn)(uintptr_t)g;
   t_bf16 = Py_NewRef(t[0]);
   t_f16 = Py_NewRef(t[1]);
   t_f32 = Py_NewRef(t[2]);
   t_i8 = Py_NewRef(t[3]);
+  dl_exchange = NULL;
+  if (capsule != Py_None) {
+    const DlExchange* e = PyCapsule_GetPointer(capsule, "dlpack_exchange_api");
+    if (!e) return NULL;
+    if (e->version.major == 1 && e->tensor_from_object) {  // (a minor version only adds to the end)
+      dl_type = (PyTypeObject*)Py_NewRef(type);
+      dl_exchange = e;
+    }
+  }
   Py_RETURN_NONE;
 }
 
@@ -503,6 +577,7 @@ static PyMethodDef methods[] = {
     {"b2b", (PyCFunction)(void (*)(void))py_b2b, METH_FASTCALL, NULL},
     {"gemm_spec", (PyCFunction)(void (*)(void))py_gemm_spec, METH_FASTCALL, NULL},
     {"bind_q8", py_bind_q8, METH_VARARGS, NULL},
+    {"describe", (PyCFunction)(void (*)(void))py_describe, METH_FASTCALL, NULL},
     {"quantize_rows", (PyCFunction)(void (*)(void))py_quantize_rows, METH_FASTCALL, NULL},
     {"gemm_q8", (PyCFunction)(void (*)(void))py_gemm_q8, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};

@@ -10,7 +10,6 @@
 // TMA; the residual comes in the same way, into the box that its sum leaves from.  A TMA store writes whole 16-byte units (measured: up to
 // seven bf16 behind the last column), so Y's map ends at the last whole unit and the columns behind it are stored one by one.
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "q8_common.cuh"
@@ -58,7 +57,7 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();  // which half of the pair
-  const long long cluster_id = blockIdx.x >> 1, clusters = gridDim.x >> 1;
+  const uint32_t cluster_id = blockIdx.x >> 1, clusters = gridDim.x >> 1, tiles = static_cast<uint32_t>(p.tiles);  // (the host keeps them below 2^31)
   const int KB = (p.K + 127) >> 7;
   const WaitCtx w{s_abort, p.status, p.timeout_ns};
   griddep_launch_dependents();  // the next kernel's set-up may overlap this kernel (it waits before touching memory)
@@ -94,15 +93,13 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
   griddep_wait();
 
   // tile -> batch, first row and column: bands of 8 row blocks, in a band column by column
-  auto decode = [&](long long tile, int& b, int& m0, int& n0) {
-    const long long per = static_cast<long long>(p.mtiles) * p.ntiles;
-    b = static_cast<int>(tile / per);
-    const long long t = tile - b * per;
-    const long long band = t / (8ll * p.ntiles);
-    const int in_band = static_cast<int>(t - band * 8 * p.ntiles), first = static_cast<int>(band * 8);
-    const int high = p.mtiles - first < 8 ? p.mtiles - first : 8;
-    n0 = (in_band / high) * BN;
-    m0 = (first + in_band % high) * 256;
+  auto decode = [&](uint32_t tile, int& b, int& m0, int& n0) {
+    const uint32_t per = static_cast<uint32_t>(p.mtiles) * static_cast<uint32_t>(p.ntiles), bt = tile / per, t = tile - bt * per;
+    const uint32_t size = 8u * static_cast<uint32_t>(p.ntiles), band = t / size, in_band = t - band * size, first = band * 8;
+    const uint32_t high = p.mtiles - first < 8 ? p.mtiles - first : 8, column = in_band / high;
+    b = static_cast<int>(bt);
+    n0 = static_cast<int>(column) * BN;
+    m0 = static_cast<int>(first + in_band - column * high) * 256;
   };
 
   if (warp == 0) {
@@ -111,7 +108,7 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (long long tile = cluster_id; tile < p.tiles && ok; tile += clusters) {
+      for (uint32_t tile = cluster_id; tile < tiles && ok; tile += clusters) {
         int b, m0, n0;
         decode(tile, b, m0, n0);
         for (int kb = 0; kb < KB; ++kb) {
@@ -131,7 +128,7 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
       uint32_t phase = 0, n = 0;
       bool ok = true;
       constexpr uint32_t idesc = make_idesc_i8(256, BN);
-      for (long long tile = cluster_id; tile < p.tiles && ok; tile += clusters, ++n) {
+      for (uint32_t tile = cluster_id; tile < tiles && ok; tile += clusters, ++n) {
         const uint32_t slot = n & 1u;
         if (!mbar_wait<false>(bar_tempty(slot), ((n >> 1) & 1u) ^ 1u, w)) break;
         tcgen05_fence_after_sync();
@@ -161,22 +158,29 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
     float2* s_vec = reinterpret_cast<float2*>(smem + Cfg::OFF_VEC);
     const int whole = gemm_q8_stored_columns(DT, p.N);  // by TMA
     uint32_t n = 0, count = 0;  // tiles, and boxes of this warp
-    for (long long tile = cluster_id; tile < p.tiles; tile += clusters, ++n) {
-      int b, m0, n0;
+    // What a tile needs from global memory is asked for under the tile before: the scale and bias of one of its channels, the row's scale.
+    const int i = static_cast<int>(threadIdx.x) - 64;  // 256 threads, BN channels
+    int b = 0, m0 = 0, n0 = 0;
+    float sa = 0.f;
+    float2 vec = make_float2(0.f, 0.f);
+    auto fetch = [&](uint32_t tile) {
+      if (tile >= tiles) return;
       decode(tile, b, m0, n0);
-      const uint32_t slot = n & 1u;
-      for (int i = static_cast<int>(threadIdx.x) - 64; i < BN; i += 32 * Cfg::kEpiWarps) {
-        const int c = n0 + i;
-        float2 v = make_float2(0.f, 0.f);
-        if (c < p.N) {
-          v.x = __ldg(p.scale_b + static_cast<long long>(b) * p.N + c);
-          if (p.bias) v.y = Elem<DT>::get(p.bias, c);
-        }
-        s_vec[slot * BN + i] = v;  // (the barrier below keeps the warps within one tile of each other)
+      const int row = m0 + static_cast<int>(rank) * 128 + q * 32 + lane, c = n0 + i;
+      sa = row < p.M ? __ldg(p.scale_a + static_cast<long long>(b) * p.M + row) : 0.f;
+      if (i < BN) {
+        vec.x = c < p.N ? __ldg(p.scale_b + static_cast<long long>(b) * p.N + c) : 0.f;
+        vec.y = p.bias && c < p.N ? Elem<DT>::get(p.bias, c) : 0.f;
       }
+    };
+    fetch(cluster_id);
+    for (uint32_t tile = cluster_id; tile < tiles; tile += clusters, ++n) {
+      const uint32_t slot = n & 1u;
+      if (i < BN) s_vec[slot * BN + i] = vec;  // (the barrier below keeps the warps within one tile of each other)
+      const int tb = b, row0 = m0 + static_cast<int>(rank) * 128 + q * 32, col0 = n0 + half * (BN / 2);
+      const float tsa = sa;
+      fetch(tile + clusters);
       named_barrier_sync(1, 32 * Cfg::kEpiWarps);
-      const int row0 = m0 + static_cast<int>(rank) * 128 + q * 32, col0 = n0 + half * (BN / 2);
-      const float sa = row0 + lane < p.M ? __ldg(p.scale_a + static_cast<long long>(b) * p.M + row0 + lane) : 0.f;
       const int left = row0 < p.M && col0 < p.N ? (p.N - col0 + E - 1) / E : 0;
       const int boxes = left < BN / 2 / E ? left : BN / 2 / E;  // that hold anything of Y
       // box k of this tile: once its staging box has been read out by the store before last, ask for the residual
@@ -186,7 +190,7 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
           else tma_store_wait_read<BOXES - 2 < 0 ? 0 : BOXES - 2>();
           const uint32_t sel = (count + k) % BOXES;
           mbar_arrive_expect_tx(bar_res(e, sel), Cfg::BOX_BYTES);
-          tma_load_3d(box0 + sel * Cfg::BOX_BYTES, &maps.R, bar_res(e, sel), col0 + k * E, row0, b);
+          tma_load_3d(box0 + sel * Cfg::BOX_BYTES, &maps.R, bar_res(e, sel), col0 + k * E, row0, tb);
         }
       };
       ask(0);
@@ -212,10 +216,10 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
           if (k == boxes - 1 && h == E / 32 - 1) release();
           float z[32];
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const float4 sv = *reinterpret_cast<const float4*>(s_vec + slot * BN + local + i);
-            z[i] = fmaf(static_cast<float>(static_cast<int>(v[i])) * sv.x, sa, sv.y);
-            z[i + 1] = fmaf(static_cast<float>(static_cast<int>(v[i + 1])) * sv.z, sa, sv.w);
+          for (int j = 0; j < 32; j += 2) {
+            const float4 sv = *reinterpret_cast<const float4*>(s_vec + slot * BN + local + j);
+            z[j] = fmaf(static_cast<float>(static_cast<int>(v[j])) * sv.x, tsa, sv.y);
+            z[j + 1] = fmaf(static_cast<float>(static_cast<int>(v[j + 1])) * sv.z, tsa, sv.w);
           }
           activate(z, p.activation);
           if (h == 0) {  // the staging box is this warp's again
@@ -242,7 +246,7 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
           }
           const int col = col0 + k * E + h * 32;
           if (col + 32 > whole && ok && row0 + lane < p.M) {
-            void* out = static_cast<char*>(p.Y) + (b * p.batch_stride_y + static_cast<long long>(row0 + lane) * p.ldy) * Elem<DT>::kBytes;
+            void* out = static_cast<char*>(p.Y) + (tb * p.batch_stride_y + static_cast<long long>(row0 + lane) * p.ldy) * Elem<DT>::kBytes;
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if (col + i >= whole && col + i < p.N) Elem<DT>::put(out, col + i, z[i]);
@@ -257,7 +261,7 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
         __syncwarp();
         if (lane == 0) {
           const int col = col0 + k * E;
-          if (ok && col < whole && COMFUSE_IN_BOUNDS(col < p.N && row0 < p.M && b < p.batch, p.status)) tma_store_3d(&maps.Y, box0 + sel * Cfg::BOX_BYTES, col, row0, b);
+          if (ok && col < whole && COMFUSE_IN_BOUNDS(col < p.N && row0 < p.M && tb < p.batch, p.status)) tma_store_3d(&maps.Y, box0 + sel * Cfg::BOX_BYTES, col, row0, tb);
           tma_store_commit();
         }
       }
@@ -304,18 +308,20 @@ cudaError_t launch_instance(const GemmQ8PairMaps& maps, const GemmQ8Params& p, c
   return cudaLaunchKernelEx(&cfg, kern, maps, p);
 }
 
+// Columns of a tile, stages of the ring, staging boxes an epilogue warp.  Behind a long contraction the ring's depth is what counts (8192 x 4096 x
+// 4096 with 5 / 4 / 3 stages: 92 / 99 / 112 us), behind a short one the stores (96 x 504 x 504 x 64 with 1 / 2 boxes: 21 / 19 us in bf16).
 template <int DT>
 cudaError_t launch_columns(int columns, const GemmQ8PairMaps& maps, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
   if (columns == 128) return launch_instance<DT, 128, 6, 2>(maps, p, dev, stream);
-  return launch_instance<DT, 256, 5, 1>(maps, p, dev, stream);
+  return p.K <= 1024 ? launch_instance<DT, 256, 4, 2>(maps, p, dev, stream) : launch_instance<DT, 256, 5, 1>(maps, p, dev, stream);
 }
 
 }  // namespace
 
-int gemm_q8_pair_columns(int batch, int M, int N, int K, const DeviceInfo& dev) {
-  if (getenv("TC")) return atoi(getenv("TC"));
-  const long long blocks = static_cast<long long>(batch) * ((M + 255) / 256);
-  return 2 * blocks * ((N + 255) / 256) <= dev.sm_count / 2 || N <= 128 ? 128 : 256;
+int gemm_q8_pair_columns(int batch, int M, int N, const DeviceInfo& dev) {
+  // Narrow tiles where they still run in one round: 512 x 4096 x 4096 13.0 us with tiles of 128 columns, 17.5 with 256, but 768 rows, two rounds, 18.7 / 17.0.
+  const long long tiles = static_cast<long long>(batch) * ((M + 255ll) / 256) * ((N + 255) / 256);
+  return 2 * tiles <= dev.sm_count / 2 || N <= 128 ? 128 : 256;
 }
 
 cudaError_t launch_gemm_q8_pair(int dtype, int columns, const GemmQ8PairMaps& maps, GemmQ8Params p, const DeviceInfo& dev, cudaStream_t stream) {

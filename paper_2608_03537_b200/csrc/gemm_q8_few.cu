@@ -1,12 +1,12 @@
 // The 8-bit integer product for few rows: Y = act(sa sb (A . B^T) + bias) + R.
 //
 // What bounds it: the weights' bytes, and for small layers the latency of one pass.  As in the bf16 form for few rows the product is turned
-// round: the weights are the UMMA's 128-row operand, the rows its N operand (MT = 16 .. 256), so a CTA computes 128 channels of MT rows
+// round: the weights are the UMMA's 128-row operand, the rows its N operand (MT = 16 .. 128), so a CTA computes 128 channels of MT rows
 // and the tensor core's work follows the rows that exist.  A cluster of `split` CTAs shares a tile's contraction.  Their int32
 // accumulators go to shared memory as [row][channel]; behind a cluster barrier each CTA adds its slice of the rows from all of them through
 // distributed shared memory and finishes it, a warp per row and 4 channels per lane.  Integer sums are exact, so the split changes no bit
 // of the result.
-#include <cstdlib>
+#include <algorithm>
 #include <type_traits>
 
 #include "q8_common.cuh"
@@ -22,22 +22,22 @@ struct FewCfg {
   static constexpr int W_BYTES = 128 * 128;  // weights of one K block: 128 channels x 128 bytes
   static constexpr int X_BYTES = MT * 128;
   static constexpr int STAGE_BYTES = W_BYTES + X_BYTES;
-  // up to 64 rows: two CTAs share an SM, so that tiles x split need not be a multiple of the SMs
-  static constexpr int PER_SM = MT <= 64 ? 2 : 1;
   static constexpr int MISC_BYTES = 256 + 1024;
-  static constexpr int NSTAGES = (233472 / PER_SM - 1024 - MISC_BYTES) / STAGE_BYTES > 10 ? 10 : (233472 / PER_SM - 1024 - MISC_BYTES) / STAGE_BYTES;
+  // The ring takes all of an SM: its depth is worth more than a second CTA beside it, which would even out the SMs' shares (40 x 4096 x 4096 with
+  // 9 stages 7.7 us, with 4 stages and two CTAs an SM 8.8; 64 x 4096 x 16384 15.6 / 18.5; 40 x 16384 x 4096 14.9 / 15.6).
+  static constexpr int NSTAGES = (232448 - MISC_BYTES) / STAGE_BYTES > 10 ? 10 : (232448 - MISC_BYTES) / STAGE_BYTES;
+  static constexpr int ASK = 8;  // 128 KB of weights
   static constexpr int OFF_BAR = NSTAGES * STAGE_BYTES;
   static constexpr int SMEM_BYTES = OFF_BAR + MISC_BYTES;
   static constexpr int ROW_BYTES = 128 * 4;  // one row of the tile's accumulators
   static constexpr int TMEM_COLS = MT <= 32 ? 32 : MT;
   static_assert(MT * ROW_BYTES <= NSTAGES * STAGE_BYTES, "the accumulators are staged in the idle ring");
   static_assert((2 * NSTAGES + 1) * 8 + 16 <= 256, "barrier room");
-  static_assert(PER_SM * TMEM_COLS <= 512, "tensor memory");
-  static_assert(SMEM_BYTES <= 232448, "shared memory");
+  static_assert(SMEM_BYTES <= 232448 && SMEM_BYTES > 116 * 1024, "one CTA per SM (tensor-memory allocation never waits)");
 };
 
 template <int DT, int MT>
-__global__ void __launch_bounds__(FewCfg<MT>::kThreads) gemm_q8_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
+__global__ void __launch_bounds__(FewCfg<MT>::kThreads, 1) gemm_q8_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX,
                                                                           const GemmQ8Params p) {
   using Cfg = FewCfg<MT>;
   constexpr int NSTAGES = Cfg::NSTAGES;
@@ -75,6 +75,13 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads) gemm_q8_few_kernel(const
     fence_mbar_init();
     prefetch_tensormap(&tmW);
     prefetch_tensormap(&tmX);
+  }
+  // The weights are asked of the L2 while the previous kernel may still run (a prefetch returns nothing, so it may stand in front of the wait
+  // whoever writes them: writes meet in the L2 too): 128 KB a CTA, by one group of rows.  us with weights from memory, without / with: 8 x 4096 x 4096
+  // 7.0 / 6.8, 40 x 16384 x 4096 14.9 / 14.7, 64 x 1024 x 4096 6.3 / 6.0; 128 rows 10.7 / 10.9, so not there.
+  if (MT <= 64 && warp == 2 && grp == 0 && elect_one()) {
+#pragma unroll 1
+    for (int kb = kb0; kb < kb1 && kb < kb0 + Cfg::ASK; ++kb) tma_prefetch_l2_3d(&tmW, kb * 128, n0, b);
   }
   if (warp == 1) {
     tmem_alloc(smem_u32(s_tmem_base), Cfg::TMEM_COLS);
@@ -286,8 +293,7 @@ cudaError_t launch_rows(int rows, const CUtensorMap& tmW, const CUtensorMap& tmX
     case 16: return launch_instance<DT, 16>(tmW, tmX, p, stream);
     case 32: return launch_instance<DT, 32>(tmW, tmX, p, stream);
     case 64: return launch_instance<DT, 64>(tmW, tmX, p, stream);
-    case 128: return launch_instance<DT, 128>(tmW, tmX, p, stream);
-    default: return launch_instance<DT, 256>(tmW, tmX, p, stream);
+    default: return launch_instance<DT, 128>(tmW, tmX, p, stream);
   }
 }
 
@@ -295,18 +301,22 @@ cudaError_t launch_rows(int rows, const CUtensorMap& tmW, const CUtensorMap& tmX
 
 GemmQ8FewPlan gemm_q8_few_plan(int batch, int M, int N, int K, const DeviceInfo& dev) {
   GemmQ8FewPlan c;
-  if (getenv("TR")) c.rows = atoi(getenv("TR")); else
-  c.rows = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
-  const long long tiles = static_cast<long long>(batch) * ((M + c.rows - 1) / c.rows) * ((N + 127) / 128);
-  const long long slots = static_cast<long long>(dev.sm_count) * (c.rows <= 64 ? 2 : 1);
-  if (getenv("TC")) { c.rows = 0; return c; }
-  if (tiles > slots && !getenv("TR")) {
-    c.rows = 0;
-    return c;
-  }
   const int KB = (K + 127) / 128;
-  if (getenv("TS")) { c.split = atoi(getenv("TS")); return c; }
-  while (c.split < 8 && tiles * c.split * 2 <= slots && KB >= 4 * c.split) c.split *= 2;
+  c.rows = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+  const long long tiles = static_cast<long long>(batch) * ((M + c.rows - 1ll) / c.rows) * ((N + 127) / 128);
+  const int most = tiles < dev.sm_count ? static_cast<int>(dev.sm_count / tiles) : 1;
+  // Shares: while one keeps 4 K blocks, and behind less than 64 K blocks no more than fill two thirds of the SMs.  us with 1 / 2 / 3 / 4 shares
+  // (40 rows): 4096 x 4096 9.5 / 7.7 / 7.7 / 8.0, 4096 x 16384 23.0 / 16.4 / 15.2 / 15.3, 1024 x 1024 4.8 / 4.3 / 4.4 / 4.5.
+  const long long want = KB >= 64 ? most : 2ll * dev.sm_count / 3 / tiles;
+  c.split = static_cast<int>(std::min<long long>({8, most, std::max<long long>(want, 2), std::max(KB / 4, 1)}));
+  // Where the rows fill 64 and more of the UMMA's columns the tile kernel is in reach: both times by their K blocks, fitted to 64 .. 256 rows
+  // (4096 x 4096, 256 rows: 12.1 us here, 11.9 there; 4096 x 16384 22.4 / 32.7; 1024 x 1024 7.2 / 6.2; 16384 x 4096 36 / 22).
+  if (M > 64) {
+    const long long here = (tiles * c.split + dev.sm_count - 1) / dev.sm_count, pairs = dev.sm_count / 2;
+    const long long there = (static_cast<long long>(batch) * ((M + 255ll) / 256) * ((N + 127) / 128) + pairs - 1) / pairs;
+    if (here * (6.5 + 0.25 * KB / c.split) >= 3.5 + there * std::max(0.26 * KB, 1.7)) c.rows = 0;
+  }
+  if (tiles * c.split > 0x7FFFFFFF) c.rows = 0;  // (a grid is counted in 32 bits)
   return c;
 }
 

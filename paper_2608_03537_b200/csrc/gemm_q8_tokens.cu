@@ -10,7 +10,6 @@
 //   * `split` warps of a CTA share the contraction of their channels, 128 bytes in turn, so that small layers fill the SMs.  U steps of
 //     weights are asked for at once: 8 KB a warp.
 //   * The shares meet in shared memory; the sums are exact in any order.
-#include <cstdlib>
 #include <type_traits>
 
 #include "q8_common.cuh"
@@ -61,6 +60,15 @@ __global__ void __launch_bounds__(32 * kWarps, 2) gemm_q8_tokens_kernel(const Ge
   for (int i = 0; i < NT; ++i) {
     const int m = 8 * i + (lane >> 2);
     x[i] = A + (m < p.M ? m : p.M - 1) * t.lda;
+  }
+  // The first round of weights is asked of the L2 while the previous kernel may still run (a prefetch returns nothing, so it may stand in front of
+  // the wait whoever writes them): 16 channels x U steps of one line, two lines a lane.
+  {
+    const int k = share * 128 + (lane & 3) * p.split * 128;
+    if (k < p.K) {
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(w0 + k));
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(w1 + k));
+    }
   }
   griddep_wait();
 
@@ -137,20 +145,26 @@ cudaError_t launch_instance(const GemmQ8TokensParams& t, const GemmQ8Params& p, 
 template <int DT>
 cudaError_t launch_rows(const GemmQ8TokensParams& t, const GemmQ8Params& p, cudaStream_t stream) {
   if (p.M <= 8) return launch_instance<DT, 1>(t, p, stream);
-  if (p.M <= 16) return launch_instance<DT, 2>(t, p, stream);
-  return launch_instance<DT, 4>(t, p, stream);
+  return launch_instance<DT, 2>(t, p, stream);
 }
 
 }  // namespace
 
-bool gemm_q8_tokens_fits(int batch, int M) { return M <= kGemmQ8Tokens && batch <= 65535; }
+bool gemm_q8_tokens_fits(int batch, int M, int N, int K, const DeviceInfo& dev) {
+  if (M > kGemmQ8Tokens || batch > 65535) return false;
+  // Where the weights are many enough that their stream is all that counts, the other form's deeper ring is ahead, up to one round of its
+  // 128-channel tiles.  us, this form / that one: 1 row 4096 x 4096 5.5 / 6.7, 16384 x 4096 13.2 / 12.5, 65536 x 4096 43.6 / 48.9; 8 rows 6.0 / 6.8,
+  // 14.6 / 12.8, 49.9 / 50.2; 16 rows 1024 x 1024 2.8 / 3.8, 4096 x 4096 6.7 / 6.9, 16384 x 4096 17.6 / 13.1.
+  const long long codes = static_cast<long long>(batch) * N * K, tiles = static_cast<long long>(batch) * ((N + 127) / 128);
+  return M <= 8 ? codes <= 3ll << 24 || tiles > dev.sm_count : codes <= 1ll << 25;
+}
 
 cudaError_t launch_gemm_q8_tokens(int dtype, const GemmQ8TokensParams& t, GemmQ8Params p, const DeviceInfo& dev, cudaStream_t stream) {
-  // shares: until there are 16 warps for each SM, while a share keeps a round of loads
+  // Shares: up to the 16 warps that an SM holds, while each has a step.  us with 1 / 2 / 4 / 8 shares (8 rows): 4096 x 4096 12.9 / 9.8 / 7.0 / 5.9,
+  // 16384 x 4096 18.2 / 14.0 / 14.7 / 15.9, 1024 x 1024 5.1 / 3.3 / 2.9 / 2.4.
   const long long groups = static_cast<long long>(p.batch) * ((p.N + kChannels - 1) / kChannels);
   p.split = 1;
-  while (p.split < kWarps && groups * p.split < 16ll * dev.sm_count && p.K > p.split * 128) p.split *= 2;
-  if (getenv("TS")) p.split = atoi(getenv("TS"));
+  while (p.split < kWarps && groups * p.split * 2 <= 18ll * dev.sm_count && p.K > p.split * 128) p.split *= 2;
   switch (dtype) {
     case COMFUSE_DTYPE_BF16: return launch_rows<COMFUSE_DTYPE_BF16>(t, p, stream);
     case COMFUSE_DTYPE_F16: return launch_rows<COMFUSE_DTYPE_F16>(t, p, stream);

@@ -1,6 +1,5 @@
 // C entry points of the 8-bit integer layers: argument checks, tensor maps, choice of the form.
 #include <cmath>
-#include <cstdlib>
 
 #include "../../include/comfuse.h"
 #include "q8_params.h"
@@ -103,7 +102,7 @@ comfuse_status_t comfuse_gemm_q8(const comfuse_gemm_q8_desc_t* desc, const int8_
   p.status = dev->status_word;
   p.timeout_ns = timeout_ns();
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (few_rows_enabled() && gemm_q8_tokens_fits(d.batch, d.M) && !getenv("TR")) {
+  if (few_rows_enabled() && gemm_q8_tokens_fits(d.batch, d.M, d.N, d.K, *dev)) {
     const GemmQ8TokensParams t = {A, B, d.lda, d.ldb, d.batch > 1 ? d.batch_stride_a : 0, d.batch > 1 ? d.batch_stride_b : 0};
     return launch_gemm_q8_tokens(d.dtype, t, p, *dev, st) == cudaSuccess ? COMFUSE_OK : COMFUSE_ERR_CUDA;
   }
@@ -121,7 +120,8 @@ comfuse_status_t comfuse_gemm_q8(const comfuse_gemm_q8_desc_t* desc, const int8_
   const CUtensorMapDataType type = d.dtype == COMFUSE_DTYPE_BF16  ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                    : d.dtype == COMFUSE_DTYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                                                   : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
-  const int columns = gemm_q8_pair_columns(d.batch, d.M, d.N, d.K, *dev), e = dtype_bytes(d.dtype);
+  if (static_cast<long long>(d.batch) * ((d.M + 255ll) / 256) * ((d.N + 127) / 128) > 0x7FFFFFFF) return COMFUSE_ERR_UNSUPPORTED;  // (tiles are counted in 32 bits)
+  const int columns = gemm_q8_pair_columns(d.batch, d.M, d.N, *dev), e = dtype_bytes(d.dtype);
   const int stored = gemm_q8_stored_columns(d.dtype, d.N);  // (0: no store goes through the map)
   GemmQ8PairMaps maps;
   if (!encode_tmap_128b_3d(&maps.A, kCodes, 1, A, d.K, d.M, d.batch, d.lda, bsa, 128) ||

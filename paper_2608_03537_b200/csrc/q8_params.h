@@ -37,15 +37,15 @@ struct GemmQ8Params {
 };
 
 // A handful of rows: the operands themselves (the other forms read them through tensor maps).
-constexpr int kGemmQ8Tokens = 32;
+constexpr int kGemmQ8Tokens = 16;
 struct GemmQ8TokensParams {
   const int8_t *A, *B;
   long long lda, ldb, batch_stride_a, batch_stride_b;
 };
-bool gemm_q8_tokens_fits(int batch, int M);
+bool gemm_q8_tokens_fits(int batch, int M, int N, int K, const DeviceInfo& dev);
 cudaError_t launch_gemm_q8_tokens(int dtype, const GemmQ8TokensParams& t, GemmQ8Params p, const DeviceInfo& dev, cudaStream_t stream);
 
-// Few rows: rows per group (the UMMA's N: 16, 32, 64, 128 or 256) and CTAs that share a contraction; rows = 0: the call does not take this form.
+// Few rows: rows per group (the UMMA's N: 16, 32, 64 or 128) and CTAs that share a contraction; rows = 0: the call does not take this form.
 struct GemmQ8FewPlan {
   int rows = 0, split = 1;
 };
@@ -56,7 +56,7 @@ cudaError_t launch_gemm_q8_few(int dtype, const GemmQ8FewPlan& plan, const CUten
 __host__ __device__ inline int gemm_q8_stored_columns(int dtype, int N) { return dtype == COMFUSE_DTYPE_F32 ? N & ~3 : N & ~7; }
 
 // Many rows.  `columns` of a tile (128 or 256): B's boxes have half as many rows.
-int gemm_q8_pair_columns(int batch, int M, int N, int K, const DeviceInfo& dev);
+int gemm_q8_pair_columns(int batch, int M, int N, const DeviceInfo& dev);
 struct GemmQ8PairMaps {
   CUtensorMap A, B, R, Y;  // boxes of 128 bytes x 128 rows (A), x columns / 2 rows (B), x 32 rows (R; Y up to its last whole 16 bytes); R unused without a residual
 };

@@ -124,7 +124,7 @@ def test_binding_refuses_other_rows():
                      (dict(scale=z(4, 1)), "scale has a shape"), (dict(scale=z(8)[::2]), "dense"), (dict(values=z(4, 16)), "values has another"), (dict(device=0), "x is not on the current device")):
         with pytest.raises(AssertionError, match=text):
             call(**kw)
-    with pytest.raises(IndexError):
+    with pytest.raises(AssertionError, match="x has a shape"):
         _bound("quantize_rows", 0, z(16), None, None, None, z(16, dtype=i8), z(1), None, 0.0, -1, _Stream())
     with pytest.raises(TypeError):
         _bound("quantize_rows", 0)
@@ -144,6 +144,25 @@ def test_binding_refuses_products():
 def test_unknown_activations_are_refused():
     with pytest.raises(ValueError, match="silu"):
         cf.gemm_q8(None, None, None, None, None, activation="silu")
+
+
+def test_both_ways_to_describe_a_tensor_agree():
+    """Through the class's DLPack exchange interface, where it has one, and through the tensor's Python interface."""
+    b = cf._bound_q8()
+    base = torch.zeros(6, 40, dtype=bf)
+    some = [base, base[1:4, 8:24], base.view(2, 3, 40)[:, 1:], z(7, dtype=i8), z(3, 4, 5, dtype=torch.float16).transpose(0, 1), z(2, 2), z(0, 4), z(2, 3, dtype=torch.int32),
+            z(4, dtype=torch.float64), torch.nn.Parameter(z(3, 8)), z(3, 8).requires_grad_(True)]
+    class Plain:   # nothing but the Python interface
+        def __init__(self, t):
+            self.t, self.dtype, self.shape = t, t.dtype, t.shape
+            self.stride, self.get_device, self.data_ptr = t.stride, t.get_device, t.data_ptr
+    for t in some:
+        fast, slow = b.describe(t), b.describe(Plain(t))
+        kind = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2, torch.int8: 3}.get(t.dtype, -1)
+        assert fast[:4] == slow[:4] == (kind, -1, t.data_ptr(), tuple(t.shape))
+        assert all(f == s or n <= 1 for f, s, n in zip(fast[4], slow[4], t.shape))   # (the stride of a dimension of one element may read as 1)
+    with pytest.raises(AttributeError):
+        b.describe(3)
 
 
 # per file: the barriers that must be drained behind an expired wait -- the last commit in front of the release of tensor memory, landing loads
