@@ -511,13 +511,16 @@ ACTIVATIONS = {None: 0, "none": 0, "relu": OPS["relu"], "gelu_tanh": OPS["gelu_t
 _q8 = None   # the marshalling extension, once the 8-bit entry points are in it
 
 
-def _bound_q8():
+def _bound_q8(device=True):
     global _q8, _current_device
     if _q8 is None:
         import torch
         b = _bound()
         b.bind_q8(*(ctypes.cast(f, c_void_p).value for f in (lib().comfuse_quantize_rows, lib().comfuse_gemm_q8)),
                   torch.bfloat16, torch.float16, torch.float32, torch.int8, torch.Tensor, getattr(torch.Tensor, "__dlpack_c_exchange_api__", None))
+        if not device:   # (the marshalling alone)
+            return b
+        _current_stream()   # (sets the device up)
         _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _q8 = b
     return _q8
@@ -527,13 +530,10 @@ def _current_device() -> int:   # (replaced by the bare call once the entry poin
     raise RuntimeError("no call has bound the 8-bit entry points yet")
 
 
-def _device_of(stream, q8) -> int:
+def _device_of(stream) -> int:
     """The device that a call's tensors have to be on: the current one, which the given stream has to belong to."""
-    if stream is None:
-        _current_stream()   # (sets the device up on first use)
-        return _current_device()
     device = _current_device()
-    if getattr(stream, "device_index", device) != device:
+    if stream is not None and getattr(stream, "device_index", device) != device:
         raise AssertionError("the stream does not belong to the current device")
     return device
 
@@ -543,7 +543,7 @@ def quantize_rows(x, q, scale, *, values=None, stream=None):
     bf16, fp16 or fp32, ``q`` [M, N] int8, ``scale`` [M] fp32; ``values`` [M, N] bf16, if given, receives q * scale.  Rows start on 16-byte
     boundaries (allocate a leading dimension that is a multiple of 16 bytes).  A row with an infinity or NaN has scale NaN."""
     b = _q8 or _bound_q8()
-    st = b.quantize_rows(QUANTIZE_PLAIN, x, None, None, None, q, scale, values, 0.0, _device_of(stream, b), _current_stream if stream is None else stream)
+    st = b.quantize_rows(QUANTIZE_PLAIN, x, None, None, None, q, scale, values, 0.0, _device_of(stream), _current_stream if stream is None else stream)
     if st != OK:
         raise ComfuseError(st, "comfuse_quantize_rows")
     return q, scale
@@ -554,7 +554,7 @@ def rmsnorm_quantize_rows(x, q, scale, *, residual=None, gamma=None, h=None, val
     receives t (it may be ``residual`` or ``x`` itself: the residual stream updated in place).  x, residual, h [M, N] and gamma [N] have one
     type (bf16, fp16 or fp32); q, scale, values as in quantize_rows."""
     b = _q8 or _bound_q8()
-    st = b.quantize_rows(QUANTIZE_RMSNORM, x, residual, gamma, h, q, scale, values, eps, _device_of(stream, b), _current_stream if stream is None else stream)
+    st = b.quantize_rows(QUANTIZE_RMSNORM, x, residual, gamma, h, q, scale, values, eps, _device_of(stream), _current_stream if stream is None else stream)
     if st != OK:
         raise ComfuseError(st, "comfuse_quantize_rows")
     return q, scale
@@ -565,10 +565,10 @@ def gemm_q8(A, scale_a, B, scale_b, Y, *, bias=None, residual=None, activation=N
     (a linear layer's weight, an output channel per row), scales fp32 [M] and [N]; Y, bias and residual bf16, fp16 or fp32, one type.
     With a leading batch dimension everywhere (bias excepted): a product per batch.  ``activation``: None, "relu", "gelu_tanh", "tanh" or
     "sigmoid".  Rows start on 16-byte boundaries; ``residual`` may be ``Y`` itself."""
-    b = _q8 or _bound_q8()
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation: one of {list(ACTIVATIONS)} is expected, got {activation!r}")
-    st = b.gemm_q8(A, scale_a, B, scale_b, Y, bias, residual, ACTIVATIONS[activation], _device_of(stream, b), _current_stream if stream is None else stream)
+    b = _q8 or _bound_q8()
+    st = b.gemm_q8(A, scale_a, B, scale_b, Y, bias, residual, ACTIVATIONS[activation], _device_of(stream), _current_stream if stream is None else stream)
     if st != OK:
         raise ComfuseError(st, "comfuse_gemm_q8")
     return Y

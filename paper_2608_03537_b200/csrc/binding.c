@@ -359,6 +359,7 @@ typedef struct {
   void* previous;
   void *allocate, *managed_from_object, *managed_to_object;
   int (*tensor_from_object)(void* object, DlTensor* out);  // a view for the length of the call; 0 = filled in, -1 = a Python error is set
+  int (*current_stream)(int32_t device_type, int32_t device_id, void** out);
 } DlExchange;
 static const DlExchange* dl_exchange;
 static PyTypeObject* dl_type;  // the class whose tensors it takes
@@ -445,6 +446,15 @@ static int float_type(const Described* d, const char* what, int* type) {
   return d->type == TYPE_BF16 || d->type == TYPE_F16 || d->type == TYPE_F32 ? 1 : refuse(what, "has another element type than the call takes");
 }
 
+// The stream of a call: as in stream_of, or, for the function that returns the current stream's handle, through the exchange interface.
+static int stream_on(PyObject* s, int64_t device, void** out) {
+  if (dl_exchange && dl_exchange->current_stream && PyFunction_Check(s)) {
+    if (dl_exchange->current_stream(2, (int32_t)device, out) == 0) return 1;
+    PyErr_Clear();
+  }
+  return stream_of(s, out);
+}
+
 // quantize_rows(kind, x, residual, gamma, h, q, scale, values, eps, device, stream) -> status
 static PyObject* py_quantize_rows(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   comfuse_quantize_desc_t d;
@@ -459,7 +469,7 @@ static PyObject* py_quantize_rows(PyObject* self, PyObject* const* a, Py_ssize_t
   const int64_t M = x.g.size[0], N = x.g.size[1];
   if (!optional_matrix(a[2], type, device, -1, M, N, "residual", &r) || !vector(a[3], type, device, -1, N, "gamma", &gamma) ||
       !optional_matrix(a[4], type, device, -1, M, N, "h", &h) || !matrix(a[5], TYPE_I8, device, -1, M, N, "q", &q) ||
-      !vector(a[6], TYPE_F32, device, -1, M, "scale", &scale) || !optional_matrix(a[7], TYPE_BF16, device, -1, M, N, "values", &v) || !stream_of(a[10], &stream))
+      !vector(a[6], TYPE_F32, device, -1, M, "scale", &scale) || !optional_matrix(a[7], TYPE_BF16, device, -1, M, N, "values", &v) || !stream_on(a[10], device, &stream))
     return NULL;
   if (!require(M <= INT32_MAX && N <= INT32_MAX, "sizes are 32-bit numbers")) return NULL;
   memset(&d, 0, sizeof(d));
@@ -497,7 +507,7 @@ static PyObject* py_gemm_q8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   const int64_t N = B.g.size[B.g.n - 2];
   if (!vector(a[1], TYPE_F32, device, batch, M, "scale_a", &sa) || !vector(a[3], TYPE_F32, device, batch, N, "scale_b", &sb) ||
       !matrix(a[4], type, device, batch, M, N, "Y", &Y) || !vector(a[5], type, device, -1, N, "bias", &bias) ||
-      !optional_matrix(a[6], type, device, batch, M, N, "residual", &r) || !stream_of(a[9], &stream))
+      !optional_matrix(a[6], type, device, batch, M, N, "residual", &r) || !stream_on(a[9], device, &stream))
     return NULL;
   if (!require(batch <= INT32_MAX && M <= INT32_MAX && N <= INT32_MAX && K <= INT32_MAX, "sizes are 32-bit numbers")) return NULL;
   memset(&d, 0, sizeof(d));
@@ -522,6 +532,14 @@ static PyObject* py_gemm_q8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   st = f_gemm_q8(&d, (const int8_t*)A.p, (const float*)sa, (const int8_t*)B.p, (const float*)sb, bias, r.p, (void*)Y.p, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong((long)st);
+}
+
+// stream(function or stream object, device) -> the handle that a call would use
+static PyObject* py_stream(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int64_t device;
+  void* out;
+  if (!fixed_args(n, 2, "stream") || !to_i64(a[1], &device) || !stream_on(a[0], device, &out)) return NULL;
+  return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)out);
 }
 
 // describe(tensor) -> (element type, device, address, shape, strides), as the 8-bit entry points see it
@@ -577,6 +595,7 @@ static PyMethodDef methods[] = {
     {"b2b", (PyCFunction)(void (*)(void))py_b2b, METH_FASTCALL, NULL},
     {"gemm_spec", (PyCFunction)(void (*)(void))py_gemm_spec, METH_FASTCALL, NULL},
     {"bind_q8", py_bind_q8, METH_VARARGS, NULL},
+    {"stream", (PyCFunction)(void (*)(void))py_stream, METH_FASTCALL, NULL},
     {"describe", (PyCFunction)(void (*)(void))py_describe, METH_FASTCALL, NULL},
     {"quantize_rows", (PyCFunction)(void (*)(void))py_quantize_rows, METH_FASTCALL, NULL},
     {"gemm_q8", (PyCFunction)(void (*)(void))py_gemm_q8, METH_FASTCALL, NULL},

@@ -158,6 +158,17 @@ def test_another_stream_and_a_captured_graph(cuda_device):
         _check(h, q, s, torch.bfloat16, norm=False)
 
 
+def test_the_binding_finds_the_current_stream(cuda_device):
+    b = cf._bound_q8()
+    side = torch.cuda.Stream()
+    current = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    assert b.stream(current, 0) == current()
+    with torch.cuda.stream(side):
+        assert b.stream(current, 0) == side.cuda_stream == current()
+    assert b.stream(side, 0) == side.cuda_stream
+    assert b.stream(current, 0) == current()
+
+
 def test_the_same_call_gives_the_same_bits(cuda_device):
     g = np.random.default_rng(8)
     x, r = (q8.put(g.standard_normal((200, 9000)), torch.bfloat16, cuda_device) for _ in range(2))

@@ -99,7 +99,7 @@ class _Stream:
 
 def _bound(name, *args):
     """A call through the binding with CPU tensors (whose device is -1); the library is never reached by what is refused."""
-    return getattr(cf._bound_q8(), name)(*args)
+    return getattr(cf._bound_q8(device=False), name)(*args)
 
 
 @pytest.mark.parametrize("args,text", [
@@ -144,11 +144,12 @@ def test_binding_refuses_products():
 def test_unknown_activations_are_refused():
     with pytest.raises(ValueError, match="silu"):
         cf.gemm_q8(None, None, None, None, None, activation="silu")
+    assert set(cf.ACTIVATIONS) == {None, "none", "relu", "gelu_tanh", "tanh", "sigmoid"}
 
 
 def test_both_ways_to_describe_a_tensor_agree():
     """Through the class's DLPack exchange interface, where it has one, and through the tensor's Python interface."""
-    b = cf._bound_q8()
+    b = cf._bound_q8(device=False)
     base = torch.zeros(6, 40, dtype=bf)
     some = [base, base[1:4, 8:24], base.view(2, 3, 40)[:, 1:], z(7, dtype=i8), z(3, 4, 5, dtype=torch.float16).transpose(0, 1), z(2, 2), z(0, 4), z(2, 3, dtype=torch.int32),
             z(4, dtype=torch.float64), torch.nn.Parameter(z(3, 8)), z(3, 8).requires_grad_(True)]
