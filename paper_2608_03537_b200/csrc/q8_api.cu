@@ -79,6 +79,7 @@ comfuse_status_t comfuse_quantize_rows(const comfuse_quantize_desc_t* desc, cons
   p.q = q; p.scale = scale; p.values = static_cast<uint16_t*>(values);
   p.ldx = desc->ldx; p.ldr = desc->ldr; p.ldh = desc->ldh; p.ldq = desc->ldq; p.ldv = desc->ldv;
   p.eps = desc->eps;
+  p.status = dev->status_word;
   const cudaError_t e = launch_quantize_rows(desc->dtype, desc->kind == COMFUSE_QUANTIZE_RMSNORM, p, *dev, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? COMFUSE_OK : COMFUSE_ERR_CUDA;
 }

@@ -19,6 +19,7 @@ struct QuantizeRowsParams {
   uint16_t* values;
   long long ldx, ldr, ldh, ldq, ldv;
   float eps;
+  unsigned int* status;
 };
 cudaError_t launch_quantize_rows(int dtype, bool norm, QuantizeRowsParams p, const DeviceInfo& dev, cudaStream_t stream);
 

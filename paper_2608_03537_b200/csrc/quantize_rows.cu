@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kMaxThreads) quantize_rows_kernel(const Quanti
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       w[k] = __byte_perm(__byte_perm(b[4 * k], b[4 * k + 1], 0x0040), __byte_perm(b[4 * k + 2], b[4 * k + 3], 0x0040), 0x5410);
-    st_8(qrow + 8 * c, w);
+    if (COMFUSE_IN_BOUNDS(row < p.rows && 8 * c + 7 < p.N, p.status)) st_8(qrow + 8 * c, w);
     if (p.values) store_chunk<COMFUSE_DTYPE_BF16>(reinterpret_cast<char*>(vrow + 8 * c), yj);
   }
   if (tail) {

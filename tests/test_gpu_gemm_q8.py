@@ -42,6 +42,7 @@ def run_case(M, N, K, name, device, batch=None, activation=None, bias=True, resi
 
 SIZES = [(1, 1, 1), (1, 4096, 4096), (2, 5, 17), (3, 130, 31), (15, 128, 128), (16, 127, 129), (17, 129, 640), (31, 257, 1000), (33, 1000, 2049), (64, 640, 1300), (65, 256, 300), (100, 1001, 700),
          (128, 384, 2056), (129, 200, 515), (200, 1300, 4100), (256, 640, 256), (257, 3, 4), (300, 777, 1032), (513, 1024, 64), (700, 72, 5000), (1000, 1000, 100),
+         (12, 8200, 4100), (8, 20000, 2700), (60, 40000, 260), (90, 300, 20000), (520, 4000, 300), (5000, 100, 700),
          (3000, 1700, 300), (2817, 2001, 131), (40000, 8, 64)]
 
 
@@ -139,6 +140,28 @@ def test_split_sums_do_not_change_a_bit(cuda_device):
         assert torch.equal(z, y[:M]), M
 
 
+def test_offsets_beyond_32_bits(cuda_device):
+    """A result, and a batch of operands, of more than 2^32 bytes."""
+    g = torch.Generator(device=cuda_device).manual_seed(3)
+    rand = lambda *s: torch.randint(-127, 128, s, dtype=torch.int8, device=cuda_device, generator=g)  # noqa: E731
+    M, N, K = 70000, 33000, 64
+    a, b = rand(M, K), rand(N, K)
+    sa, sb = torch.rand(M, device=cuda_device, generator=g), torch.rand(N, device=cuda_device, generator=g)
+    y = torch.empty(M, N, dtype=torch.bfloat16, device=cuda_device)
+    cf.gemm_q8(a, sa, b, sb, y)
+    for rows in (slice(0, 3), slice(65000, 65100), slice(M - 50, M)):
+        want = (a[rows].double() @ b.double().mT) * sa[rows].double()[:, None] * sb.double()
+        assert ((y[rows].double() - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -20)).all()
+    del y
+    batch, M, N, K = 70, 3, 512, 131056
+    a, b = rand(batch, M, K), rand(batch, N, K)
+    sa, sb = torch.rand(batch, M, device=cuda_device, generator=g), torch.rand(batch, N, device=cuda_device, generator=g)
+    y = torch.empty(batch, M, N, device=cuda_device)
+    cf.gemm_q8(a, sa, b, sb, y)
+    want = torch.stack([(a[i].double() @ b[i].double().mT) for i in (0, 35, 69)]) * sa[[0, 35, 69], :, None].double() * sb[[0, 35, 69], None].double()
+    assert ((y[[0, 35, 69]].double() - want).abs() <= want.abs() * 2.0 ** -20).all()
+
+
 CHILD = """
 import torch
 from tests import test_gpu_gemm_q8 as t
@@ -155,6 +178,31 @@ assert cf.last_device_status() == cf.OK
 def test_the_tile_kernel_at_small_sizes(cuda_device):
     """With the form for few rows off every size runs on the tile kernel: one tile, partial tiles, short and long contractions."""
     r = subprocess.run([sys.executable, "-c", CHILD], cwd=ROOT, env=dict(os.environ, PYTHONPATH=ROOT, COMFUSE_FEW_ROWS="0"), capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-1000:] + r.stderr[-3000:]
+
+
+CHECKED = """
+import torch
+import paper_2608_03537_b200 as cf
+from tests import test_gpu_gemm_q8 as t, test_gpu_quantize_rows as r
+assert cf.LIB_PATH.endswith("libcomfuse_checked.so"), cf.LIB_PATH
+d = torch.device("cuda:0")
+for M, N, K in t.SIZES:
+    t.run_case(M, N, K, "bf16", d, seed=M)
+    t.run_case(M, N, K, "f32", d, seed=N, activation="gelu_tanh")
+for M, N in ((1, 7), (3, 1000), (300, 4099), (5, 65536), (9000, 250)):
+    r._run(M, N, "bf16", True, True, True, d, N)
+    r._run(M, N, "f32", False, False, False, d, N)
+assert cf.last_device_status() == cf.OK
+"""
+
+
+def test_no_bounds_predicate_fails_in_the_checked_build(cuda_device):
+    lib = os.path.join(ROOT, "paper_2608_03537_b200", "libcomfuse_checked.so")
+    if not os.path.exists(lib):
+        from paper_2608_03537_b200 import build
+        build.build(checked=True)
+    r = subprocess.run([sys.executable, "-c", CHECKED], cwd=ROOT, env=dict(os.environ, PYTHONPATH=ROOT, COMFUSE_LIB=lib), capture_output=True, text=True, timeout=900)
     assert r.returncode == 0, r.stdout[-1000:] + r.stderr[-3000:]
 
 

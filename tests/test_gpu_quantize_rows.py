@@ -118,6 +118,59 @@ def test_rows_out_of_the_ordinary(N, norm, cuda_device):
     q8.check_surroundings({"q": q, "scale": s, "values": v})
 
 
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("N", [5, 200, 801, 1500, 17000])
+def test_rows_that_are_not_finite(N, name, norm, cuda_device):
+    """One infinity or NaN, of either sign, at any place of a row, makes that row NaN and no other."""
+    g = np.random.default_rng(N)
+    M = 40
+    x = g.standard_normal((M, N)).astype(np.float32)
+    bad = {}
+    for i in range(0, M, 3):
+        bad[i] = [np.inf, -np.inf, np.nan, -np.nan][(i // 3) % 4]
+        x[i, [0, N - 1, N // 2, (i * 37) % N][(i // 12) % 4]] = bad[i]
+    X = q8.put(x, q8.TYPES[name], cuda_device)
+    q, s, v = q8.out((M, N), torch.int8, cuda_device), q8.out((M,), torch.float32, cuda_device), q8.out((M, N), torch.bfloat16, cuda_device)
+    if norm:
+        cf.rmsnorm_quantize_rows(X, q, s, values=v, eps=EPS)
+    else:
+        cf.quantize_rows(X, q, s, values=v)
+    torch.cuda.synchronize()
+    i = torch.tensor(sorted(bad), device=cuda_device)
+    j = torch.tensor([k for k in range(M) if k not in bad], device=cuda_device)
+    assert torch.isnan(s[i]).all() and (q[i] == 0).all() and torch.isnan(v[i].float()).all()
+    _check(X[j], q[j], s[j], q8.TYPES[name], values=v[j], norm=norm)
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16"])
+def test_the_middle_of_two_codes_goes_to_the_even_one(name, cuda_device):
+    """max = 127 / 2^k: the codes of multiples of 2^-k / 2 lie exactly between two whole numbers."""
+    x = torch.zeros(8, 256, device=cuda_device)
+    x[:, 0] = 127
+    x[:, 1:254] = (torch.arange(253, device=cuda_device) - 126) / 2
+    x *= 2.0 ** torch.arange(-4, 4, device=cuda_device)[:, None]
+    q, s = torch.empty(8, 256, dtype=torch.int8, device=cuda_device), torch.empty(8, device=cuda_device)
+    cf.quantize_rows(x.to(q8.TYPES[name]), q, s)
+    want = torch.zeros(256, device=cuda_device)
+    want[0], want[1:254] = 127, ((torch.arange(253, device=cuda_device) - 126) / 2).round()   # (ties to even)
+    assert (q == want).all() and torch.equal(s, 2.0 ** torch.arange(-4, 4, device=cuda_device))
+
+
+def test_offsets_beyond_32_bits(cuda_device):
+    """More than 2^32 bytes of rows: the last ones are read and written where they stand."""
+    M, N = 70000, 65536
+    x = torch.zeros(M, N, dtype=torch.bfloat16, device=cuda_device)
+    q, s = torch.empty(M, N, dtype=torch.int8, device=cuda_device), torch.empty(M, device=cuda_device)
+    rows = [0, 32767, 32768, 65535, 65536, M - 1]
+    for k in rows:
+        x[k] = torch.randn(N, device=cuda_device)
+    cf.rmsnorm_quantize_rows(x, q, s, h=x, eps=EPS)
+    i = torch.tensor(rows, device=cuda_device)
+    _check(x[i], q[i], s[i], torch.bfloat16)
+    assert int((s != 0).sum()) == len(rows) and not q[1:32767].any() and not q[65537:M - 1].any()
+
+
 @pytest.mark.parametrize("N", [1, 40, 500, 3000, 65536])
 def test_squares_beyond_fp32(N, cuda_device):
     """Rows whose sum of squares, or whose single squares, leave fp32's range, in every element or in some."""
