@@ -5,7 +5,7 @@
 // more SMs).  Clusters of two are persistent and walk the tiles in bands of 8 row blocks, so that the tiles in flight share their
 // operands in the L2.  Two accumulators alternate: a tile's epilogue runs under the next one's products.
 //
-// Epilogue: thread = one row of the tile, 32 columns at a time, a warp half of the columns.  The channel's scale and bias come from shared
+// Epilogue: thread = one row of the tile, 32 columns (16 with sixteen warps) at a time, a warp half or a quarter of the columns.  The channel's scale and bias come from shared
 // memory (broadcast), the row's scale is a register.  Results leave as boxes of 32 rows x 128 bytes staged in shared memory and stored by
 // TMA; the residual comes in the same way, into the box that its sum leaves from.  A TMA store writes whole 16-byte units (measured: up to
 // seven bf16 behind the last column), so Y's map ends at the last whole unit and the columns behind it are stored one by one.
@@ -18,10 +18,10 @@
 namespace comfuse {
 namespace {
 
-template <int BN, int STAGES, int BOXES>
+template <int BN, int STAGES, int BOXES, int EPW>
 struct PairQ8Cfg {
   static constexpr int NSTAGES = STAGES;
-  static constexpr int kEpiWarps = 8;
+  static constexpr int kEpiWarps = 4 * EPW;  // EPW for each quarter of the accumulator's lanes
   static constexpr int kThreads = 32 * (2 + kEpiWarps);
   static constexpr int A_BYTES = 128 * 128;              // 128 rows of A x 128 bytes
   static constexpr int STAGE_BYTES = A_BYTES + BN / 2 * 128;
@@ -36,10 +36,10 @@ struct PairQ8Cfg {
   static_assert(SMEM_BYTES <= 232448 && SMEM_BYTES > 116 * 1024, "one CTA per SM");
 };
 
-template <int DT, int BN, int STAGES, int BOXES>
-__global__ void __launch_bounds__(PairQ8Cfg<BN, STAGES, BOXES>::kThreads, 1)
+template <int DT, int BN, int STAGES, int BOXES, int EPW>
+__global__ void __launch_bounds__(PairQ8Cfg<BN, STAGES, BOXES, EPW>::kThreads, 1)
 gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Params p) {
-  using Cfg = PairQ8Cfg<BN, STAGES, BOXES>;
+  using Cfg = PairQ8Cfg<BN, STAGES, BOXES, EPW>;
   constexpr int NSTAGES = Cfg::NSTAGES;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
@@ -150,16 +150,17 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
     }
   } else {
     // ------------------------------------------------------------------------------------------ epilogue warps
-    const int e = warp - 2, q = warp & 3, half = e >> 2;  // TMEM lane quarter: rows 32q ..; which half of the columns
+    const int e = warp - 2, q = warp & 3, part = e >> 2;  // TMEM lane quarter: rows 32q ..; which BN / EPW of the columns
+    constexpr int S = EPW == 4 ? 16 : 32;                   // columns at a time (what the registers of that many warps hold)
     constexpr int E = 128 / Elem<DT>::kBytes;               // columns of a box
-    const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + half * (BN / 2);
+    const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + part * (BN / EPW);
     const uint32_t tempty = map_to_cta(bar_tempty(0), 0);
     const uint32_t box0 = smem_base + Cfg::OFF_BOX + e * BOXES * Cfg::BOX_BYTES;
     float2* s_vec = reinterpret_cast<float2*>(smem + Cfg::OFF_VEC);
     const int whole = gemm_q8_stored_columns(DT, p.N);  // by TMA
     uint32_t n = 0, count = 0;  // tiles, and boxes of this warp
     // What a tile needs from global memory is asked for under the tile before: the scale and bias of one of its channels, the row's scale.
-    const int i = static_cast<int>(threadIdx.x) - 64;  // 256 threads, BN channels
+    const int i = static_cast<int>(threadIdx.x) - 64;  // one thread a channel
     int b = 0, m0 = 0, n0 = 0;
     float sa = 0.f;
     float2 vec = make_float2(0.f, 0.f);
@@ -177,12 +178,12 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
     for (uint32_t tile = cluster_id; tile < tiles; tile += clusters, ++n) {
       const uint32_t slot = n & 1u;
       if (i < BN) s_vec[slot * BN + i] = vec;  // (the barrier below keeps the warps within one tile of each other)
-      const int tb = b, row0 = m0 + static_cast<int>(rank) * 128 + q * 32, col0 = n0 + half * (BN / 2);
+      const int tb = b, row0 = m0 + static_cast<int>(rank) * 128 + q * 32, col0 = n0 + part * (BN / EPW);
       const float tsa = sa;
       fetch(tile + clusters);
       named_barrier_sync(1, 32 * Cfg::kEpiWarps);
       const int left = row0 < p.M && col0 < p.N ? (p.N - col0 + E - 1) / E : 0;
-      const int boxes = left < BN / 2 / E ? left : BN / 2 / E;  // that hold anything of Y
+      const int boxes = left < BN / EPW / E ? left : BN / EPW / E;  // that hold anything of Y
       // box k of this tile: once its staging box has been read out by the store before last, ask for the residual
       auto ask = [&](int k) {
         if (lane == 0 && p.residual && k < boxes) {
@@ -209,14 +210,17 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
         if (BOXES > 1) ask(k + 1);
         else if (k > 0) ask(k);
 #pragma unroll
-        for (int h = 0; h < E / 32; ++h) {
-          const int local = half * (BN / 2) + k * E + h * 32;
-          uint32_t v[32];
-          tmem_ld_32cols(lane_addr + slot * BN + k * E + h * 32, v);
-          if (k == boxes - 1 && h == E / 32 - 1) release();
-          float z[32];
+        for (int h = 0; h < E / S; ++h) {
+          const int local = part * (BN / EPW) + k * E + h * S;
+          uint32_t v[S];
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) {
+          for (int j = 0; j < S; j += 16) tmem_ld_issue_16(lane_addr + slot * BN + k * E + h * S + j, v + j);
+#pragma unroll
+          for (int j = 0; j < S; j += 16) tmem_ld_wait_16(v + j);
+          if (k == boxes - 1 && h == E / S - 1) release();
+          float z[S];
+#pragma unroll
+          for (int j = 0; j < S; j += 2) {
             const float4 sv = *reinterpret_cast<const float4*>(s_vec + slot * BN + local + j);
             z[j] = fmaf(static_cast<float>(static_cast<int>(v[j])) * sv.x, tsa, sv.y);
             z[j + 1] = fmaf(static_cast<float>(static_cast<int>(v[j + 1])) * sv.z, tsa, sv.w);
@@ -230,7 +234,7 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
             }
             __syncwarp();
           }
-          constexpr int kChunks = 2 * Elem<DT>::kBytes;  // 16-byte chunks of 32 columns
+          constexpr int kChunks = S * Elem<DT>::kBytes / 16;
           uint32_t at[kChunks];
 #pragma unroll
           for (int c = 0; c < kChunks; ++c) at[c] = row_addr + (((h * kChunks + c) ^ (lane & 7)) << 4);
@@ -244,11 +248,11 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
               for (int i = 0; i < kEach; ++i) z[c * kEach + i] += Elem<DT>::of(r, i);
             }
           }
-          const int col = col0 + k * E + h * 32;
-          if (col + 32 > whole && ok && row0 + lane < p.M) {
+          const int col = col0 + k * E + h * S;
+          if (col + S > whole && ok && row0 + lane < p.M) {
             void* out = static_cast<char*>(p.Y) + (tb * p.batch_stride_y + static_cast<long long>(row0 + lane) * p.ldy) * Elem<DT>::kBytes;
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
+            for (int i = 0; i < S; ++i)
               if (col + i >= whole && col + i < p.N) Elem<DT>::put(out, col + i, z[i]);
           }
           uint32_t ow[4 * kChunks];
@@ -283,10 +287,10 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
   }
 }
 
-template <int DT, int BN, int STAGES, int BOXES>
+template <int DT, int BN, int STAGES, int BOXES, int EPW>
 cudaError_t launch_instance(const GemmQ8PairMaps& maps, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
-  using Cfg = PairQ8Cfg<BN, STAGES, BOXES>;
-  auto kern = gemm_q8_pair_kernel<DT, BN, STAGES, BOXES>;
+  using Cfg = PairQ8Cfg<BN, STAGES, BOXES, EPW>;
+  auto kern = gemm_q8_pair_kernel<DT, BN, STAGES, BOXES, EPW>;
   static ResidentClusters resident;  // (sets the kernel's attributes on the device the first time it is asked)
   const int fit = resident.of(reinterpret_cast<const void*>(kern), Cfg::kThreads, Cfg::SMEM_BYTES, 2, dev);
   if (fit < 1) return cudaErrorLaunchOutOfResources;
@@ -308,12 +312,17 @@ cudaError_t launch_instance(const GemmQ8PairMaps& maps, const GemmQ8Params& p, c
   return cudaLaunchKernelEx(&cfg, kern, maps, p);
 }
 
-// Columns of a tile, stages of the ring, staging boxes an epilogue warp.  Behind a long contraction the ring's depth is what counts (8192 x 4096 x
-// 4096 with 5 / 4 / 3 stages: 92 / 99 / 112 us), behind a short one the stores (96 x 504 x 504 x 64 with 1 / 2 boxes: 21 / 19 us in bf16).
+// Columns of a tile, stages of the ring, staging boxes an epilogue warp, epilogue warps a lane quarter.  Behind a long contraction the ring's
+// depth is what counts, behind a short one the epilogue: more boxes, or, where an activation makes its arithmetic long, more warps.  us, 8192 x
+// 4096 in bf16, 5 stages / 4 with two boxes / 4 with sixteen warps: K = 4096 86 / 94 / 98, K = 512 25.0 / 24.3 / 25.4, with GELU K = 512 42.0 / 42.3 / 38.4,
+// K = 1536 47.0 / 48.9 / 45.0, K = 2048 52.8 / 57.8 / 54.0; 96 x 504 x 504 x 64 21 / 19 / 20.
 template <int DT>
 cudaError_t launch_columns(int columns, const GemmQ8PairMaps& maps, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
-  if (columns == 128) return launch_instance<DT, 128, 6, 2>(maps, p, dev, stream);
-  return p.K <= 1024 ? launch_instance<DT, 256, 4, 2>(maps, p, dev, stream) : launch_instance<DT, 256, 5, 1>(maps, p, dev, stream);
+  const bool long_epilogue = p.activation != 0 && p.activation != COMFUSE_OP_RELU;
+  if (columns == 128) return launch_instance<DT, 128, 6, 2, 2>(maps, p, dev, stream);
+  if (long_epilogue && p.K <= 1536) return launch_instance<DT, 256, 4, 1, 4>(maps, p, dev, stream);
+  if (p.K <= 1024) return launch_instance<DT, 256, 4, 2, 2>(maps, p, dev, stream);
+  return launch_instance<DT, 256, 5, 1, 2>(maps, p, dev, stream);
 }
 
 }  // namespace
