@@ -18,7 +18,7 @@
 namespace comfuse {
 namespace {
 
-template <int BN, int STAGES, int BOXES, int EPW>
+template <int DT, int BN, int STAGES, int BOXES, int EPW>
 struct PairQ8Cfg {
   static constexpr int NSTAGES = STAGES;
   static constexpr int kEpiWarps = 4 * EPW;  // EPW for each quarter of the accumulator's lanes
@@ -27,8 +27,9 @@ struct PairQ8Cfg {
   static constexpr int STAGE_BYTES = A_BYTES + BN / 2 * 128;
   static constexpr int BOX_BYTES = 32 * 128;
   static constexpr int OFF_BOX = NSTAGES * STAGE_BYTES;  // BOXES staging boxes a warp
-  static constexpr int OFF_VEC = OFF_BOX + kEpiWarps * BOXES * BOX_BYTES;  // [2][BN] (scale, bias) of the tile's channels
-  static constexpr int OFF_BAR = OFF_VEC + 2 * BN * 8;
+  static constexpr int VEC_BYTES = BN * (4 + Elem<DT>::kBytes);  // scales and biases of a tile's channels, two sets
+  static constexpr int OFF_VEC = OFF_BOX + kEpiWarps * BOXES * BOX_BYTES;
+  static constexpr int OFF_BAR = OFF_VEC + 2 * VEC_BYTES;
   static constexpr int NUM_BARS = 2 * NSTAGES + 5 + kEpiWarps * BOXES;
   static constexpr int OFF_MISC = OFF_BAR + NUM_BARS * 8;
   static constexpr int SMEM_BYTES = OFF_MISC + 16 + 1024;
@@ -37,9 +38,9 @@ struct PairQ8Cfg {
 };
 
 template <int DT, int BN, int STAGES, int BOXES, int EPW>
-__global__ void __launch_bounds__(PairQ8Cfg<BN, STAGES, BOXES, EPW>::kThreads, 1)
+__global__ void __launch_bounds__(PairQ8Cfg<DT, BN, STAGES, BOXES, EPW>::kThreads, 1)
 gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Params p) {
-  using Cfg = PairQ8Cfg<BN, STAGES, BOXES, EPW>;
+  using Cfg = PairQ8Cfg<DT, BN, STAGES, BOXES, EPW>;
   constexpr int NSTAGES = Cfg::NSTAGES;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
@@ -156,28 +157,34 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
     const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + part * (BN / EPW);
     const uint32_t tempty = map_to_cta(bar_tempty(0), 0);
     const uint32_t box0 = smem_base + Cfg::OFF_BOX + e * BOXES * Cfg::BOX_BYTES;
-    float2* s_vec = reinterpret_cast<float2*>(smem + Cfg::OFF_VEC);
+    using Word = typename Elem<DT>::Word;
     const int whole = gemm_q8_stored_columns(DT, p.N);  // by TMA
     uint32_t n = 0, count = 0;  // tiles, and boxes of this warp
     // What a tile needs from global memory is asked for under the tile before: the scale and bias of one of its channels, the row's scale.
     const int i = static_cast<int>(threadIdx.x) - 64;  // one thread a channel
     int b = 0, m0 = 0, n0 = 0;
     float sa = 0.f;
-    float2 vec = make_float2(0.f, 0.f);
+    float scale = 0.f;
+    Word bias = 0;
     auto fetch = [&](uint32_t tile) {
       if (tile >= tiles) return;
       decode(tile, b, m0, n0);
       const int row = m0 + static_cast<int>(rank) * 128 + q * 32 + lane, c = n0 + i;
       sa = row < p.M ? __ldg(p.scale_a + static_cast<long long>(b) * p.M + row) : 0.f;
       if (i < BN) {
-        vec.x = c < p.N ? __ldg(p.scale_b + static_cast<long long>(b) * p.N + c) : 0.f;
-        vec.y = p.bias && c < p.N ? Elem<DT>::get(p.bias, c) : 0.f;
+        scale = c < p.N ? __ldg(p.scale_b + static_cast<long long>(b) * p.N + c) : 0.f;
+        bias = p.bias && c < p.N ? __ldg(static_cast<const Word*>(p.bias) + c) : static_cast<Word>(0);
       }
     };
     fetch(cluster_id);
     for (uint32_t tile = cluster_id; tile < tiles; tile += clusters, ++n) {
       const uint32_t slot = n & 1u;
-      if (i < BN) s_vec[slot * BN + i] = vec;  // (the barrier below keeps the warps within one tile of each other)
+      float* s_scale = reinterpret_cast<float*>(smem + Cfg::OFF_VEC + slot * Cfg::VEC_BYTES);
+      Word* s_bias = reinterpret_cast<Word*>(s_scale + BN);
+      if (i < BN) {  // (the barrier below keeps the warps within one tile of each other)
+        s_scale[i] = scale;
+        s_bias[i] = bias;
+      }
       const int tb = b, row0 = m0 + static_cast<int>(rank) * 128 + q * 32, col0 = n0 + part * (BN / EPW);
       const float tsa = sa;
       fetch(tile + clusters);
@@ -220,10 +227,19 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
           if (k == boxes - 1 && h == E / S - 1) release();
           float z[S];
 #pragma unroll
-          for (int j = 0; j < S; j += 2) {
-            const float4 sv = *reinterpret_cast<const float4*>(s_vec + slot * BN + local + j);
-            z[j] = fmaf(static_cast<float>(static_cast<int>(v[j])) * sv.x, tsa, sv.y);
-            z[j + 1] = fmaf(static_cast<float>(static_cast<int>(v[j + 1])) * sv.z, tsa, sv.w);
+          for (int j = 0; j < S; j += 4) {
+            const float4 sv = *reinterpret_cast<const float4*>(s_scale + local + j);
+            uint32_t bw[Elem<DT>::kBytes];
+            if constexpr (Elem<DT>::kBytes == 4) {
+              const uint4 bv = *reinterpret_cast<const uint4*>(s_bias + local + j);
+              bw[0] = bv.x; bw[1] = bv.y; bw[2] = bv.z; bw[3] = bv.w;
+            } else {
+              const uint2 bv = *reinterpret_cast<const uint2*>(s_bias + local + j);
+              bw[0] = bv.x; bw[1] = bv.y;
+            }
+            const float f[4] = {sv.x, sv.y, sv.z, sv.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) z[j + u] = fmaf(static_cast<float>(static_cast<int>(v[j + u])) * f[u], tsa, Elem<DT>::of(bw, u));
           }
           activate(z, p.activation);
           if (h == 0) {  // the staging box is this warp's again
@@ -289,7 +305,7 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
 
 template <int DT, int BN, int STAGES, int BOXES, int EPW>
 cudaError_t launch_instance(const GemmQ8PairMaps& maps, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
-  using Cfg = PairQ8Cfg<BN, STAGES, BOXES, EPW>;
+  using Cfg = PairQ8Cfg<DT, BN, STAGES, BOXES, EPW>;
   auto kern = gemm_q8_pair_kernel<DT, BN, STAGES, BOXES, EPW>;
   static ResidentClusters resident;  // (sets the kernel's attributes on the device the first time it is asked)
   const int fit = resident.of(reinterpret_cast<const void*>(kern), Cfg::kThreads, Cfg::SMEM_BYTES, 2, dev);
@@ -315,7 +331,8 @@ cudaError_t launch_instance(const GemmQ8PairMaps& maps, const GemmQ8Params& p, c
 // Columns of a tile, stages of the ring, staging boxes an epilogue warp, epilogue warps a lane quarter.  Behind a long contraction the ring's
 // depth is what counts, behind a short one the epilogue: more boxes, or, where an activation makes its arithmetic long, more warps.  us, 8192 x
 // 4096 in bf16, 5 stages / 4 with two boxes / 4 with sixteen warps: K = 4096 86 / 94 / 98, K = 512 25.0 / 24.3 / 25.4, with GELU K = 512 42.0 / 42.3 / 38.4,
-// K = 1536 47.0 / 48.9 / 45.0, K = 2048 52.8 / 57.8 / 54.0; 96 x 504 x 504 x 64 21 / 19 / 20.
+// K = 1536 47.0 / 48.9 / 45.0, K = 2048 52.8 / 57.8 / 54.0; 96 x 504 x 504 x 64 21 / 19 / 20.  (A sixth stage, in the room of one of the two sets of scales:
+// between 3 % faster and 7 % slower from call to call under the power limit.)
 template <int DT>
 cudaError_t launch_columns(int columns, const GemmQ8PairMaps& maps, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
   const bool long_epilogue = p.activation != 0 && p.activation != COMFUSE_OP_RELU;
