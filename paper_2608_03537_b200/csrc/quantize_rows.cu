@@ -287,13 +287,17 @@ cudaError_t launch_form(QuantizeRowsParams p, const DeviceInfo& dev, cudaStream_
   // Rows longer than 16384: at most 8192 elements a CTA, so that an SM holds several (2048 x 65536 norm 233 -> 221 us, fp32 436 -> 413).
   if (chunks > 2048)
     while (chunks > p.split * 1024) p.split *= 2;
-  while (p.split < 8 && static_cast<long long>(p.rows) * p.split * 2 <= dev.sm_count && chunks >= p.split * 512) p.split *= 2;
+  // Few rows: CTAs of 256 .. 512 chunks.  us with 1 / 2 / 4 / 8 a row (norm, bf16): 1 x 16384 4.1 / 3.6 / 2.9 / 2.4, 40 x 8192 3.7 / 4.0 / 3.6 / 3.8, 100 x 16384
+  // 7.7 / 6.2 / 5.9 / 5.9; 40 x 4096 2.4 / 2.7 / 2.6 / 2.8, so from 8192 on.
+  const bool many = static_cast<long long>(p.rows) * chunks >= 4096ll * dev.sm_count;
+  if (!many && chunks >= 1024)
+    while (p.split < 8 && static_cast<long long>(p.rows) * p.split <= 4ll * dev.sm_count && chunks >= p.split * 512) p.split *= 2;
   const int per = (chunks + p.split - 1) / p.split;
-  // Chunks a thread: few where latency counts, many where bytes under way do.  us with 1 / 2 / 4 / 8 (16 bits): norm 40 x 4096 2.7 / 2.9 / 3.5 / 4.7, 600 x
+  // Chunks a thread: few where latency counts, many where bytes under way do.  us with 1 / 2 / 4 / 8 (16 bits): norm 40 x 4096 2.6 / 2.4 / 3.5 / 4.7, 600 x
   // 4096 7.8 / 6.7 / 7.4 / 7.8, 8192 x 4096 66 / 55 / 49 / 51; without norm 8192 x 2048 21.0 / 16.3 / 15.5 / 16.3, 8192 x 16384 - / - / 124 / 109; fp32 norm 8192 x
   // 4096 87 / 78 / 79 / 124, without 8192 x 4096 52 / 40 / 38 / 40.
-  const bool many = static_cast<long long>(p.rows) * chunks >= 4096ll * dev.sm_count;
-  int ch = many ? (NORM ? (k16 && per >= 256 ? 4 : 2) : k16 ? (per > 512 ? 8 : 4) : (per >= 512 ? 4 : 2)) : per > 128 && (p.rows >= 2 * dev.sm_count || (!NORM && k16)) ? 2 : 1;
+  int ch = many ? (NORM ? (k16 && per >= 256 ? 4 : 2) : k16 ? (per > 512 ? 8 : 4) : (per >= 512 ? 4 : 2))
+                : per > 256 || (per > 128 && static_cast<long long>(p.rows) * p.split > dev.sm_count) ? 2 : 1;
   while (per > ch * kMaxThreads) ch *= 2;
   const unsigned threads = static_cast<unsigned>(((per + ch - 1) / ch + 31) / 32 * 32), grid = static_cast<unsigned>(p.rows) * static_cast<unsigned>(p.split);
   if (ch == 1) return launch_instance<DT, NORM, 1, false>(p, grid, threads, stream);
