@@ -468,7 +468,7 @@ comfuse_status_t comfuse_quantize_rows(const comfuse_quantize_desc_t* desc, cons
 
 typedef struct {
   int32_t batch;              /* >= 1; A, B, residual, Y and the scales are batched, bias is shared */
-  int32_t M, N, K;            /* A int8 [M, K], B int8 [N, K] (one output channel per row), residual and Y [M, N]; N <= 65536, K <= 131071 */
+  int32_t M, N, K;            /* A int8 [M, K], B int8 [N, K] (one output channel per row), residual and Y [M, N]; M < 2^31 - 256, N <= 65536, K <= 131071 */
   int64_t lda, ldb, ldr, ldy; /* elements; ldr matters where residual is given */
   int64_t batch_stride_a, batch_stride_b, batch_stride_r, batch_stride_y; /* elements, multiples of 16 bytes; matter for batch > 1 */
   int32_t dtype;              /* comfuse_dtype_t of bias, residual and Y */

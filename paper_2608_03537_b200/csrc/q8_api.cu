@@ -55,7 +55,8 @@ comfuse_status_t check_gemm(const comfuse_gemm_q8_desc_t* d, const void* A, cons
     return COMFUSE_ERR_ALIGNMENT;
   if (!aligned(A, 16) || !aligned(B, 16) || !aligned(bias, 16) || !aligned(residual, 16) || !aligned(Y, 16) || !aligned(scale_a, 4) || !aligned(scale_b, 4))
     return COMFUSE_ERR_ALIGNMENT;
-  if (d->N > 65536 || d->K > 131071) return COMFUSE_ERR_UNSUPPORTED;  // 131072 * 128 * 128 leaves int32
+  // 131072 * 128 * 128 leaves int32, and so would the rows of the last tile
+  if (d->N > 65536 || d->K > 131071 || d->M >= 0x7FFFFF00) return COMFUSE_ERR_UNSUPPORTED;
   return COMFUSE_OK;
 }
 

@@ -56,19 +56,6 @@ __device__ __forceinline__ void ld_8(const void* p, uint32_t* w) {
 __device__ __forceinline__ void st_8(void* p, const uint32_t* w) {
   asm volatile("st.global.v2.b32 [%0], {%1, %2};" ::"l"(p), "r"(w[0]), "r"(w[1]) : "memory");
 }
-// A whole 32-byte sector at once (sm_100); the address is a multiple of 32.
-__device__ __forceinline__ void ld_32(const void* p, uint32_t* w) {
-  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-               : "l"(p)
-               : "memory");
-}
-__device__ __forceinline__ void st_32(void* p, const uint32_t* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
-               "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-
 // 1 / (1 + e^-x) from ex2 and rcp: relative error 2^-22 + |x| 2^-24 (the exponent's rounding); 0 where e^-x leaves fp32.
 __device__ __forceinline__ float sigmoid_f32(float x) { return rcp_approx(1.f + ex2_approx(x * -1.4426950408889634f)); }
 

@@ -3,8 +3,8 @@
 Bounds (u = 2^-24, half a step of fp32; t = scale_a scale_b S the scaled product, S its exact integer sum).
   codes   127 h gamma / max|h gamma|: h, h gamma and the quotient are one rounding each, and max carries two of its element: 5 u of at most 127, in
           front of the rounding to a whole number: |q - v| <= 1/2 + 127 * 5 u.
-  scale   without the norm one rounding (the division by 127).  With it: the sum of squares is at most 8 + 4 + 5 + 16 + 8 additions
-          deep (chunk, chunks, lanes, warps, CTAs), with h's rounding twice 43 u, half of that behind the root; mean, + eps,
+  scale   without the norm one rounding (the division by 127).  With it: the sum of squares is at most 8 + 4 + 1 + 5 + 16 + 8 additions
+          deep (chunk, chunks, the element behind them, lanes, warps, CTAs), with h's rounding twice 44 u, half of that behind the root; mean, + eps,
           the reciprocal root (2 steps of fp32 = 4 u), the maximum (2 u), product, division: 22 + 1 + 1 + 4 + 2 + 1 + 1 = 32 u = 2^-19.
   product S to fp32, its product with scale_b, the fused multiply-add: (2 |t| + |z|) u, z = t + bias.  Activations change that by at most
           1.13 and add: sigmoid (and GELU's) relative 2^-21 (1 + |x|) of sigmoid(x), x GELU's inner argument with 5 u of its own;

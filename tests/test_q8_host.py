@@ -87,6 +87,8 @@ def test_gemm_q8_refuses():
         assert _gemm(**kw) == cf.ERR_ALIGNMENT, kw
     assert _gemm(K=131072, lda=131072, ldb=131072) == cf.ERR_UNSUPPORTED                        # sums may leave int32
     assert _gemm(N=65537, ldy=65544) == cf.ERR_UNSUPPORTED
+    for M in (2 ** 31 - 256, 2 ** 31 - 1):                                                      # a tile's last row is counted in 32 bits
+        assert _gemm(M=M) == cf.ERR_UNSUPPORTED
 
 
 bf, i8, f32 = torch.bfloat16, torch.int8, torch.float32
