@@ -5,7 +5,7 @@
 // more SMs).  Clusters of two are persistent and walk the tiles in bands of 8 row blocks, so that the tiles in flight share their
 // operands in the L2.  Two accumulators alternate: a tile's epilogue runs under the next one's products.
 //
-// Epilogue: thread = one row of the tile, 32 columns (16 with sixteen warps) at a time, a warp half or a quarter of the columns.  The
+// Epilogue: thread = one row of the tile, 32 columns (16 with sixteen warps in fp32) at a time, a warp half or a quarter of the columns.  The
 // channel's scale and bias come from shared memory (broadcast), the row's scale is a register.  Results leave as boxes of 32 rows x 128 bytes staged in shared memory and stored by
 // TMA; the residual comes in the same way, into the box that its sum leaves from.  A TMA store writes whole 16-byte units (measured: up to
 // seven bf16 behind the last column), so Y's map ends at the last whole unit and the columns behind it are stored one by one.
@@ -153,7 +153,8 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
   } else {
     // ------------------------------------------------------------------------------------------ epilogue warps
     const int e = warp - 2, q = warp & 3, part = e >> 2;  // TMEM lane quarter: rows 32q ..; which part of the columns
-    constexpr int S = EPW == 4 ? 16 : 32;                   // columns at a time (what the registers of that many warps hold)
+    // columns at a time (sixteen warps in fp32: what their registers hold; 16 bits with 16 columns 8192 x 4096 x 64 19.2 us, with 32 18.2)
+    constexpr int S = EPW == 4 && Elem<DT>::kBytes == 4 ? 16 : 32;
     constexpr int E = 128 / Elem<DT>::kBytes;               // columns of a box
     const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + part * Cfg::COLS;
     const uint32_t tempty = map_to_cta(bar_tempty(0), 0);
@@ -336,15 +337,18 @@ cudaError_t launch_instance(const GemmQ8PairMaps& maps, const GemmQ8Params& p, c
 }
 
 // Columns of a tile, stages of the ring, staging boxes an epilogue warp, epilogue warps a lane quarter.  Behind a long contraction the ring's
-// depth is what counts, behind a short one the epilogue: more boxes, or, where an activation makes its arithmetic long, more warps.  us, 8192 x
-// 4096 in bf16, 5 stages / 4 with two boxes / 4 with sixteen warps: K = 4096 86 / 94 / 98, K = 512 25.0 / 24.3 / 25.4, with GELU K = 512 42.0 / 42.3 / 38.4,
-// K = 1536 47.0 / 48.9 / 45.0, K = 2048 52.8 / 57.8 / 54.0; 96 x 504 x 504 x 64 21 / 19 / 20.  (A sixth stage, in the room of one of the two sets of scales:
-// between 3 % faster and 7 % slower from call to call under the power limit.)
+// depth is what counts, behind a short one the epilogue: more warps, which overlap each other's steps, or more boxes.  us, 8192 x 4096 bf16, 5
+// stages / 4 with two boxes / 4 with sixteen warps: K = 4096 86 / 94 / 98, K = 1024 - / 31 / 32, K = 768 - / 25.8 / 26.4, K = 512 25.0 / 23.5 / 20.7, with a
+// residual K = 768 - / 35.0 / 33.7, K = 512 - / 32.2 / 30.1, with GELU K = 512 42.0 / 40.6 / 31.6, K = 1536 47.0 / 48.9 / 41.9, K = 2048 52.8 / 57.8 / 54.0.
+// fp32: sixteen warps only where Y fits the L2; beyond it HBM takes their smaller pieces more slowly (eight / sixteen, K = 64: 96 x 504 x 504 22.3 / 19.8,
+// 8192 x 2048 16.2 / 16.3, 8192 x 4096 26.2 / 27.5, 148 x 512 x 512 30.3 / 32.1, with a residual 8192 x 4096 50.6 / 55.3).  (A sixth stage,
+// in the room of a box: between 3 % faster and 7 % slower from call to call under the power limit.)
 template <int DT>
 cudaError_t launch_columns(int columns, const GemmQ8PairMaps& maps, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
-  const bool long_epilogue = p.activation != 0 && p.activation != COMFUSE_OP_RELU;
   if (columns == 128) return launch_instance<DT, 128, 6, 2, 2>(maps, p, dev, stream);
-  if (long_epilogue && p.K <= 1536) return launch_instance<DT, 256, 4, 1, 4>(maps, p, dev, stream);
+  const bool long_epilogue = p.activation != 0 && p.activation != COMFUSE_OP_RELU;
+  const bool in_l2 = static_cast<long long>(p.batch) * p.M * p.N * Elem<DT>::kBytes <= 100ll << 20;
+  if (long_epilogue ? p.K <= 1536 : DT != COMFUSE_DTYPE_F32 ? p.K <= 768 : p.K <= 256 && !p.residual && in_l2) return launch_instance<DT, 256, 4, 1, 4>(maps, p, dev, stream);
   if (p.K <= 1024) return launch_instance<DT, 256, 4, 2, 2>(maps, p, dev, stream);
   return launch_instance<DT, 256, 5, 1, 2>(maps, p, dev, stream);
 }

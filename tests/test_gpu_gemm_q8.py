@@ -65,6 +65,18 @@ def test_batches(batch, M, N, K, cuda_device):
     run_case(M, N, K, "bf16", cuda_device, batch=batch, seed=batch + 1, extra=3, activation="gelu_tanh")
 
 
+@pytest.mark.parametrize("K", [64, 250, 300, 900, 1200])
+def test_rings_and_epilogue_warps_by_the_contraction(K, cuda_device):
+    """Tiles of 256 columns in every cut of the ring and of the epilogue: by type, length, residual, activation and the size of the result."""
+    for name in ("bf16", "f32"):
+        run_case(2900, 1801, K, name, cuda_device, residual=False, seed=K)
+        run_case(2817, 1807, K, name, cuda_device, residual=True, seed=K + 1, extra=1)
+        run_case(2900, 1799, K, name, cuda_device, residual=True, activation="sigmoid", seed=K + 2)
+    run_case(130, 504, K, "f32", cuda_device, batch=96, residual=False, seed=K + 3)
+    if K == 64:
+        run_case(7001, 4001, K, "f32", cuda_device, residual=False, seed=5)
+
+
 @pytest.mark.parametrize("M,N,K,batch", [(20, 300, 600, None), (2900, 1800, 140, None), (9, 33, 300, 4)])
 def test_in_place(M, N, K, batch, cuda_device):
     run_case(M, N, K, "bf16", cuda_device, batch=batch, in_place=True, extra=1)
