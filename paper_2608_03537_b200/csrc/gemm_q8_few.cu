@@ -299,7 +299,7 @@ cudaError_t launch_rows(int rows, const CUtensorMap& tmW, const CUtensorMap& tmX
 
 }  // namespace
 
-GemmQ8FewPlan gemm_q8_few_plan(int batch, int M, int N, int K, const DeviceInfo& dev) {
+GemmQ8FewPlan gemm_q8_few_plan(int batch, int M, int N, int K, bool long_epilogue, const DeviceInfo& dev) {
   GemmQ8FewPlan c;
   const int KB = (K + 127) / 128;
   c.rows = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
@@ -315,6 +315,16 @@ GemmQ8FewPlan gemm_q8_few_plan(int batch, int M, int N, int K, const DeviceInfo&
     const long long here = (tiles * c.split + dev.sm_count - 1) / dev.sm_count, pairs = dev.sm_count / 2;
     const long long there = (static_cast<long long>(batch) * ((M + 255ll) / 256) * ((N + 127) / 128) + pairs - 1) / pairs;
     if (here * (6.5 + 0.25 * KB / c.split) >= 3.5 + there * std::max(0.26 * KB, 1.7)) c.rows = 0;
+  }
+  // Fewer rows in more tiles than SMs (many channels, or batches): a CTA here does one tile and the next one's set-up starts behind it, while the tile
+  // kernel is persistent.  us, here / there: 96 x 40 x 1024 x 64 26.6 / 15.4, 96 x 20 x 504 x 256 12.0 / 10.3, 32 x 40 x 1024 x 256 9.6 / 8.4, 32 x 20 x 1024 x 256
+  // 7.9 / 8.1, 20 x 20000 x 1024 9.8 / 11.8, 64 x 65536 x 4096 61.7 / 57.6, 20 x 65536 x 4096 53 / 76; with GELU and a residual 50 x 30 x 900 x 100 13.6 / 15.7,
+  // 96 x 60 x 700 x 200 32.2 / 20.7.
+  if (M <= 64 && tiles > dev.sm_count) {
+    const long long here = (tiles + dev.sm_count - 1) / dev.sm_count, pairs = dev.sm_count / 2;  // rounds; tiles there have 256 columns then
+    const long long there = (static_cast<long long>(batch) * ((N + 255) / 256) + pairs - 1) / pairs;
+    if (here * (2.5 + 0.047 * M) + 0.34 * KB * tiles / dev.sm_count >= 4.0 + there * std::max(0.4 * KB + 0.6, long_epilogue ? 3.9 : 2.0))
+      c.rows = 0;
   }
   if (tiles * c.split > 0x7FFFFFFF) c.rows = 0;  // (a grid is counted in 32 bits)
   return c;

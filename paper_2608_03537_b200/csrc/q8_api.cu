@@ -109,7 +109,8 @@ comfuse_status_t comfuse_gemm_q8(const comfuse_gemm_q8_desc_t* desc, const int8_
     return launch_gemm_q8_tokens(d.dtype, t, p, *dev, st) == cudaSuccess ? COMFUSE_OK : COMFUSE_ERR_CUDA;
   }
   GemmQ8FewPlan few;
-  if (few_rows_enabled()) few = gemm_q8_few_plan(d.batch, d.M, d.N, d.K, *dev);
+  const bool long_epilogue = residual || (d.activation != 0 && d.activation != COMFUSE_OP_RELU);
+  if (few_rows_enabled()) few = gemm_q8_few_plan(d.batch, d.M, d.N, d.K, long_epilogue, *dev);
   constexpr CUtensorMapDataType kCodes = CU_TENSOR_MAP_DATA_TYPE_UINT8;
   const uint64_t bsa = stride(d.batch_stride_a, d.M, d.lda), bsb = stride(d.batch_stride_b, d.N, d.ldb);
   if (few.rows) {

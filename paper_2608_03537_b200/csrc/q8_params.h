@@ -50,7 +50,8 @@ cudaError_t launch_gemm_q8_tokens(int dtype, const GemmQ8TokensParams& t, GemmQ8
 struct GemmQ8FewPlan {
   int rows = 0, split = 1;
 };
-GemmQ8FewPlan gemm_q8_few_plan(int batch, int M, int N, int K, const DeviceInfo& dev);
+// long_epilogue: a residual, or an activation that is more than a comparison.
+GemmQ8FewPlan gemm_q8_few_plan(int batch, int M, int N, int K, bool long_epilogue, const DeviceInfo& dev);
 // tmW: the weights in boxes of 128 bytes x 128 rows, tmX: the rows in boxes of 128 bytes x plan.rows rows.
 cudaError_t launch_gemm_q8_few(int dtype, const GemmQ8FewPlan& plan, const CUtensorMap& tmW, const CUtensorMap& tmX, GemmQ8Params p, cudaStream_t stream);
 // Columns of Y that leave by TMA: up to the last whole 16-byte unit of a row.
