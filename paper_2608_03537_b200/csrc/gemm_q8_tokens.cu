@@ -165,17 +165,19 @@ bool gemm_q8_tokens_fits(int batch, int M, int N, int K, const DeviceInfo& dev) 
   if (M > kGemmQ8Tokens || batch > 65535) return false;
   // Where the weights are many enough that their stream is all that counts, the other form's deeper ring is ahead, up to one round of its
   // 128-channel tiles.  us, this form / that one: 1 row 4096 x 4096 5.5 / 6.7, 16384 x 4096 13.2 / 12.5, 65536 x 4096 43.6 / 48.9; 8 rows 6.0 / 6.8,
-  // 14.6 / 12.8, 49.9 / 50.2; 16 rows 1024 x 1024 2.8 / 3.8, 4096 x 4096 6.7 / 6.9, 16384 x 4096 17.6 / 13.1.
+  // 14.6 / 12.8, 49.9 / 50.2; 16 rows 1024 x 1024 2.3 / 3.8, 4096 x 4096 6.3 / 6.9, 16384 x 4096 17.6 / 13.1; batches 32 x 16 x 1024 x 256 7.3 / 7.9, 96 x 16 x 504 x 64
+  // 12.4 / 9.6, 96 x 16 x 1024 x 256 19.8 / 16.5.
   const long long codes = static_cast<long long>(batch) * N * K, tiles = static_cast<long long>(batch) * ((N + 127) / 128);
-  return M <= 8 ? codes <= 3ll << 24 || tiles > dev.sm_count : codes <= 1ll << 25;
+  return M <= 8 ? codes <= 3ll << 24 || tiles > dev.sm_count : codes <= 1ll << 25 && tiles <= 2ll * dev.sm_count;
 }
 
 cudaError_t launch_gemm_q8_tokens(int dtype, const GemmQ8TokensParams& t, GemmQ8Params p, const DeviceInfo& dev, cudaStream_t stream) {
   // Shares: up to the 16 warps that an SM holds, while each has a step.  us with 1 / 2 / 4 / 8 shares (8 rows): 4096 x 4096 12.9 / 9.8 / 7.0 / 5.9,
-  // 16384 x 4096 18.2 / 14.0 / 14.7 / 15.9, 1024 x 1024 5.1 / 3.3 / 2.9 / 2.4.
+  // 16384 x 4096 18.2 / 14.0 / 14.7 / 15.9, 1024 x 1024 5.1 / 3.3 / 2.9 / 2.4; a few CTAs more than fit at once cost a second round (1 row 5120 x 1024 with
+  // 4 / 8 shares 3.4 / 4.8, 20 batches of 1024 x 256 with 1 / 2 3.3 / 4.9).
   const long long groups = static_cast<long long>(p.batch) * ((p.N + kChannels - 1) / kChannels);
   p.split = 1;
-  while (p.split < kWarps && groups * p.split * 2 <= 18ll * dev.sm_count && p.K > p.split * 128) p.split *= 2;
+  while (p.split < kWarps && groups * p.split * 2 <= 16ll * dev.sm_count && p.K > p.split * 128) p.split *= 2;
   switch (dtype) {
     case COMFUSE_DTYPE_BF16: return launch_rows<COMFUSE_DTYPE_BF16>(t, p, stream);
     case COMFUSE_DTYPE_F16: return launch_rows<COMFUSE_DTYPE_F16>(t, p, stream);

@@ -60,7 +60,7 @@ def test_activations_and_absent_operands(M, N, K, activation, cuda_device):
 
 
 @pytest.mark.parametrize("batch,M,N,K", [(1, 5, 40, 64), (3, 1, 1000, 300), (5, 33, 129, 65), (96, 126, 126, 64), (7, 600, 1500, 80), (96, 20, 504, 64),
-                                         (60, 50, 520, 300), (30, 40, 1020, 70)])
+                                         (60, 50, 520, 300), (30, 40, 1020, 70), (96, 16, 500, 70)])
 def test_batches(batch, M, N, K, cuda_device):
     run_case(M, N, K, "f32", cuda_device, batch=batch, seed=batch)
     run_case(M, N, K, "bf16", cuda_device, batch=batch, seed=batch + 1, extra=3, activation="gelu_tanh")
