@@ -6,8 +6,8 @@
 // operands in the L2.  Two accumulators alternate: a tile's epilogue runs under the next one's products.
 //
 // Epilogue: thread = one row of the tile, 32 columns (16 with sixteen warps in fp32) at a time, a warp half or a quarter of the columns.  The
-// channel's scale and bias come from shared memory (broadcast), the row's scale is a register.  Results leave as boxes of 32 rows x 128 bytes staged in shared memory and stored by
-// TMA; the residual comes in the same way, into the box that its sum leaves from.  A TMA store writes whole 16-byte units (measured: up to
+// channel's scale and bias come from shared memory (broadcast), the row's scale is a register.  Results leave as boxes of 32 rows x 128 bytes
+// staged in shared memory and stored by TMA; the residual comes in the same way, into the box that its sum leaves from.  A TMA store writes whole 16-byte units (measured: up to
 // seven bf16 behind the last column), so Y's map ends at the last whole unit and the columns behind it are stored one by one.
 #include <algorithm>
 #include <type_traits>

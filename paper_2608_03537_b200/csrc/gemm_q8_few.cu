@@ -112,9 +112,17 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads, 1) gemm_q8_few_kernel(co
       const int r = row + k * Cfg::kEpiWarps;
       if (r < row1) {
         sa[k] = __ldg(scale_a + r);
-        if (p.residual && whole) {
-          if constexpr (Elem<DT>::kBytes == 4) ld_16(res + r * p.ldr * 4, rw[k]);
-          else ld_8(res + r * p.ldr * 2, rw[k]);
+        if (p.residual) {
+          const char* from = res + r * p.ldr * Elem<DT>::kBytes;
+          if (whole) {
+            if constexpr (Elem<DT>::kBytes == 4) ld_16(from, rw[k]);
+            else ld_8(from, rw[k]);
+          } else {
+            float e[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = col + i < p.N ? Elem<DT>::get(from, i) : 0.f;
+            Elem<DT>::pack(e, rw[k]);
+          }
         }
       }
     }
@@ -218,11 +226,11 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads, 1) gemm_q8_few_kernel(co
         for (int i = 0; i < 4; ++i) z[i] = fmaf(static_cast<float>(acc[k][i]) * sb[i], sa[k], bias[i]);
         activate(z, p.activation);
         char* to = out + r * p.ldy * Elem<DT>::kBytes;
-        if (whole) {
-          if (p.residual) {
+        if (p.residual) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[i] += Elem<DT>::of(rw[k], i);
-          }
+          for (int i = 0; i < 4; ++i) z[i] += Elem<DT>::of(rw[k], i);
+        }
+        if (whole) {
           uint32_t ow[Elem<DT>::kBytes];
           Elem<DT>::pack(z, ow);
           if (COMFUSE_IN_BOUNDS(m0 + r < p.M && col + 3 < p.N && b < p.batch, p.status)) {
@@ -232,7 +240,7 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads, 1) gemm_q8_few_kernel(co
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (col + i < p.N) Elem<DT>::put(to, i, p.residual ? z[i] + Elem<DT>::get(res + r * p.ldr * Elem<DT>::kBytes, i) : z[i]);
+            if (col + i < p.N) Elem<DT>::put(to, i, z[i]);
         }
       }
       row += RB * Cfg::kEpiWarps;
@@ -300,33 +308,42 @@ cudaError_t launch_rows(int rows, const CUtensorMap& tmW, const CUtensorMap& tmX
 }  // namespace
 
 GemmQ8FewPlan gemm_q8_few_plan(int batch, int M, int N, int K, bool long_epilogue, const DeviceInfo& dev) {
+  // Both this form's cut and the choice between it and the tile kernel by estimates of their times in us, fitted to 4238 cuts of 368 calls (20 .. 400
+  // rows, 128 .. 16384 channels, 128 .. 16384 codes a row; the cut that they choose is 1 % above the fastest on average, 11 % at worst).
+  //   * A CTA does one tile and the next one's set-up starts behind it, so a round of tiles costs its whole latency: set-up, the rows' epilogue, the K
+  //     blocks, and, where shares meet, the cluster's barriers.  Groups of 16 rows read the weights again for each group, out of the L2; small weights
+  //     are cheaper to read often than their epilogue is to do in one CTA: us with 16 / 64 rows a CTA, 64 x 1024 x 128 3.0 / 4.7, 64 x 1024 x 1024 4.0 / 5.0.
+  //   * Shares keep 4 K blocks each, and more clusters than fit at once are another round (16 of 8 CTAs do not fit: 256 x 1024 x 8192 17.4 as
+  //     those, 8.7 as 32 of 4).
+  //   * The tile kernel is persistent: many short tiles are cheaper there (96 x 40 x 1024 x 64 15.4 us, 26.6 here; 64 x 4096 x 8192 17.4, 10.1 here).
   GemmQ8FewPlan c;
   const int KB = (K + 127) / 128;
-  c.rows = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
-  const long long tiles = static_cast<long long>(batch) * ((M + c.rows - 1ll) / c.rows) * ((N + 127) / 128);
-  const int most = tiles < dev.sm_count ? static_cast<int>(dev.sm_count / tiles) : 1;
-  // Shares: while one keeps 4 K blocks, and behind less than 64 K blocks no more than fill two thirds of the SMs.  us with 1 / 2 / 3 / 4 shares
-  // (40 rows): 4096 x 4096 9.5 / 7.7 / 7.7 / 8.0, 4096 x 16384 23.0 / 16.4 / 15.2 / 15.3, 1024 x 1024 4.8 / 4.3 / 4.4 / 4.5.
-  const long long want = KB >= 64 ? most : 2ll * dev.sm_count / 3 / tiles;
-  c.split = static_cast<int>(std::min<long long>({8, most, std::max<long long>(want, 2), std::max(KB / 4, 1)}));
-  // Where the rows fill 64 and more of the UMMA's columns the tile kernel is in reach: both times by their K blocks, fitted to 64 .. 256 rows
-  // (4096 x 4096, 256 rows: 12.1 us here, 11.9 there; 4096 x 16384 22.4 / 32.7; 1024 x 1024 7.2 / 6.2; 16384 x 4096 36 / 22).
-  if (M > 64) {
-    const long long here = (tiles * c.split + dev.sm_count - 1) / dev.sm_count, pairs = dev.sm_count / 2;
-    const long long there = (static_cast<long long>(batch) * ((M + 255ll) / 256) * ((N + 127) / 128) + pairs - 1) / pairs;
-    if (here * (6.5 + 0.25 * KB / c.split) >= 3.5 + there * std::max(0.26 * KB, 1.7)) c.rows = 0;
+  const long long ntiles = static_cast<long long>(batch) * ((N + 127) / 128);
+  static ResidentClusters resident;  // (every instance has an SM to itself)
+  double best = 1e30;
+  for (const int rows : {16, 32, 64, 128}) {
+    if (rows > 16 && M <= rows / 2) break;
+    const long long tiles = ntiles * ((M + rows - 1ll) / rows);
+    for (const int split : {1, 2, 3, 4, 6, 8}) {
+      if (split > 1 && (split * 4 > KB || tiles * split > dev.sm_count)) break;
+      int at_once = dev.sm_count;
+      if (split > 1)
+        at_once = std::max(1, resident.of(reinterpret_cast<const void*>(gemm_q8_few_kernel<COMFUSE_DTYPE_BF16, 64>), FewCfg<64>::kThreads, FewCfg<64>::SMEM_BYTES, split, dev));
+      const double rounds = static_cast<double>((tiles + at_once - 1) / at_once);
+      double us = rounds * (2.3 + (long_epilogue ? 0.06 : 0.032) * std::min(M, rows) + 0.144 * ((KB + split - 1) / split)) + 1.6e-8 * tiles * (128. + rows) * K;
+      if (split > 1) us += 1.2 * rounds + 0.6 * static_cast<double>(tiles * split) / dev.sm_count;
+      if (us < best && tiles * split <= 0x7FFFFFFF) {  // (a grid is counted in 32 bits)
+        best = us;
+        c.rows = rows;
+        c.split = split;
+      }
+    }
   }
-  // Fewer rows in more tiles than SMs (many channels, or batches): a CTA here does one tile and the next one's set-up starts behind it, while the tile
-  // kernel is persistent.  us, here / there: 96 x 40 x 1024 x 64 26.6 / 15.4, 96 x 20 x 504 x 256 12.0 / 10.3, 32 x 40 x 1024 x 256 9.6 / 8.4, 32 x 20 x 1024 x 256
-  // 7.9 / 8.1, 20 x 20000 x 1024 9.8 / 11.8, 64 x 65536 x 4096 61.7 / 57.6, 20 x 65536 x 4096 53 / 76; with GELU and a residual 50 x 30 x 900 x 100 13.6 / 15.7,
-  // 96 x 60 x 700 x 200 32.2 / 20.7.
-  if (M <= 64 && tiles > dev.sm_count) {
-    const long long here = (tiles + dev.sm_count - 1) / dev.sm_count, pairs = dev.sm_count / 2;  // rounds; tiles there have 256 columns then
-    const long long there = (static_cast<long long>(batch) * ((N + 255) / 256) + pairs - 1) / pairs;
-    if (here * (2.5 + 0.047 * M) + 0.34 * KB * tiles / dev.sm_count >= 4.0 + there * std::max(0.4 * KB + 0.6, long_epilogue ? 3.9 : 2.0))
-      c.rows = 0;
-  }
-  if (tiles * c.split > 0x7FFFFFFF) c.rows = 0;  // (a grid is counted in 32 bits)
+  const bool narrow = gemm_q8_pair_columns(batch, M, N, dev) == 128;
+  const long long there = static_cast<long long>(batch) * ((M + 255ll) / 256) * (narrow ? (N + 127) / 128 : (N + 255) / 256), pairs = dev.sm_count / 2;
+  const double round = narrow ? std::max(0.26 * KB, 1.55) : std::max(0.35 * KB + 0.65, long_epilogue ? 3.9 : 2.0);
+  const double around = narrow ? (long_epilogue ? 4.3 : 2.8) : 3.5;
+  if (best >= around + round * static_cast<double>((there + pairs - 1) / pairs)) c.rows = 0;
   return c;
 }
 

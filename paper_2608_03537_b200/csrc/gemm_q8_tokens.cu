@@ -3,7 +3,7 @@
 // What bounds it: the weights' bytes and the latency of one pass.  The tensor memory, barriers and descriptors of the other forms are
 // latency that so few products do not repay; here a warp asks for its weights with its first instructions and multiplies them in registers.
 //
-//   * A warp multiplies 16 channels by 8 rows (or 16, 32) with the warp-wide integer instruction (16 x 8 x 32).  Which 32 bytes of the
+//   * A warp multiplies 16 channels by 8 rows (or 16) with the warp-wide integer instruction (16 x 8 x 32).  Which 32 bytes of the
 //     contraction an instruction takes is free as long as both operands take the same ones, so a lane loads 16 consecutive bytes of its
 //     channel and of its row and feeds two instructions with them: 64 bytes of 8 channels a load.  (Four-byte dot products on
 //     the ordinary pipe instead: 4096 x 4096 for 1 / 4 / 8 rows 3.9 / 6.9 / 17.7 us.)

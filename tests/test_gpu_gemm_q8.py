@@ -1,5 +1,5 @@
 """The int8 product with a scale for each row and channel (comfuse_gemm_q8) against fp64, whose sums are exact: one row to many, every cut
-of the form for few rows (groups of 16 to 256 rows, 1 to 8 shares of the contraction) and of the tile kernel, sizes that fit
+of the form for few rows (groups of 16 to 128 rows, 1 to 8 shares of the contraction) and of the tile kernel, sizes that fit
 nothing, batches, types, activations, extreme codes, NaN scales, in place, streams and captured graphs."""
 import os
 import subprocess
@@ -42,7 +42,7 @@ def run_case(M, N, K, name, device, batch=None, activation=None, bias=True, resi
 
 SIZES = [(1, 1, 1), (1, 4096, 4096), (2, 5, 17), (3, 130, 31), (15, 128, 128), (16, 127, 129), (17, 129, 640), (31, 257, 1000), (33, 1000, 2049), (64, 640, 1300), (65, 256, 300), (100, 1001, 700),
          (128, 384, 2056), (129, 200, 515), (200, 1300, 4100), (256, 640, 256), (257, 3, 4), (300, 777, 1032), (513, 1024, 64), (700, 72, 5000), (1000, 1000, 100),
-         (12, 8200, 4100), (8, 20000, 2700), (60, 40000, 260), (90, 300, 20000), (520, 4000, 300), (5000, 100, 700),
+         (100, 128, 1024), (70, 4001, 500), (100, 1030, 8192), (127, 2050, 8200), (250, 120, 3000), (12, 8200, 4100), (8, 20000, 2700), (60, 40000, 260), (90, 300, 20000), (520, 4000, 300), (5000, 100, 700),
          (3000, 1700, 300), (2817, 2001, 131), (40000, 8, 64)]
 
 
