@@ -247,3 +247,55 @@ def test_another_stream_and_captured_graphs(cuda_device):
         for a, sa, y, graph in sets:
             want = ((a.double() @ w.double().mT) * sa.double()[:, None] * sw.double()).clamp_min(0)
             assert ((y.double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -20)).all()
+
+
+FIRST = """
+import torch
+import paper_2608_03537_b200 as cf
+d = torch.device("cuda:0")
+K, N = 8192, 1024
+w, sw = torch.randint(-127, 128, (N, K), dtype=torch.int8, device=d), torch.rand(N, device=d)
+sets = [(torch.randn(M, K, device=d), torch.zeros(M, K, dtype=torch.int8, device=d), torch.zeros(M, device=d), torch.zeros(M, N, device=d)) for M in (1, 40, 250, 3000)]
+graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph, stream=side):
+    for x, q, s, y in sets:
+        cf.quantize_rows(x, q, s)
+        cf.gemm_q8(q, s, w, sw, y)
+graph.replay()
+torch.cuda.synchronize()
+for x, q, s, y in sets:
+    want = (q.double() @ w.double().mT) * s.double()[:, None] * sw.double()
+    assert bool((s > 0).all()) and ((y.double() - want).abs() <= want.abs() * 2.0 ** -20).all(), x.shape
+assert cf.last_device_status() == cf.OK
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured(cuda_device):
+    """Nothing that a form sets up on its first call (attributes, how many clusters fit) disturbs a capture."""
+    r = subprocess.run([sys.executable, "-c", FIRST], cwd=ROOT, env=dict(os.environ, PYTHONPATH=ROOT), capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-1000:] + r.stderr[-3000:]
+
+
+def test_threads_with_streams_of_their_own(cuda_device):
+    """Calls from several threads at once, each on its stream: every form, eager."""
+    from concurrent.futures import ThreadPoolExecutor
+    K, N = 2048, 1000
+    w, sw = torch.randint(-127, 128, (N, K), dtype=torch.int8, device=cuda_device), torch.rand(N, device=cuda_device)
+
+    def work(M):
+        torch.cuda.set_device(cuda_device)
+        side = torch.cuda.Stream()
+        x = torch.randn(M, K, device=cuda_device)
+        q, s, y = torch.empty(M, K, dtype=torch.int8, device=cuda_device), torch.empty(M, device=cuda_device), torch.empty(M, N, device=cuda_device)
+        side.wait_stream(torch.cuda.current_stream())
+        for _ in range(50):
+            cf.quantize_rows(x, q, s, stream=side)
+            cf.gemm_q8(q, s, w, sw, y, stream=side)
+        side.synchronize()
+        want = (q.double() @ w.double().mT) * s.double()[:, None] * sw.double()
+        return bool(((y.double() - want).abs() <= want.abs() * 2.0 ** -20).all())
+
+    torch.cuda.synchronize()
+    with ThreadPoolExecutor(4) as pool:
+        assert all(pool.map(work, (1, 40, 300, 3000)))
