@@ -176,12 +176,12 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
       if (tile >= tiles) return;
       decode(tile, b, m0, n0);
       const int row = m0 + static_cast<int>(rank) * 128 + q * 32 + lane;
-      sa = row < p.M ? __ldg(p.scale_a + static_cast<long long>(b) * p.M + row) : 0.f;
+      sa = row < p.M ? p.scale_a[static_cast<long long>(b) * p.M + row] : 0.f;
 #pragma unroll
       for (int i = 0; i < C; ++i) {
         const int c = n0 + part * Cfg::COLS + 32 * i + lane;
-        scale[i] = c < p.N ? __ldg(p.scale_b + static_cast<long long>(b) * p.N + c) : 0.f;
-        bias[i] = p.bias && c < p.N ? __ldg(static_cast<const Word*>(p.bias) + c) : static_cast<Word>(0);
+        scale[i] = c < p.N ? p.scale_b[static_cast<long long>(b) * p.N + c] : 0.f;
+        bias[i] = p.bias && c < p.N ? static_cast<const Word*>(p.bias)[c] : static_cast<Word>(0);
       }
     };
     fetch(cluster_id);

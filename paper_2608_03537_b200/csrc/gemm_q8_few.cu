@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads, 1) gemm_q8_few_kernel(co
     for (int k = 0; k < RB; ++k) {
       const int r = row + k * Cfg::kEpiWarps;
       if (r < row1) {
-        sa[k] = __ldg(scale_a + r);
+        sa[k] = scale_a[r];
         if (p.residual) {
           const char* from = res + r * p.ldr * Elem<DT>::kBytes;
           if (whole) {
@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads, 1) gemm_q8_few_kernel(co
     fetch();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      sb[i] = col + i < p.N ? __ldg(p.scale_b + static_cast<long long>(b) * p.N + col + i) : 0.f;
+      sb[i] = col + i < p.N ? p.scale_b[static_cast<long long>(b) * p.N + col + i] : 0.f;
       bias[i] = p.bias && col + i < p.N ? Elem<DT>::get(p.bias, col + i) : 0.f;
     }
     mbar_wait<false>(bar_acc, 0, w);

@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) gemm_q8_tokens_kernel(const Ge
     if (col < p.N) {
       int s = 0;
       for (int j = 0; j < p.split; ++j) s += s_part[(j * ROWS + m) * channels + c];
-      const float sb = __ldg(p.scale_b + static_cast<long long>(b) * p.N + col), sa = __ldg(p.scale_a + static_cast<long long>(b) * p.M + m);
+      const float sb = p.scale_b[static_cast<long long>(b) * p.N + col], sa = p.scale_a[static_cast<long long>(b) * p.M + m];
       float z[1] = {fmaf(static_cast<float>(s) * sb, sa, p.bias ? Elem<DT>::get(p.bias, col) : 0.f)};
       activate(z, p.activation);
       if (p.residual) z[0] += Elem<DT>::get(p.residual, b * p.batch_stride_r + m * p.ldr + col);

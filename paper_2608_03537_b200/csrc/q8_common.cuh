@@ -43,7 +43,9 @@ struct Elem {
   }
 };
 
-// Data that is read or written once, by one thread: past the L1.  (Not the read-only path: outputs may be an input, in place.)
+// No load of these kernels takes the read-only path (__ldg): with programmatic launch they are on the SMs while the kernels in front of them
+// still write scales and rows, and that path is for data that nobody writes while a kernel runs; it may also be an output, in place.
+// Data that is read or written once, by one thread: past the L1.
 __device__ __forceinline__ void ld_16(const void* p, uint32_t* w) {
   asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
 }

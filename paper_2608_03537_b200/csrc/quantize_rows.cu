@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kMaxThreads) quantize_rows_kernel(const Quanti
         const uint4* at = reinterpret_cast<const uint4*>(static_cast<const char*>(p.gamma) + c * kChunk);
 #pragma unroll
         for (int k = 0; k < kWords / 4; ++k) {
-          const uint4 v = __ldg(at + k);
+          const uint4 v = at[k];
           g[j][4 * k] = v.x; g[j][4 * k + 1] = v.y; g[j][4 * k + 2] = v.z; g[j][4 * k + 3] = v.w;
         }
       }
