@@ -143,7 +143,7 @@ __device__ __forceinline__ void load_mask_32(const uint16_t* seg, int valid, flo
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint4 q = make_uint4(0u, 0u, 0u, 0u);
-    if (8 * i < valid) q = __ldg(reinterpret_cast<const uint4*>(seg) + i);
+    if (8 * i < valid) q = ld_ordinary(reinterpret_cast<const uint4*>(seg) + i);
     const uint32_t w4[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) m2[4 * i + k] = bf16x2_to_f2(w4[k]);

@@ -265,9 +265,9 @@ few_rows_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     for (int t = 0; t < NT; ++t) {
       col[t] = n0 + t * 128 + 4 * lane;
       in[t] = col[t] < p.N;  // (N is a multiple of 8: a group of four is inside or outside)
-      bias[t] = p.bias && in[t] ? __ldg(reinterpret_cast<const uint2*>(p.bias + col[t])) : zero;
-      gamma[t] = p.gamma && in[t] ? __ldg(reinterpret_cast<const uint2*>(p.gamma + col[t])) : one;
-      beta[t] = EPI == EPI_LN && p.beta && in[t] ? __ldg(reinterpret_cast<const uint2*>(p.beta + col[t])) : zero;
+      bias[t] = p.bias && in[t] ? ld_ordinary(reinterpret_cast<const uint2*>(p.bias + col[t])) : zero;
+      gamma[t] = p.gamma && in[t] ? ld_ordinary(reinterpret_cast<const uint2*>(p.gamma + col[t])) : one;
+      beta[t] = EPI == EPI_LN && p.beta && in[t] ? ld_ordinary(reinterpret_cast<const uint2*>(p.beta + col[t])) : zero;
     }
     const int row0 = m0 + ks * rs;  // first row of the slice
     // asked for while the MainLoop runs: the rows' residual
@@ -279,9 +279,9 @@ few_rows_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
       for (int t = 0; t < NT; ++t) {
         res[i][t] = zero;
         if (EPI == EPI_SOFTMAX && p.mask && r < rv && in[t])  // (the mask is the softmax kind's full-tensor operand)
-          res[i][t] = __ldg(reinterpret_cast<const uint2*>(p.mask + static_cast<long long>(row0 + r) * p.N + col[t]));
+          res[i][t] = ld_ordinary(reinterpret_cast<const uint2*>(p.mask + static_cast<long long>(row0 + r) * p.N + col[t]));
         if (EPI != EPI_SOFTMAX && p.residual && r < rv && in[t])
-          res[i][t] = __ldg(reinterpret_cast<const uint2*>(p.residual + static_cast<long long>(b) * p.batch_stride_r +
+          res[i][t] = ld_ordinary(reinterpret_cast<const uint2*>(p.residual + static_cast<long long>(b) * p.batch_stride_r +
                                                            static_cast<long long>(row0 + r) * p.ldr + col[t]));
       }
     }

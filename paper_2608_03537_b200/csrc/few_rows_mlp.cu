@@ -187,19 +187,19 @@ few_rows_mlp_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_consta
     const int q = warp & 3;  // TMEM lane quarter: hidden units / output columns 32q .. 32q+31
     const int h = e >> 2;    // rows h * MOVE .. of what this warp takes out of tensor memory
     const int unit = q * 32 + lane;
-    const float b1 = p.b1 && n0 + unit < p.N1 ? bf16_lo(__ldg(p.b1 + n0 + unit)) : 0.f;  // (units from N1 on: zeros all the way)
+    const float b1 = p.b1 && n0 + unit < p.N1 ? bf16_lo(ld_ordinary(p.b1 + n0 + unit)) : 0.f;  // (units from N1 on: zeros all the way)
     // row stage: lane = columns 4 lane .. 4 lane + 3, rows e, e + 16, ... of the slice
     const uint2 zero = make_uint2(0u, 0u), one = make_uint2(0x3F803F80u, 0x3F803F80u);
-    const uint2 b2 = p.b2 ? __ldg(reinterpret_cast<const uint2*>(p.b2) + lane) : zero;
-    const uint2 gamma = p.gamma ? __ldg(reinterpret_cast<const uint2*>(p.gamma) + lane) : one;
-    const uint2 beta = p.beta ? __ldg(reinterpret_cast<const uint2*>(p.beta) + lane) : zero;
+    const uint2 b2 = p.b2 ? ld_ordinary(reinterpret_cast<const uint2*>(p.b2) + lane) : zero;
+    const uint2 gamma = p.gamma ? ld_ordinary(reinterpret_cast<const uint2*>(p.gamma) + lane) : one;
+    const uint2 beta = p.beta ? ld_ordinary(reinterpret_cast<const uint2*>(p.beta) + lane) : zero;
     const int row0 = m0 + rank * rs;
     uint2 res[RC];
 #pragma unroll
     for (int i = 0; i < RC; ++i) {
       const int r = e + i * Cfg::kEpiWarps;
       res[i] = zero;
-      if (r < rv) res[i] = __ldg(reinterpret_cast<const uint2*>(p.X + static_cast<long long>(row0 + r) * 128) + lane);
+      if (r < rv) res[i] = ld_ordinary(reinterpret_cast<const uint2*>(p.X + static_cast<long long>(row0 + r) * 128) + lane);
     }
 
     mbar_wait<false>(bar_d1, 0, w);

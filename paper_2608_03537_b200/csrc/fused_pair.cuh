@@ -573,7 +573,7 @@ fused_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                   float2 bb = splat2(0.f);
-                  if (p.bias && c0 + 2 * j < p.N) bb = bf16x2_to_f2(__ldg(reinterpret_cast<const uint32_t*>(p.bias + c0) + j));
+                  if (p.bias && c0 + 2 * j < p.N) bb = bf16x2_to_f2(ld_ordinary(reinterpret_cast<const uint32_t*>(p.bias + c0) + j));
                   float2 z = fma2(al, f2_from_bits(v[2 * j], v[2 * j + 1]), bb);
                   switch (p.activation) {
                     case COMFUSE_OP_RELU: z = make_float2(fmaxf(z.x, 0.f), fmaxf(z.y, 0.f)); break;

@@ -10,6 +10,7 @@
 
 #include "host_common.h"
 #include "row_params.h"
+#include "sm100_primitives.cuh"
 
 namespace comfuse {
 namespace {
@@ -300,8 +301,8 @@ __global__ void __launch_bounds__(256) wide_row_finish_kernel(const RowParams p,
       if (vi >= nvec) continue;
       float xf[8], gf[8], bf[8], o[8];
       unpack8_f16(xq[u], xf);
-      unpack8(p.gamma ? __ldg(reinterpret_cast<const uint4*>(p.gamma) + vi) : one, gf);
-      unpack8((KIND == EPI_LN && p.beta) ? __ldg(reinterpret_cast<const uint4*>(p.beta) + vi) : make_uint4(0, 0, 0, 0), bf);
+      unpack8(p.gamma ? ld_ordinary(reinterpret_cast<const uint4*>(p.gamma) + vi) : one, gf);
+      unpack8((KIND == EPI_LN && p.beta) ? ld_ordinary(reinterpret_cast<const uint4*>(p.beta) + vi) : make_uint4(0, 0, 0, 0), bf);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if constexpr (KIND == EPI_LN) {
@@ -354,8 +355,8 @@ __global__ void __launch_bounds__(256) wide_row_finish_block_kernel(const RowPar
   for (int u = 0; u < VPT; ++u) {
     const int vi = threadIdx.x + u * 256;
     if (vi < nvec) xq[u] = __ldcs(reinterpret_cast<const uint4*>(y) + vi);
-    gq[u] = p.gamma && vi < nvec ? __ldg(reinterpret_cast<const uint4*>(p.gamma) + vi) : one;
-    bq[u] = KIND == EPI_LN && p.beta && vi < nvec ? __ldg(reinterpret_cast<const uint4*>(p.beta) + vi) : make_uint4(0, 0, 0, 0);
+    gq[u] = p.gamma && vi < nvec ? ld_ordinary(reinterpret_cast<const uint4*>(p.gamma) + vi) : one;
+    bq[u] = KIND == EPI_LN && p.beta && vi < nvec ? ld_ordinary(reinterpret_cast<const uint4*>(p.beta) + vi) : make_uint4(0, 0, 0, 0);
   }
   // every warp merges the row's partials on its own: lane k takes blocks k, k + 32, ...
   const float2* q = partials + r * nblocks;
@@ -399,8 +400,8 @@ __global__ void __launch_bounds__(256) wide_row_finish_block_kernel(const RowPar
       if (vi >= nvec) continue;
       float xf[8], gf[8], bf[8], o[8];
       unpack8_f16(v0 == 0 ? xq[u] : __ldcs(reinterpret_cast<const uint4*>(y) + vi), xf);
-      unpack8(v0 == 0 ? gq[u] : p.gamma ? __ldg(reinterpret_cast<const uint4*>(p.gamma) + vi) : one, gf);
-      unpack8(v0 == 0 ? bq[u] : KIND == EPI_LN && p.beta ? __ldg(reinterpret_cast<const uint4*>(p.beta) + vi) : make_uint4(0, 0, 0, 0), bf);
+      unpack8(v0 == 0 ? gq[u] : p.gamma ? ld_ordinary(reinterpret_cast<const uint4*>(p.gamma) + vi) : one, gf);
+      unpack8(v0 == 0 ? bq[u] : KIND == EPI_LN && p.beta ? ld_ordinary(reinterpret_cast<const uint4*>(p.beta) + vi) : make_uint4(0, 0, 0, 0), bf);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if constexpr (KIND == EPI_LN) {

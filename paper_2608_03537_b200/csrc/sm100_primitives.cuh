@@ -72,6 +72,12 @@ __device__ __forceinline__ void cluster_sync_after_init() {
 // kernel must execute it before its first access to global memory.  Both are no-ops without such a dependency.
 __device__ __forceinline__ void griddep_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// What a kernel that waits so reads: an ordinary load, behind the wait.  Never __ldg: the kernel is on the SMs while those in front of it still write,
+// and the read-only path is for data that nobody writes meanwhile (it may load ahead of the wait, or from an older line of the L1).
+template <typename T>
+__device__ __forceinline__ T ld_ordinary(const T* p) {
+  return *p;
+}
 
 __device__ __forceinline__ void named_barrier_sync(int id, int nthreads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
