@@ -94,6 +94,11 @@ bool leader_reduce_enabled() {
   return on;
 }
 
+bool verbose_enabled() {
+  static const bool on = std::getenv("COMFUSE_VERBOSE") != nullptr;
+  return on;
+}
+
 bool programmatic_launch_enabled() {
   static const bool on = [] {
     const char* e = std::getenv("COMFUSE_PDL");

@@ -10,6 +10,7 @@
 // staged in shared memory and stored by TMA; the residual comes in the same way, into the box that its sum leaves from.  A TMA store writes whole 16-byte units (measured: up to
 // seven bf16 behind the last column), so Y's map ends at the last whole unit and the columns behind it are stored one by one.
 #include <algorithm>
+#include <cstdio>
 #include <type_traits>
 
 #include "q8_common.cuh"
@@ -318,6 +319,9 @@ cudaError_t launch_instance(const GemmQ8PairMaps& maps, const GemmQ8Params& p, c
   static ResidentClusters resident;  // (sets the kernel's attributes on the device the first time it is asked)
   const int fit = resident.of(reinterpret_cast<const void*>(kern), Cfg::kThreads, Cfg::SMEM_BYTES, 2, dev);
   if (fit < 1) return cudaErrorLaunchOutOfResources;
+  if (verbose_enabled())
+    std::fprintf(stderr, "comfuse: gemm_q8 dtype=%d: pairs, columns=%d stages=%d boxes=%d epilogue_warps=%d, %lld tiles on %d pairs\n", DT, BN, STAGES, BOXES,
+                 Cfg::kEpiWarps, p.tiles, fit);
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   cfg.gridDim = dim3(static_cast<unsigned>(2 * std::min<long long>(p.tiles, fit)), 1, 1);

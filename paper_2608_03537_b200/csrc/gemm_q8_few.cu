@@ -7,6 +7,7 @@
 // distributed shared memory and finishes it, a warp per row and 4 channels per lane.  Integer sums are exact, so the split changes no bit
 // of the result.
 #include <algorithm>
+#include <cstdio>
 #include <type_traits>
 
 #include "q8_common.cuh"
@@ -352,6 +353,9 @@ cudaError_t launch_gemm_q8_few(int dtype, const GemmQ8FewPlan& plan, const CUten
   p.mtiles = (p.M + plan.rows - 1) / plan.rows;
   p.ntiles = (p.N + 127) / 128;
   p.tiles = static_cast<long long>(p.batch) * p.mtiles * p.ntiles;
+  if (verbose_enabled())
+    std::fprintf(stderr, "comfuse: gemm_q8 dtype=%d: few rows, rows=%d shares=%d long_epilogue=%d\n", dtype, plan.rows, plan.split,
+                 p.residual || (p.activation != 0 && p.activation != COMFUSE_OP_RELU));
   switch (dtype) {
     case COMFUSE_DTYPE_BF16: return launch_rows<COMFUSE_DTYPE_BF16>(plan.rows, tmW, tmX, p, stream);
     case COMFUSE_DTYPE_F16: return launch_rows<COMFUSE_DTYPE_F16>(plan.rows, tmW, tmX, p, stream);

@@ -10,6 +10,7 @@
 //   * `split` warps of a CTA share the contraction of their channels, 128 bytes in turn, so that small layers fill the SMs.  Up to four steps
 //     of weights are asked for at once: 8 KB a warp.
 //   * The shares meet in shared memory; the sums are exact in any order.
+#include <cstdio>
 #include <type_traits>
 
 #include "q8_common.cuh"
@@ -178,6 +179,7 @@ cudaError_t launch_gemm_q8_tokens(int dtype, const GemmQ8TokensParams& t, GemmQ8
   const long long groups = static_cast<long long>(p.batch) * ((p.N + kChannels - 1) / kChannels);
   p.split = 1;
   while (p.split < kWarps && groups * p.split * 2 <= 16ll * dev.sm_count && p.K > p.split * 128) p.split *= 2;
+  if (verbose_enabled()) std::fprintf(stderr, "comfuse: gemm_q8 dtype=%d: a handful of rows, rows=%d shares=%d\n", dtype, p.M <= 8 ? 8 : 16, p.split);
   switch (dtype) {
     case COMFUSE_DTYPE_BF16: return launch_rows<COMFUSE_DTYPE_BF16>(t, p, stream);
     case COMFUSE_DTYPE_F16: return launch_rows<COMFUSE_DTYPE_F16>(t, p, stream);

@@ -56,6 +56,7 @@ bool encode_tmap_128b_3d(CUtensorMap* out, CUtensorMapDataType type, int bytes, 
 comfuse_status_t check_device(const DeviceInfo** out);
 unsigned long long timeout_ns();  // limit of every bounded wait (COMFUSE_TIMEOUT_MS)
 bool few_rows_enabled();          // COMFUSE_FEW_ROWS
+bool verbose_enabled();           // COMFUSE_VERBOSE
 
 // Tensor maps of one GEMM -> subgraph call: operands A [batch, M, K] and B [batch, K, N], residual R and output Y
 // [batch, M, N]; all bf16, 128-byte swizzle, boxes of 64 elements by 128 rows (A, R), 64 rows (B) or 32 rows (Y: one

@@ -11,6 +11,7 @@
 //   * A thread owns chunks of 8 elements: 16-byte accesses of 16-bit types, 8 bytes of codes; chunk j of a row belongs to thread j mod T.
 //   * The maximum is taken over the bit patterns of |h gamma| as unsigned integers, where infinities and NaNs lie above every number: one
 //     warp reduction instruction finds the maximum and whether the row is finite.
+#include <cstdio>
 #include <type_traits>
 
 #include "q8_common.cuh"
@@ -267,6 +268,8 @@ cudaError_t launch_instance(const QuantizeRowsParams& p, unsigned grid, unsigned
   }
   cfg.attrs = attr;
   cfg.numAttrs = n;
+  if (verbose_enabled())
+    std::fprintf(stderr, "comfuse: quantize_rows dtype=%d norm=%d: %s, chunks=%d ctas=%d threads=%u\n", DT, NORM, WARP ? "a warp a row" : "CTAs a row", CH, p.split, threads);
   count_launch();
   return cudaLaunchKernelEx(&cfg, quantize_rows_kernel<DT, NORM, CH, WARP>, p);
 }
