@@ -277,7 +277,7 @@ gemm_q8_pair_kernel(const __grid_constant__ GemmQ8PairMaps maps, const GemmQ8Par
             void* out = static_cast<char*>(p.Y) + (tb * p.batch_stride_y + static_cast<long long>(row0 + lane) * p.ldy) * Elem<DT>::kBytes;
 #pragma unroll
             for (int i = 0; i < S; ++i)
-              if (col + i >= whole && col + i < p.N) Elem<DT>::put(out, col + i, z[i]);
+              if (col + i >= whole && col + i < p.N && COMFUSE_IN_BOUNDS(row0 + lane < p.M && tb < p.batch, p.status)) Elem<DT>::put(out, col + i, z[i]);
           }
           __syncwarp();
           uint32_t ow[4 * kChunks];

@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(FewCfg<MT>::kThreads, 1) gemm_q8_few_kernel(co
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (col + i < p.N) Elem<DT>::put(to, i, z[i]);
+            if (col + i < p.N && COMFUSE_IN_BOUNDS(m0 + r < p.M && b < p.batch, p.status)) Elem<DT>::put(to, i, z[i]);
         }
       }
       row += RB * Cfg::kEpiWarps;

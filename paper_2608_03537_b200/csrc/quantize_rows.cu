@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kMaxThreads) quantize_rows_kernel(const Quanti
 #pragma unroll
           for (int i = 0; i < 8; ++i) y[j][i] += Elem<DT>::of(r[j], i);
         }
-        if (p.h) store_chunk<DT>(hrow + c * kChunk, y[j]);
+        if (p.h && COMFUSE_IN_BOUNDS(row < p.rows && 8 * c + 7 < p.N, p.status)) store_chunk<DT>(hrow + c * kChunk, y[j]);
         add_squares(y[j], sum, high);
         if (p.gamma) {
 #pragma unroll
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kMaxThreads) quantize_rows_kernel(const Quanti
     yt[0] = Elem<DT>::get(xrow, behind);
     if constexpr (NORM) {
       if (p.residual) yt[0] += Elem<DT>::get(rrow, behind);
-      if (p.h) Elem<DT>::put(hrow, behind, yt[0]);
+      if (p.h && COMFUSE_IN_BOUNDS(row < p.rows && behind < p.N, p.status)) Elem<DT>::put(hrow, behind, yt[0]);
       add_squares(yt, sum, high);
       if (p.gamma) yt[0] *= Elem<DT>::get(p.gamma, behind);
     }
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kMaxThreads) quantize_rows_kernel(const Quanti
     }
   }
   const RowScale s = row_scale<NORM>(sum, top, p);
-  if (tid == 0 && rank == 0) p.scale[row] = s.scale;
+  if (tid == 0 && rank == 0 && COMFUSE_IN_BOUNDS(row < p.rows, p.status)) p.scale[row] = s.scale;
   int8_t* qrow = p.q + row * p.ldq;
   uint16_t* vrow = p.values + row * p.ldv;
 #pragma unroll
@@ -238,13 +238,17 @@ __global__ void __launch_bounds__(kMaxThreads) quantize_rows_kernel(const Quanti
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       w[k] = __byte_perm(__byte_perm(b[4 * k], b[4 * k + 1], 0x0040), __byte_perm(b[4 * k + 2], b[4 * k + 3], 0x0040), 0x5410);
-    if (COMFUSE_IN_BOUNDS(row < p.rows && 8 * c + 7 < p.N, p.status)) st_8(qrow + 8 * c, w);
-    if (p.values) store_chunk<COMFUSE_DTYPE_BF16>(reinterpret_cast<char*>(vrow + 8 * c), yj);
+    if (COMFUSE_IN_BOUNDS(row < p.rows && 8 * c + 7 < p.N, p.status)) {
+      st_8(qrow + 8 * c, w);
+      if (p.values) store_chunk<COMFUSE_DTYPE_BF16>(reinterpret_cast<char*>(vrow + 8 * c), yj);
+    }
   }
   if (tail) {
     const float v = code_of<NORM>(yt[0], s);
-    qrow[behind] = static_cast<int8_t>(__float_as_uint(v) & 0xFFu);
-    if (p.values) Elem<COMFUSE_DTYPE_BF16>::put(vrow, behind, (v - kRound) * s.scale);
+    if (COMFUSE_IN_BOUNDS(row < p.rows && behind < p.N, p.status)) {
+      qrow[behind] = static_cast<int8_t>(__float_as_uint(v) & 0xFFu);
+      if (p.values) Elem<COMFUSE_DTYPE_BF16>::put(vrow, behind, (v - kRound) * s.scale);
+    }
   }
 }
 
