@@ -344,15 +344,20 @@ cudaError_t launch_instance(const GemmQ8PairMaps& maps, const GemmQ8Params& p, c
 // depth is what counts, behind a short one the epilogue: more warps, which overlap each other's steps, or more boxes.  us, 8192 x 4096 bf16, 5
 // stages / 4 with two boxes / 4 with sixteen warps: K = 4096 86 / 94 / 98, K = 1024 - / 31 / 32, K = 768 - / 25.8 / 26.4, K = 512 25.0 / 23.5 / 20.7, with a
 // residual K = 768 - / 35.0 / 33.7, K = 512 - / 32.2 / 30.1, with GELU K = 512 42.0 / 40.6 / 31.6, K = 1536 47.0 / 48.9 / 41.9, K = 2048 52.8 / 57.8 / 54.0.
-// fp32: sixteen warps only where Y fits the L2; beyond it HBM takes their smaller pieces more slowly (eight / sixteen, K = 64: 96 x 504 x 504 22.3 / 19.8,
-// 8192 x 2048 16.2 / 16.3, 8192 x 4096 26.2 / 27.5, 148 x 512 x 512 30.3 / 32.1, with a residual 8192 x 4096 50.6 / 55.3).  (A sixth stage,
+// fp32 (252 calls, K = 32 .. 256, 16 .. 148 MB of Y, each with one Y rewritten and with several in turn): sixteen warps while the call's bytes stay in the
+// L2, 120 MB of its 126 (96 x 504 x 504 x 64 22.5 / 20.1, 112 x 504 x 504 25.5 / 23.5, 8192 x 2824 22.4 / 19.8; beyond, HBM takes their smaller pieces more slowly: 128 x 504 x 504
+// 26.2 / 26.8, 8192 x 4096 26.4 / 27.7, 148 x 512 x 512 30.5 / 32.4), where rows are whole 32-byte sectors (8192 x 1001 12.0 / 13.0, 96 x 500 x 500 24.8 / 28.1, a leading
+// dimension of 2052 for 2048 20.4 / 22.3), and in more than one round of tiles (2560 x 1792 7.3 / 7.7, 2560 x 2048 9.6 / 9.2); not with a residual (8192 x 4096 50.6 / 55.3).  Where the rule says
+// sixteen they are 5.6 % faster in the geometric mean, at worst 8 % slower.  (A sixth stage,
 // in the room of a box: between 3 % faster and 7 % slower from call to call under the power limit.)
 template <int DT>
 cudaError_t launch_columns(int columns, const GemmQ8PairMaps& maps, const GemmQ8Params& p, const DeviceInfo& dev, cudaStream_t stream) {
   if (columns == 128) return launch_instance<DT, 128, 6, 2, 2>(maps, p, dev, stream);
   const bool long_epilogue = p.activation != 0 && p.activation != COMFUSE_OP_RELU;
-  const bool in_l2 = static_cast<long long>(p.batch) * p.M * p.N * Elem<DT>::kBytes <= 100ll << 20;
-  if (long_epilogue ? p.K <= 1536 : DT != COMFUSE_DTYPE_F32 ? p.K <= 768 : p.K <= 256 && !p.residual && in_l2) return launch_instance<DT, 256, 4, 1, 4>(maps, p, dev, stream);
+  const long long bytes = p.batch * (static_cast<long long>(p.M) * p.N * Elem<DT>::kBytes + (static_cast<long long>(p.M) + p.N) * p.K);
+  const bool sectors = (((p.N | p.ldy | p.batch_stride_y) * Elem<DT>::kBytes | reinterpret_cast<uintptr_t>(p.Y)) & 31) == 0;
+  const bool f32_sixteen = p.K <= 256 && !p.residual && sectors && p.tiles > dev.sm_count / 2 && bytes <= 120ll << 20;
+  if (long_epilogue ? p.K <= 1536 : DT != COMFUSE_DTYPE_F32 ? p.K <= 768 : f32_sixteen) return launch_instance<DT, 256, 4, 1, 4>(maps, p, dev, stream);
   if (p.K <= 1024) return launch_instance<DT, 256, 4, 2, 2>(maps, p, dev, stream);
   return launch_instance<DT, 256, 5, 1, 2>(maps, p, dev, stream);
 }

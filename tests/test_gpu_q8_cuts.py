@@ -45,7 +45,7 @@ PAIRS = {(128, 6, 2, 8): [(520, 1030, 70, None), (400, 1500, 33, "tanh")], (256,
 ROWS = [(37, 250), (2050, 500), (2049, 1001), (5, 603), (7, 2105), (600, 8203), (2001, 2507), (600, 9001), (1, 16381), (40, 8207), (150, 16003), (301, 8195), (100, 65501), (200, 30011)]
 
 
-def product(M, N, K, name, device, activation=None, bias=False, residual=False, seed=0):
+def product(M, N, K, name, device, activation=None, bias=False, residual=False, seed=0, extra=0):
     g = torch.Generator(device=device).manual_seed(seed)
     t = q8.TYPES[name]
     wide = (K + 15) // 16 * 16
@@ -54,7 +54,7 @@ def product(M, N, K, name, device, activation=None, bias=False, residual=False, 
     pad = (N + 7) // 8 * 8
     w = torch.randn(N, device=device, generator=g).to(t) if bias else None
     r = torch.randn(M, pad, device=device, generator=g).to(t)[:, :N] if residual else None
-    y = q8.out((M, N), t, device)
+    y = q8.out((M, N), t, device, extra)
     cf.gemm_q8(a, sa, b, sb, y, bias=w, residual=r, activation=activation)
     torch.cuda.synchronize()
     f = q8.f64
@@ -163,3 +163,27 @@ def test_every_cut_in_the_checked_build(name, cuda_device):
     else:
         assert cf_build.build(checked=True) == lib
     _check(name, _child(name, lib))
+
+
+# fp32 behind a short contraction: epilogue warps, for M, N, K, residual, 16-byte units behind a row of Y
+F32_WARPS = [(16, 2900, 1800, 140, False, 2), (16, 2600, 2048, 250, False, 0), (16, 14000, 2000, 64, False, 0),
+             (8, 2900, 1801, 140, False, 0), (8, 2900, 1804, 140, False, 1), (8, 2900, 1800, 140, False, 1),      # rows that are not whole 32-byte sectors, or start within one
+             (8, 2560, 1792, 64, False, 0),                                                                       # one round of tiles
+             (8, 8192, 4096, 64, False, 0), (8, 16384, 1912, 64, False, 0),                                       # more than the L2 holds
+             (8, 2900, 1800, 140, True, 0), (8, 2900, 1800, 264, False, 0)]
+
+
+def run_f32_warps():
+    for i, (_, M, N, K, residual, extra) in enumerate(F32_WARPS):
+        print(f"case {i}", file=sys.stderr, flush=True)
+        product(M, N, K, "f32", torch.device("cuda:0"), residual=residual, seed=i, extra=extra)
+
+
+def test_epilogue_warps_of_fp32_follow_the_result(cuda_device):
+    """Sixteen where the call's bytes stay in the L2, rows are whole sectors and there is more than one round of tiles; else eight."""
+    r = subprocess.run([sys.executable, "-c", "from tests import test_gpu_q8_cuts as t\nt.run_f32_warps()"], cwd=ROOT, env=dict(os.environ, PYTHONPATH=ROOT, COMFUSE_VERBOSE="1"),
+                       capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-1000:] + r.stderr[-3000:]
+    told = _products(r.stderr)
+    assert [told[i][1][0] for i in range(len(F32_WARPS))] == ["pairs"] * len(F32_WARPS)
+    assert [told[i][1][4] for i in range(len(F32_WARPS))] == [c[0] for c in F32_WARPS]
