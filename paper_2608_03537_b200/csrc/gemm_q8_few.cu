@@ -310,7 +310,9 @@ cudaError_t launch_rows(int rows, const CUtensorMap& tmW, const CUtensorMap& tmX
 
 GemmQ8FewPlan gemm_q8_few_plan(int batch, int M, int N, int K, bool long_epilogue, const DeviceInfo& dev) {
   // Both this form's cut and the choice between it and the tile kernel by estimates of their times in us, fitted to 4238 cuts of 368 calls (20 .. 400
-  // rows, 128 .. 16384 channels, 128 .. 16384 codes a row; the cut that they choose is 1 % above the fastest on average, 11 % at worst).
+  // rows, 128 .. 16384 channels, 128 .. 16384 codes a row; the cut that they choose is 1 % above the fastest cut of this form on average, 11 % at worst).
+  // Between the forms, against fixed groups of rows: 956 calls 13 % faster in the geometric mean, some slower (47 x 3593 x 3268 fp32 8.0 -> 9.1 us, 938 x 530 x
+  // 4655 14.1 -> 15.5, 82 x 13169 x 112 7.7 -> 8.3).
   //   * A CTA does one tile and the next one's set-up starts behind it, so a round of tiles costs its whole latency: set-up, the rows' epilogue, the K
   //     blocks, and, where shares meet, the cluster's barriers.  Groups of 16 rows read the weights again for each group, out of the L2; small weights
   //     are cheaper to read often than their epilogue is to do in one CTA: us with 16 / 64 rows a CTA, 64 x 1024 x 128 3.0 / 4.7, 64 x 1024 x 1024 4.0 / 5.0.

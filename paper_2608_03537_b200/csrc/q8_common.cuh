@@ -58,7 +58,8 @@ __device__ __forceinline__ void ld_8(const void* p, uint32_t* w) {
 __device__ __forceinline__ void st_8(void* p, const uint32_t* w) {
   asm volatile("st.global.v2.b32 [%0], {%1, %2};" ::"l"(p), "r"(w[0]), "r"(w[1]) : "memory");
 }
-// 1 / (1 + e^-x) from ex2 and rcp: relative error 2^-22 + |x| 2^-24 (the exponent's rounding); 0 where e^-x leaves fp32.
+// 1 / (1 + e^-x) from ex2 and rcp.  Relative error: ex2 2^-22, the addition 2^-24, rcp 2^-23, and |x| 2^-23 of the exponent (its product's rounding
+// and that of log2 e): below 2^-21 + |x| 2^-23.  A result below 2^-126 (x < -87.3) is 0: rcp flushes it.
 __device__ __forceinline__ float sigmoid_f32(float x) { return rcp_approx(1.f + ex2_approx(x * -1.4426950408889634f)); }
 
 // The activations of the library's reduction-free kinds on N values.  GELU's 0.5 (1 + tanh u) is the sigmoid of 2u: two special-function

@@ -108,7 +108,9 @@ __device__ __forceinline__ void merge(const float2* part, int n, float& sum, uin
 constexpr float kRound = 12582912.f;  // 1.5 * 2^23: behind its addition the low byte is the rounded number in two's complement
 // y's code, as a whole number plus kRound.  Without the norm the quotient is correctly rounded nearly always: rows of 16-bit values meet the exact
 // middle of two codes often (their values are few), and 127 / max alone, rounded, would send all of those in a row to one side instead of to
-// the even code.  Behind a norm such a middle is an accident and one fused operation rounds y * inv to the whole number (60000 x 256: 26 -> 24 us).
+// the even code.  Behind a norm one fused operation rounds y * inv to the whole number (60000 x 256: 26 -> 24 us): a middle may go to either code there, as the
+// interface allows.  It is met where h gamma has few values, most often without residual and gains; with both, 92 of 8192 x 4096 bf16 codes are not
+// the one that 64 bits give (with a division in fp32 61; without the norm, here, none of 8192 x 16384).
 template <bool NORM>
 __device__ __forceinline__ float code_of(float y, const RowScale& s) {
   const float v = s.finite ? y * s.lift : 0.f;
