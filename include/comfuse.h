@@ -484,6 +484,103 @@ typedef struct {
 comfuse_status_t comfuse_gemm_q8(const comfuse_gemm_q8_desc_t* desc, const int8_t* A, const float* scale_a, const int8_t* B, const float* scale_b,
                                  const void* bias, const void* residual, void* Y, void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Key-value cache (decoding; the paper has no counterpart).
+ *
+ *   comfuse_rotary           turns rows by their positions (with several axes for images and video), or back: its own gradient;
+ *   comfuse_cache_write      puts keys (turned) and values into a paged cache, in 16 bits or in 8 with a scale for each row, and turns queries;
+ *   comfuse_cache_read       reads rows of the cache back as 16-bit values;
+ *   comfuse_paged_attention  is the attention of a few new tokens of each sequence over the cache, split over the cache's length and joined.
+ * Conventions as above, except: strides are in ELEMENTS of their tensor and multiples of 16 BYTES (scales: any); the last dimension, D, is dense
+ * and a multiple of 8.  Cached rows do not overlap. */
+
+/* A row of D holds `pairs` pairs (a, b) and D - 2 * pairs elements that stay as they are.  Pair i is (x[i], x[i + pairs]), or with
+ * `adjacent` (x[2i], x[2i + 1]).  Its angle is positions[axis of the pair][token] * freqs[i]; the first sections[0] pairs belong to axis 0, and so on.
+ * (a, b) -> (a cos - b sin, a sin + b cos); `inverse` turns by the negative angle, which is the gradient: dx = rotary(dy, inverse).
+ * Angles are computed in 64 bits and reduced to one turn before they become fp32, so far positions are as exact as near ones. */
+typedef struct {
+  const int32_t* positions;   /* [axes, tokens]; 4-byte aligned */
+  const double* freqs;        /* [pairs], radians for one position; 8-byte aligned */
+  int64_t axis_stride;        /* elements; matters for axes > 1 */
+  int32_t pairs;              /* 1 <= pairs <= D / 2 */
+  int32_t axes;               /* 1 .. 4 */
+  int32_t sections[4];        /* pairs of each axis, >= 0, `pairs` in all (entries behind the last axis: 0) */
+  int32_t adjacent, inverse;  /* 0 or 1 */
+} comfuse_rotary_t;
+
+typedef struct {
+  int32_t tokens, heads, D;   /* >= 1; D <= 512, a multiple of 8 */
+  int32_t dtype;              /* comfuse_dtype_t of x and out */
+  int64_t x_strides[2], out_strides[2]; /* of a token, of a head */
+} comfuse_rotary_desc_t;
+
+/* out[t, h] = rotary(x[t, h]), computed in fp32 and rounded once.  out may be x itself (same strides); otherwise they do not overlap. */
+comfuse_status_t comfuse_rotary(const comfuse_rotary_desc_t* desc, const comfuse_rotary_t* rotary, const void* x, void* out, void* cuda_stream);
+
+/* A paged cache [pages, heads, page_size, D] with any strides: slot n is row n % page_size of page n / page_size.  8 bits: int8 codes and one
+ * fp32 scale for each row, [pages, heads, page_size] with strides of their own. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;             /* quantized: required; otherwise NULL */
+  int32_t pages, heads, page_size, D;   /* >= 1; page_size <= 65536; D <= 256, a multiple of 8 (quantized: of 16) */
+  int32_t dtype;                        /* COMFUSE_DTYPE_BF16 or _F16: what rows are written from and read back to, and, unless quantized, held in */
+  int32_t quantized;                    /* 0 or 1 */
+  int64_t k_strides[3], v_strides[3];   /* of a page, of a head, of a row */
+  int64_t k_scale_strides[3], v_scale_strides[3];
+} comfuse_kv_cache_t;
+
+typedef struct {
+  int32_t tokens;                       /* >= 1 */
+  int32_t q_heads;                      /* 0: no queries */
+  int64_t k_strides[2], v_strides[2], q_strides[2], q_out_strides[2]; /* of a token, of a head */
+} comfuse_cache_write_desc_t;
+
+/* For each token t with 0 <= slots[t] < pages * page_size (others are padding: nothing of them is stored in the cache):
+ *   cache row slots[t] of head h = rotary(k[t, h]) and v[t, h], for 16 bits rounded once; for 8 bits scale = max|y| / 127 and codes y / scale, rounded to
+ *   the nearest whole number, from the fp32 values; a row with an infinity or a NaN has scale NaN and codes 0, a row of zeros scale 0.
+ * q_out[t, h] = rotary(q[t, h]) for every token.  rotary NULL: keys stay as they are, and there are no queries.  `inverse` must be 0.
+ * No slot may stand in a call twice (which of the tokens it then holds, or parts of which, is not defined).  q_out may be q itself (same strides). */
+comfuse_status_t comfuse_cache_write(const comfuse_cache_write_desc_t* desc, const comfuse_kv_cache_t* cache, const comfuse_rotary_t* rotary, const void* k,
+                                     const void* v, const void* q, void* q_out, const int64_t* slots, void* cuda_stream);
+
+typedef struct {
+  int32_t tokens;                       /* >= 1 */
+  int32_t reserved;                     /* must be 0 */
+  int64_t k_strides[2], v_strides[2];   /* of a token, of a head */
+} comfuse_cache_read_desc_t;
+
+/* k[t, h] and v[t, h] = rows slots[t] of the cache (8 bits: code * scale rounded once).  Rows of tokens whose slot lies outside the cache stay as
+ * they were.  A slot may stand in a call any number of times. */
+comfuse_status_t comfuse_cache_read(const comfuse_cache_read_desc_t* desc, const comfuse_kv_cache_t* cache, const int64_t* slots, void* k, void* v,
+                                    void* cuda_stream);
+
+typedef struct {
+  int32_t batch, tokens;                /* sequences; new tokens of each, 1 .. 64 */
+  int32_t q_heads;                      /* a multiple of the cache's heads, at most 65536: query head i reads key head i / (q_heads / heads) */
+  int32_t table_width;                  /* entries of a row of the page table */
+  int64_t q_strides[3], out_strides[3]; /* of a sequence, of a token, of a head */
+  int64_t table_stride;                 /* of a sequence, elements */
+  int32_t max_length;                   /* no sequence is longer; 0: table_width * page_size */
+  int32_t window;                       /* > 0: a token sees that many positions, itself among them; 0: all */
+  float alpha;                          /* scales the scores; finite */
+  float softcap;                        /* > 0: scores become softcap * tanh(scores / softcap); 0: no cap */
+} comfuse_paged_attention_desc_t;
+
+/* Sequence b has lengths[b] cached tokens (clamped to 0 .. max_length), the new ones the last of them; position n is row n % page_size of page
+ * table[b, n / page_size].  For the new token i, at position m = lengths[b] - tokens + i, and query head h:
+ *   score[n] = cap(alpha * q[b, i, h] . k[n]) + slopes[h] * (n - m)   for max(0, m - window + 1) <= n <= m, and nothing for other positions
+ *   out[b, i, h] = sum_n softmax(score)[n] v[n],   lse[b, i, h] = log sum_n exp(score[n])
+ * Positions on pages outside the cache (a table entry < 0 or >= pages) count as not there.  Where nothing is left out is 0 and lse -inf.  What other
+ * positions hold, infinities and NaN too, changes nothing.  slopes (fp32 [q_heads]) and lse (fp32 [batch, tokens, q_heads], dense) may be NULL.
+ * q and out are 16-bit, of the cache's dtype.  Scores, statistics and sums are fp32; the weights enter the second product in 16 bits twice (the rounded
+ * weight and what the rounding left), or over an 8-bit cache and bf16 outputs once, as fp16.
+ * Workspace: comfuse_paged_attention_workspace_size() bytes (a function of the sizes alone, never above 32 MiB), 16-byte aligned, of any content;
+ * calls that may overlap need one each.  Results do not depend on the order in which parts finish. */
+comfuse_status_t comfuse_paged_attention_workspace_size(const comfuse_paged_attention_desc_t* desc, const comfuse_kv_cache_t* cache, size_t* bytes);
+comfuse_status_t comfuse_paged_attention(const comfuse_paged_attention_desc_t* desc, const comfuse_kv_cache_t* cache, const void* q, const int32_t* table,
+                                         const int32_t* lengths, const float* slopes, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                         void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

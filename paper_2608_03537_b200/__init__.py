@@ -13,6 +13,11 @@ Functions mirror the C entry points:
     b2b_gemm(...)           -> comfuse_b2b_gemm           (GEMM -> F -> GEMM -> post-norm tail, Sec. 4)
     quantize_rows(...), rmsnorm_quantize_rows(...) -> comfuse_quantize_rows (rows to int8 with a scale each, alone or behind a norm)
     gemm_q8(...)            -> comfuse_gemm_q8            (int8 product with a scale for each token and channel)
+    rotary(...)             -> comfuse_rotary             (rows turned by their positions, or back)
+    cache_write(...)        -> comfuse_cache_write        (keys and values into a paged cache, in 16 or 8 bits)
+    cache_read(...)         -> comfuse_cache_read
+    paged_attention(...)    -> comfuse_paged_attention    (a few new tokens of each sequence over the cache)
+    paged_attention_workspace_size(...) -> comfuse_paged_attention_workspace_size
     workspace_size(...)     -> comfuse_workspace_size
     b2b_workspace_size(...) -> comfuse_b2b_workspace_size
     last_device_status()    -> comfuse_last_device_status
@@ -56,6 +61,11 @@ EXPORTED_SYMBOLS = (
     "comfuse_program_compiler_status",
     "comfuse_quantize_rows",
     "comfuse_gemm_q8",
+    "comfuse_rotary",
+    "comfuse_cache_write",
+    "comfuse_cache_read",
+    "comfuse_paged_attention_workspace_size",
+    "comfuse_paged_attention",
     "comfuse_selftest_bounds_predicate",
     "comfuse_last_device_status",
     "comfuse_launch_count",
@@ -102,6 +112,34 @@ class GemmQ8Desc(Structure):
                 ("lda", c_int64), ("ldb", c_int64), ("ldr", c_int64), ("ldy", c_int64),
                 ("batch_stride_a", c_int64), ("batch_stride_b", c_int64), ("batch_stride_r", c_int64), ("batch_stride_y", c_int64),
                 ("dtype", c_int32), ("activation", c_int32), ("flags", ctypes.c_uint32), ("reserved", c_int32)]
+
+
+# Key-value cache
+class Rotary(Structure):
+    _fields_ = [("positions", c_void_p), ("freqs", c_void_p), ("axis_stride", c_int64), ("pairs", c_int32), ("axes", c_int32), ("sections", c_int32 * 4),
+                ("adjacent", c_int32), ("inverse", c_int32)]
+
+
+class RotaryDesc(Structure):
+    _fields_ = [("tokens", c_int32), ("heads", c_int32), ("D", c_int32), ("dtype", c_int32), ("x_strides", c_int64 * 2), ("out_strides", c_int64 * 2)]
+
+
+class KvCache(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p), ("pages", c_int32), ("heads", c_int32), ("page_size", c_int32), ("D", c_int32),
+                ("dtype", c_int32), ("quantized", c_int32), ("k_strides", c_int64 * 3), ("v_strides", c_int64 * 3), ("k_scale_strides", c_int64 * 3), ("v_scale_strides", c_int64 * 3)]
+
+
+class CacheWriteDesc(Structure):
+    _fields_ = [("tokens", c_int32), ("q_heads", c_int32), ("k_strides", c_int64 * 2), ("v_strides", c_int64 * 2), ("q_strides", c_int64 * 2), ("q_out_strides", c_int64 * 2)]
+
+
+class CacheReadDesc(Structure):
+    _fields_ = [("tokens", c_int32), ("reserved", c_int32), ("k_strides", c_int64 * 2), ("v_strides", c_int64 * 2)]
+
+
+class PagedAttentionDesc(Structure):
+    _fields_ = [("batch", c_int32), ("tokens", c_int32), ("q_heads", c_int32), ("table_width", c_int32), ("q_strides", c_int64 * 3), ("out_strides", c_int64 * 3),
+                ("table_stride", c_int64), ("max_length", c_int32), ("window", c_int32), ("alpha", c_float), ("softcap", c_float)]
 
 
 # Epilogue programs as data: the node vocabulary (comfuse_op_t), by name
@@ -195,6 +233,16 @@ def lib() -> ctypes.CDLL:
         L.comfuse_quantize_rows.restype = c_int32
         L.comfuse_gemm_q8.argtypes = [POINTER(GemmQ8Desc)] + [c_void_p] * 8
         L.comfuse_gemm_q8.restype = c_int32
+        L.comfuse_rotary.argtypes = [POINTER(RotaryDesc), POINTER(Rotary)] + [c_void_p] * 3
+        L.comfuse_rotary.restype = c_int32
+        L.comfuse_cache_write.argtypes = [POINTER(CacheWriteDesc), POINTER(KvCache), POINTER(Rotary)] + [c_void_p] * 6
+        L.comfuse_cache_write.restype = c_int32
+        L.comfuse_cache_read.argtypes = [POINTER(CacheReadDesc), POINTER(KvCache)] + [c_void_p] * 4
+        L.comfuse_cache_read.restype = c_int32
+        L.comfuse_paged_attention_workspace_size.argtypes = [POINTER(PagedAttentionDesc), POINTER(KvCache), POINTER(c_size_t)]
+        L.comfuse_paged_attention_workspace_size.restype = c_int32
+        L.comfuse_paged_attention.argtypes = [POINTER(PagedAttentionDesc), POINTER(KvCache)] + [c_void_p] * 7 + [c_size_t, c_void_p]
+        L.comfuse_paged_attention.restype = c_int32
         L.comfuse_last_device_status.argtypes = [c_void_p]
         L.comfuse_last_device_status.restype = c_int32
         L.comfuse_selftest_bounded_wait.argtypes = [ctypes.c_uint32, c_void_p, POINTER(ctypes.c_uint32)]
@@ -572,6 +620,87 @@ def gemm_q8(A, scale_a, B, scale_b, Y, *, bias=None, residual=None, activation=N
     if st != OK:
         raise ComfuseError(st, "comfuse_gemm_q8")
     return Y
+
+
+_kv = None   # the marshalling extension, once the key-value cache's entry points are in it
+
+
+def _bound_kv(device=True):
+    global _kv
+    if _kv is None:
+        import torch
+        b = _bound_q8(device)
+        L = lib()
+        b.bind_kv(*(ctypes.cast(f, c_void_p).value for f in (L.comfuse_rotary, L.comfuse_cache_write, L.comfuse_cache_read, L.comfuse_paged_attention,
+                                                              L.comfuse_paged_attention_workspace_size)), torch.int32, torch.int64, torch.float64)
+        if not device:   # (the marshalling alone)
+            return b
+        _kv = b
+    return _kv
+
+
+def rotary(x, positions, freqs, out, *, sections=None, adjacent=False, inverse=False, stream=None):
+    """Enqueue out[t, h] = x[t, h] with each pair of elements turned by its angle, positions[t] * freqs[pair].  ``x``, ``out`` [tokens, heads, D] bf16, fp16 or
+    fp32, one type (``out`` may be ``x``); ``freqs`` [pairs] fp64, radians for one position (for example base ** (-arange(pairs) / pairs)); elements
+    behind the first 2 * pairs stay as they are.  ``positions`` int32 [tokens], or [axes, tokens] with ``sections``, the number of pairs that each axis
+    (time, height, width) turns, in order.  Pairs are (x[i], x[i + pairs]), or with ``adjacent`` (x[2i], x[2i + 1]).  ``inverse`` turns back: with it the call is
+    the gradient, dx = rotary(dy, ..., inverse=True)."""
+    st = (_kv or _bound_kv()).rotary(x, positions, freqs, sections, adjacent, inverse, out, _device_of(stream), _current_stream if stream is None else stream)
+    if st != OK:
+        raise ComfuseError(st, "comfuse_rotary")
+    return out
+
+
+def cache_write(k, v, k_cache, v_cache, slots, *, k_scale=None, v_scale=None, q=None, q_out=None, positions=None, freqs=None, sections=None, adjacent=False, stream=None):
+    """Enqueue the new tokens' keys and values into a paged cache.  ``k``, ``v`` [tokens, heads, D] bf16 or fp16; caches [pages, heads, page_size, D] of the same type, or
+    int8 with fp32 ``k_scale``, ``v_scale`` [pages, heads, page_size]: a row's largest magnitude / 127.  ``slots`` int64 [tokens]: page * page_size + row of each
+    token, each at most once; a slot outside the cache (-1) is padding.  With ``positions`` and ``freqs`` (see rotary) keys are turned before they
+    are stored, and so are queries ``q`` [tokens, q_heads, D] into ``q_out`` (which may be ``q``), for padding too.  Any strides with dense rows on 16-byte
+    boundaries: views of one projection's output, a cache [pages, page_size, heads, D] transposed."""
+    st = (_kv or _bound_kv()).cache_write(k, v, k_cache, v_cache, k_scale, v_scale, slots, q, q_out, positions, freqs, sections, adjacent, False, _device_of(stream),
+                                          _current_stream if stream is None else stream)
+    if st != OK:
+        raise ComfuseError(st, "comfuse_cache_write")
+
+
+def cache_read(k_cache, v_cache, slots, k, v, *, k_scale=None, v_scale=None, stream=None):
+    """Enqueue k[t], v[t] = the cache's rows slots[t], as bf16 or fp16 values (``k``, ``v`` [tokens, heads, D]; caches, scales and slots as in cache_write).  Rows of tokens whose
+    slot lies outside the cache stay as they were."""
+    st = (_kv or _bound_kv()).cache_read(k_cache, v_cache, k_scale, v_scale, slots, k, v, _device_of(stream), _current_stream if stream is None else stream)
+    if st != OK:
+        raise ComfuseError(st, "comfuse_cache_read")
+    return k, v
+
+
+PAGED_ATTENTION_WORKSPACE_BYTES = 32 << 20   # enough for any call
+
+
+def paged_attention_workspace_size(q, k_cache, v_cache, page_table, *, k_scale=None, v_scale=None, window=0, max_length=None) -> int:
+    """Bytes of workspace that paged_attention needs for these shapes (whatever the lengths; never more than PAGED_ATTENTION_WORKSPACE_BYTES)."""
+    b = _kv or _bound_kv()
+    st, n = b.paged_attention_size(q, k_cache, v_cache, k_scale, v_scale, page_table, 1.0, 0.0, window, max_length, _device_of(None))
+    if st != OK:
+        raise ComfuseError(st, "comfuse_paged_attention_workspace_size")
+    return n
+
+
+def paged_attention(q, k_cache, v_cache, page_table, lengths, out, *, alpha=None, k_scale=None, v_scale=None, softcap=0.0, slopes=None, window=0, max_length=None, lse=None,
+                    workspace=None, stream=None):
+    """Enqueue the attention of each sequence's newest tokens over its cached ones.  ``q``, ``out`` [sequences, q_heads, D] (one new token each) or [sequences, tokens, q_heads, D]
+    (up to 64), bf16 or fp16; caches and scales as in cache_write, their heads a divisor of q_heads; ``page_table`` int32 [sequences, width]: position n of a sequence is row
+    n % page_size of page page_table[b, n // page_size] (an entry that is no page: nothing is there); ``lengths`` int32 [sequences], the new tokens, which are the last of
+    them, among them; a sequence may be empty.  A token sees itself and what is in front of it, with ``window`` > 0 that many positions.
+
+    score = alpha * q.k (``alpha``: D ** -0.5 unless given), with ``softcap`` > 0 softcap * tanh(score / softcap), plus slopes[head] * (n - its own position) where ``slopes``
+    (fp32 [q_heads]) are given.  ``lse`` (fp32, q's shape without D) receives log(sum(exp(score))).  A token that sees nothing has out 0 and lse -inf.
+
+    ``max_length``: no sequence is longer than this (else the table's width decides): fewer CTAs are started for less work.  ``workspace``: a CUDA tensor of
+    paged_attention_workspace_size() bytes or more, of any content; calls that may overlap need one each."""
+    st = (_kv or _bound_kv()).paged_attention(q, k_cache, v_cache, k_scale, v_scale, page_table, q.shape[-1] ** -0.5 if alpha is None else alpha, softcap, window, max_length, lengths, slopes,
+                                              out, lse, workspace, _device_of(stream), _current_stream if stream is None else stream)
+    if st != OK:
+        raise ComfuseError(st, "comfuse_paged_attention")
+    return out
 
 
 def last_device_status(stream=None) -> int:

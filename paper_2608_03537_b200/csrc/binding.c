@@ -365,12 +365,15 @@ static const DlExchange* dl_exchange;
 static PyTypeObject* dl_type;  // the class whose tensors it takes
 
 enum { TYPE_BF16 = COMFUSE_DTYPE_BF16, TYPE_F16 = COMFUSE_DTYPE_F16, TYPE_F32 = COMFUSE_DTYPE_F32, TYPE_I8 = 3, TYPE_OTHER = -1 };
+// types that only the key-value cache's calls take (`type` is TYPE_OTHER)
+enum { WIDE_NONE, WIDE_I32, WIDE_I64, WIDE_F64 };
 typedef struct {
   Geometry g;
-  int type;
+  int type, wide;
   int64_t device;  // -1 = host
   const void* p;
 } Described;
+static PyObject *t_i32, *t_i64, *t_f64;  // (bind_kv)
 
 static int describe(PyObject* t, Described* d) {
   if (dl_exchange && PyObject_TypeCheck(t, dl_type)) {
@@ -390,6 +393,7 @@ static int describe(PyObject* t, Described* d) {
                 : code == 2 && bits == 32 ? TYPE_F32
                 : code == 0 && bits == 8  ? TYPE_I8
                                           : TYPE_OTHER;
+      d->wide = v.dtype.lanes != 1 ? WIDE_NONE : code == 0 && bits == 32 ? WIDE_I32 : code == 0 && bits == 64 ? WIDE_I64 : code == 2 && bits == 64 ? WIDE_F64 : WIDE_NONE;
       d->device = v.device.type == 2 ? v.device.id : v.device.type == 1 ? -1 : -2;
       d->p = (const char*)v.data + v.byte_offset;
       return 1;
@@ -401,6 +405,7 @@ static int describe(PyObject* t, Described* d) {
   if (!type) return 0;
   Py_DECREF(type);  // (a tensor's type outlives it)
   d->type = type == t_bf16 ? TYPE_BF16 : type == t_f16 ? TYPE_F16 : type == t_f32 ? TYPE_F32 : type == t_i8 ? TYPE_I8 : TYPE_OTHER;
+  d->wide = type == t_i32 ? WIDE_I32 : type == t_i64 ? WIDE_I64 : type == t_f64 ? WIDE_F64 : WIDE_NONE;
   return shape_of(t, &d->g) && tuple_i64(PyObject_CallMethodNoArgs(t, s_stride), d->g.stride, &n) && method_i64(t, s_get_device, &d->device) && pointer(t, &d->p);
 }
 static int refuse(const char* what, const char* why) {
@@ -534,6 +539,310 @@ static PyObject* py_gemm_q8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong((long)st);
 }
 
+// ---- the key-value cache
+typedef comfuse_status_t (*rotary_fn)(const comfuse_rotary_desc_t*, const comfuse_rotary_t*, const void*, void*, void*);
+typedef comfuse_status_t (*cache_write_fn)(const comfuse_cache_write_desc_t*, const comfuse_kv_cache_t*, const comfuse_rotary_t*, const void*, const void*, const void*, void*, const int64_t*,
+                                           void*);
+typedef comfuse_status_t (*cache_read_fn)(const comfuse_cache_read_desc_t*, const comfuse_kv_cache_t*, const int64_t*, void*, void*, void*);
+typedef comfuse_status_t (*paged_attention_fn)(const comfuse_paged_attention_desc_t*, const comfuse_kv_cache_t*, const void*, const int32_t*, const int32_t*, const float*, void*, float*, void*,
+                                               size_t, void*);
+typedef comfuse_status_t (*paged_attention_size_fn)(const comfuse_paged_attention_desc_t*, const comfuse_kv_cache_t*, size_t*);
+static rotary_fn f_rotary;
+static cache_write_fn f_cache_write;
+static cache_read_fn f_cache_read;
+static paged_attention_fn f_paged_attention;
+static paged_attention_size_fn f_paged_attention_size;
+
+// A tensor of n dimensions with the given element type (or, type < 0, wide type) and, where they are given (>= 0), sizes; its last dimension is dense.
+static int tensor(PyObject* t, int type, int wide, int64_t device, int n, const int64_t* sizes, const char* what, Described* d) {
+  if (!describe(t, d)) return 0;
+  if (type >= 0 ? d->type != type : d->wide != wide) return refuse(what, "has another element type than the call takes");
+  int same = d->g.n == n;
+  for (int i = 0; same && i < n; ++i) same = sizes[i] < 0 ? d->g.size[i] <= INT32_MAX : d->g.size[i] == sizes[i];
+  if (!same) return refuse(what, "has a shape that does not match the call");
+  if (d->device != device) return refuse(what, "is not on the current device");
+  if (n > 0 && d->g.stride[n - 1] != 1 && d->g.size[n - 1] != 1) return refuse(what, "must be dense in its last dimension");
+  return 1;
+}
+static int dense(const Described* d, const char* what) {
+  int64_t want = 1;
+  for (int i = d->g.n - 1; i >= 0; --i) {
+    if (d->g.size[i] != 1 && d->g.stride[i] != want) return refuse(what, "must be dense");
+    want *= d->g.size[i];
+  }
+  return 1;
+}
+static int type_16(PyObject* t, const char* what, int* type) {
+  Described d;
+  if (!describe(t, &d)) return 0;
+  *type = d.type;
+  return d.type == TYPE_BF16 || d.type == TYPE_F16 ? 1 : refuse(what, "has another element type than the call takes");
+}
+static int no_negative_strides(const Described* d, const char* what) {
+  for (int i = 0; i < d->g.n; ++i)
+    if (d->g.stride[i] < 0) return refuse(what, "has a negative stride");
+  return 1;
+}
+
+// a = (positions, freqs, sections, adjacent, inverse), for `tokens` rows
+static int fill_rotary(PyObject* const* a, int64_t device, int64_t tokens, comfuse_rotary_t* r) {
+  Described pos, freqs;
+  memset(r, 0, sizeof(*r));
+  const int64_t any[1] = {-1};
+  if (!tensor(a[1], -1, WIDE_F64, device, 1, any, "freqs", &freqs) || !describe(a[0], &pos)) return 0;
+  const int axes = pos.g.n == 2 ? (int)(pos.g.size[0] <= 4 ? pos.g.size[0] : 5) : 1;
+  const int64_t one[1] = {tokens}, more[2] = {-1, tokens};
+  if (!tensor(a[0], -1, WIDE_I32, device, pos.g.n == 2 ? 2 : 1, pos.g.n == 2 ? more : one, "positions", &pos) || !no_negative_strides(&pos, "positions")) return 0;
+  if (!require(axes <= 4, "positions has more than 4 axes")) return 0;
+  r->positions = pos.p;
+  r->axis_stride = axes > 1 ? pos.g.stride[0] : 0;
+  r->axes = axes;
+  r->freqs = freqs.p;
+  r->pairs = (int32_t)freqs.g.size[0];
+  if (a[2] == Py_None) {
+    if (!require(axes == 1, "sections has to say how many pairs belong to each axis")) return 0;
+    r->sections[0] = r->pairs;
+  } else {
+    int64_t s[MAX_DIMS], sum = 0;
+    int n = 0;
+    if (!tuple_i64(Py_NewRef(a[2]), s, &n)) return 0;
+    if (!require(n == axes, "sections and positions name different numbers of axes")) return 0;
+    for (int i = 0; i < n; ++i) {
+      if (!require(s[i] >= 0 && s[i] <= r->pairs, "sections does not add up to the pairs")) return 0;
+      r->sections[i] = (int32_t)s[i];
+      sum += s[i];
+    }
+    if (!require(sum == r->pairs, "sections does not add up to the pairs")) return 0;
+  }
+  r->adjacent = PyObject_IsTrue(a[3]);
+  r->inverse = PyObject_IsTrue(a[4]);
+  return r->adjacent >= 0 && r->inverse >= 0;
+}
+
+// a = (k_cache, v_cache, k_scale, v_scale), `type` of the rows around
+static int fill_cache(PyObject* const* a, int type, int64_t device, comfuse_kv_cache_t* c) {
+  Described k, v, ks, vs;
+  const int64_t any[4] = {-1, -1, -1, -1};
+  memset(c, 0, sizeof(*c));
+  if (!describe(a[0], &k)) return 0;
+  const int held = k.type == TYPE_I8 ? TYPE_I8 : type;
+  if (!tensor(a[0], held, 0, device, 4, any, "k_cache", &k) || !tensor(a[1], held, 0, device, 4, k.g.size, "v_cache", &v) || !no_negative_strides(&k, "k_cache") ||
+      !no_negative_strides(&v, "v_cache"))
+    return 0;
+  c->k = (void*)k.p;
+  c->v = (void*)v.p;
+  c->pages = (int32_t)k.g.size[0];
+  c->heads = (int32_t)k.g.size[1];
+  c->page_size = (int32_t)k.g.size[2];
+  c->D = (int32_t)k.g.size[3];
+  c->dtype = type;
+  c->quantized = held == TYPE_I8;
+  memcpy(c->k_strides, k.g.stride, sizeof(c->k_strides));
+  memcpy(c->v_strides, v.g.stride, sizeof(c->v_strides));
+  if (!c->quantized) return require(a[2] == Py_None && a[3] == Py_None, "k_scale and v_scale belong to a cache of int8 codes");
+  if (!require(a[2] != Py_None && a[3] != Py_None, "a cache of int8 codes has k_scale and v_scale")) return 0;
+  if (!describe(a[2], &ks) || !describe(a[3], &vs)) return 0;
+  const Described* const both[2] = {&ks, &vs};
+  for (int i = 0; i < 2; ++i) {  // (any strides, the last one too)
+    const char* what = i ? "v_scale" : "k_scale";
+    const Described* d = both[i];
+    if (d->type != TYPE_F32) return refuse(what, "has another element type than the call takes");
+    if (d->g.n != 3 || memcmp(d->g.size, k.g.size, 3 * sizeof(int64_t)) != 0) return refuse(what, "has a shape that does not match the call");
+    if (d->device != device) return refuse(what, "is not on the current device");
+    if (!no_negative_strides(d, what)) return 0;
+  }
+  c->k_scale = (float*)ks.p;
+  c->v_scale = (float*)vs.p;
+  memcpy(c->k_scale_strides, ks.g.stride, sizeof(c->k_scale_strides));
+  memcpy(c->v_scale_strides, vs.g.stride, sizeof(c->v_scale_strides));
+  return 1;
+}
+// Rows [tokens, heads, D]
+static int rows_of(PyObject* t, int type, int64_t device, int64_t tokens, int64_t heads, int64_t D, const char* what, int64_t* strides, Described* d) {
+  const int64_t sizes[3] = {tokens, heads, D};
+  if (!tensor(t, type, 0, device, 3, sizes, what, d) || !no_negative_strides(d, what)) return 0;
+  strides[0] = d->g.stride[0];
+  strides[1] = d->g.stride[1];
+  return 1;
+}
+static int slots_of(PyObject* t, int64_t device, int64_t tokens, Described* d) {
+  const int64_t sizes[1] = {tokens};
+  return tensor(t, -1, WIDE_I64, device, 1, sizes, "slots", d);
+}
+
+// rotary(x, positions, freqs, sections, adjacent, inverse, out, device, stream) -> status
+static PyObject* py_rotary(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  comfuse_rotary_desc_t d;
+  comfuse_rotary_t r;
+  Described x, out;
+  int64_t device;
+  void* stream;
+  int type;
+  memset(&d, 0, sizeof(d));
+  if (!fixed_args(n, 9, "rotary") || !to_i64(a[7], &device) || !describe(a[0], &x) || !float_type(&x, "x", &type)) return NULL;
+  if (!rows_of(a[0], type, device, -1, -1, -1, "x", d.x_strides, &x) || !fill_rotary(a + 1, device, x.g.size[0], &r) ||
+      !rows_of(a[6], type, device, x.g.size[0], x.g.size[1], x.g.size[2], "out", d.out_strides, &out) || !stream_on(a[8], device, &stream))
+    return NULL;
+  d.tokens = (int32_t)x.g.size[0];
+  d.heads = (int32_t)x.g.size[1];
+  d.D = (int32_t)x.g.size[2];
+  d.dtype = type;
+  comfuse_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_rotary(&d, &r, x.p, (void*)out.p, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong((long)st);
+}
+
+// cache_write(k, v, k_cache, v_cache, k_scale, v_scale, slots, q, q_out, positions, freqs, sections, adjacent, inverse, device, stream) -> status
+static PyObject* py_cache_write(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  comfuse_cache_write_desc_t d;
+  comfuse_kv_cache_t c;
+  comfuse_rotary_t r;
+  Described k, v, q, q_out, slots;
+  int64_t device;
+  void* stream;
+  int type;
+  memset(&d, 0, sizeof(d));
+  q.p = q_out.p = NULL;
+  if (!fixed_args(n, 16, "cache_write") || !to_i64(a[14], &device) || !type_16(a[0], "k", &type) || !fill_cache(a + 2, type, device, &c)) return NULL;
+  if (!rows_of(a[0], type, device, -1, c.heads, c.D, "k", d.k_strides, &k)) return NULL;
+  const int64_t tokens = k.g.size[0];
+  if (!rows_of(a[1], type, device, tokens, c.heads, c.D, "v", d.v_strides, &v) || !slots_of(a[6], device, tokens, &slots)) return NULL;
+  if (!require((a[7] == Py_None) == (a[8] == Py_None), "q and q_out come together") || !require((a[9] == Py_None) == (a[10] == Py_None), "positions and freqs come together") ||
+      !require(a[7] == Py_None || a[9] != Py_None, "q is there to be turned: positions and freqs are missing"))
+    return NULL;
+  const int turned = a[9] != Py_None;
+  if (turned && !fill_rotary(a + 9, device, tokens, &r)) return NULL;
+  if (a[7] != Py_None) {
+    if (!rows_of(a[7], type, device, tokens, -1, c.D, "q", d.q_strides, &q) || !rows_of(a[8], type, device, tokens, q.g.size[1], c.D, "q_out", d.q_out_strides, &q_out)) return NULL;
+    if (!require(q.g.size[1] > 0, "q has no heads")) return NULL;
+    d.q_heads = (int32_t)q.g.size[1];
+  }
+  if (!stream_on(a[15], device, &stream)) return NULL;
+  d.tokens = (int32_t)tokens;
+  comfuse_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_cache_write(&d, &c, turned ? &r : NULL, k.p, v.p, q.p, (void*)q_out.p, (const int64_t*)slots.p, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong((long)st);
+}
+
+// cache_read(k_cache, v_cache, k_scale, v_scale, slots, k, v, device, stream) -> status
+static PyObject* py_cache_read(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  comfuse_cache_read_desc_t d;
+  comfuse_kv_cache_t c;
+  Described k, v, slots;
+  int64_t device;
+  void* stream;
+  int type;
+  memset(&d, 0, sizeof(d));
+  if (!fixed_args(n, 9, "cache_read") || !to_i64(a[7], &device) || !type_16(a[5], "k", &type) || !fill_cache(a, type, device, &c)) return NULL;
+  if (!rows_of(a[5], type, device, -1, c.heads, c.D, "k", d.k_strides, &k)) return NULL;
+  const int64_t tokens = k.g.size[0];
+  if (!rows_of(a[6], type, device, tokens, c.heads, c.D, "v", d.v_strides, &v) || !slots_of(a[4], device, tokens, &slots) || !stream_on(a[8], device, &stream)) return NULL;
+  d.tokens = (int32_t)tokens;
+  comfuse_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_cache_read(&d, &c, (const int64_t*)slots.p, (void*)k.p, (void*)v.p, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong((long)st);
+}
+
+// a = (q, k_cache, v_cache, k_scale, v_scale, table, alpha, softcap, window, max_length): what the workspace's size depends on
+static int fill_attention(PyObject* const* a, int64_t device, comfuse_paged_attention_desc_t* d, comfuse_kv_cache_t* c, Described* q, Described* table, int* type) {
+  int64_t window, max_length;
+  double alpha, softcap;
+  memset(d, 0, sizeof(*d));
+  if (!type_16(a[0], "q", type) || !fill_cache(a + 1, *type, device, c) || !describe(a[0], q)) return 0;
+  const int dims = q->g.n == 3 ? 3 : 4;  // [sequences, heads, D]: one new token each
+  const int64_t three[3] = {-1, -1, c->D}, four[4] = {-1, -1, -1, c->D};
+  if (!tensor(a[0], *type, 0, device, dims, dims == 3 ? three : four, "q", q) || !no_negative_strides(q, "q")) return 0;
+  const int64_t batch = q->g.size[0], width[2] = {batch, -1};
+  if (!tensor(a[5], -1, WIDE_I32, device, 2, width, "page_table", table) || !no_negative_strides(table, "page_table")) return 0;
+  if (a[6] == Py_None) alpha = 0.;
+  else if (!to_f64(a[6], &alpha)) return 0;
+  if (!to_f64(a[7], &softcap) || !to_i64(a[8], &window)) return 0;
+  if (a[9] == Py_None) max_length = 0;
+  else if (!to_i64(a[9], &max_length) || !require(max_length >= 1, "max_length is at least 1")) return 0;
+  if (!require(window >= 0, "window is not negative")) return 0;
+  d->batch = (int32_t)batch;
+  d->tokens = dims == 3 ? 1 : (int32_t)q->g.size[1];
+  d->q_heads = (int32_t)q->g.size[dims - 2];
+  d->table_width = (int32_t)table->g.size[1];
+  d->table_stride = table->g.stride[0];
+  d->q_strides[0] = q->g.stride[0];
+  d->q_strides[1] = dims == 3 ? 0 : q->g.stride[1];
+  d->q_strides[2] = q->g.stride[dims - 2];
+  d->max_length = (int32_t)(max_length > INT32_MAX ? INT32_MAX : max_length);
+  d->window = (int32_t)(window > INT32_MAX ? INT32_MAX : window);
+  d->alpha = (float)alpha;
+  d->softcap = (float)softcap;
+  return 1;
+}
+
+// paged_attention(<the arguments of fill_attention>, lengths, slopes, out, lse, workspace, device, stream) -> status
+static PyObject* py_paged_attention(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  comfuse_paged_attention_desc_t d;
+  comfuse_kv_cache_t c;
+  Described q, table, lengths, slopes, out, lse, ws;
+  int64_t device;
+  void* stream;
+  int type;
+  size_t ws_bytes = 0;
+  slopes.p = lse.p = ws.p = NULL;
+  if (!fixed_args(n, 17, "paged_attention") || !to_i64(a[15], &device) || !fill_attention(a, device, &d, &c, &q, &table, &type)) return NULL;
+  const int dims = q.g.n;
+  const int64_t batch[1] = {d.batch}, heads[1] = {d.q_heads};
+  if (!tensor(a[10], -1, WIDE_I32, device, 1, batch, "lengths", &lengths) || !tensor(a[12], type, 0, device, dims, q.g.size, "out", &out) || !no_negative_strides(&out, "out")) return NULL;
+  if (a[11] != Py_None && !tensor(a[11], TYPE_F32, 0, device, 1, heads, "slopes", &slopes)) return NULL;
+  if (a[13] != Py_None && (!tensor(a[13], TYPE_F32, 0, device, dims - 1, q.g.size, "lse", &lse) || !dense(&lse, "lse"))) return NULL;
+  if (a[14] != Py_None) {
+    void* p;
+    if (!describe(a[14], &ws)) return NULL;
+    if (ws.device != device) return refuse("workspace", "is not on the current device"), NULL;
+    if (!dense(&ws, "workspace") || !workspace_of(a[14], &p, &ws_bytes)) return NULL;
+  }
+  if (!stream_on(a[16], device, &stream)) return NULL;
+  d.out_strides[0] = out.g.stride[0];
+  d.out_strides[1] = dims == 3 ? 0 : out.g.stride[1];
+  d.out_strides[2] = out.g.stride[dims - 2];
+  comfuse_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f_paged_attention(&d, &c, q.p, table.p, lengths.p, slopes.p, (void*)out.p, (float*)lse.p, (void*)ws.p, ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong((long)st);
+}
+
+// paged_attention_size(<the arguments of fill_attention>, device) -> (status, bytes)
+static PyObject* py_paged_attention_size(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  comfuse_paged_attention_desc_t d;
+  comfuse_kv_cache_t c;
+  Described q, table;
+  int64_t device;
+  int type;
+  size_t bytes = 0;
+  if (!fixed_args(n, 11, "paged_attention_size") || !to_i64(a[10], &device) || !fill_attention(a, device, &d, &c, &q, &table, &type)) return NULL;
+  const comfuse_status_t st = f_paged_attention_size(&d, &c, &bytes);
+  return Py_BuildValue("iK", (int)st, (unsigned long long)bytes);
+}
+
+// bind_kv(addresses of comfuse_rotary, _cache_write, _cache_read, _paged_attention, _paged_attention_workspace_size, the tensor library's int32, int64 and fp64 types)
+static PyObject* py_bind_kv(PyObject* self, PyObject* args) {
+  unsigned long long f[5];
+  PyObject* t[3];
+  if (!PyArg_ParseTuple(args, "KKKKKOOO", f, f + 1, f + 2, f + 3, f + 4, t, t + 1, t + 2)) return NULL;
+  f_rotary = (rotary_fn)(uintptr_t)f[0];
+  f_cache_write = (cache_write_fn)(uintptr_t)f[1];
+  f_cache_read = (cache_read_fn)(uintptr_t)f[2];
+  f_paged_attention = (paged_attention_fn)(uintptr_t)f[3];
+  f_paged_attention_size = (paged_attention_size_fn)(uintptr_t)f[4];
+  t_i32 = Py_NewRef(t[0]);
+  t_i64 = Py_NewRef(t[1]);
+  t_f64 = Py_NewRef(t[2]);
+  Py_RETURN_NONE;
+}
+
 // stream(function or stream object, device) -> the handle that a call would use
 static PyObject* py_stream(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   int64_t device;
@@ -597,6 +906,12 @@ static PyMethodDef methods[] = {
     {"bind_q8", py_bind_q8, METH_VARARGS, NULL},
     {"stream", (PyCFunction)(void (*)(void))py_stream, METH_FASTCALL, NULL},
     {"describe", (PyCFunction)(void (*)(void))py_describe, METH_FASTCALL, NULL},
+    {"bind_kv", py_bind_kv, METH_VARARGS, NULL},
+    {"rotary", (PyCFunction)(void (*)(void))py_rotary, METH_FASTCALL, NULL},
+    {"cache_write", (PyCFunction)(void (*)(void))py_cache_write, METH_FASTCALL, NULL},
+    {"cache_read", (PyCFunction)(void (*)(void))py_cache_read, METH_FASTCALL, NULL},
+    {"paged_attention", (PyCFunction)(void (*)(void))py_paged_attention, METH_FASTCALL, NULL},
+    {"paged_attention_size", (PyCFunction)(void (*)(void))py_paged_attention_size, METH_FASTCALL, NULL},
     {"quantize_rows", (PyCFunction)(void (*)(void))py_quantize_rows, METH_FASTCALL, NULL},
     {"gemm_q8", (PyCFunction)(void (*)(void))py_gemm_q8, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};

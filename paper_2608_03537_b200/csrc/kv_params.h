@@ -1,0 +1,82 @@
+// Parameter blocks and launchers of the key-value cache (plain data).  Strides are in BYTES unless said otherwise.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "host_common.h"
+
+namespace comfuse {
+
+// Where a cached row lies: base + page * page_stride + head * head_stride + row * row_stride.
+struct CacheSide {
+  char* rows;
+  float* scale;
+  long long page, head, row;                    // bytes
+  long long scale_page, scale_head, scale_row;  // elements
+};
+
+struct RowsSide {
+  const char* in;
+  char* out;
+  long long in_token, in_head, out_token, out_head;
+};
+
+struct RotaryWriteParams {
+  int tokens, q_heads, kv_heads, D;
+  int tokens_per_cta;
+  RowsSide q, k, v;      // (k, v: in only)
+  CacheSide kc, vc;
+  const long long* slots;
+  long long capacity;    // slots of the cache
+  int page_size;
+  const int* positions;  // null: nothing is turned
+  const double* freqs;
+  long long axis_stride; // elements
+  int pairs, adjacent;
+  int section_end[4];    // the first pair behind each axis
+  float sign;            // of the sine
+  unsigned int* status;
+};
+// dtype: of q, k, v; cached: keys and values go into the cache; quantized: in 8 bits
+cudaError_t launch_rotary_write(int dtype, bool cached, bool quantized, RotaryWriteParams p, const DeviceInfo& dev, cudaStream_t stream);
+
+struct CacheReadParams {
+  int tokens, heads, D, page_size;
+  CacheSide kc, vc;
+  RowsSide k, v;         // (out only)
+  const long long* slots;
+  long long capacity;
+  unsigned int* status;
+};
+cudaError_t launch_cache_read(int dtype, bool quantized, const CacheReadParams& p, const DeviceInfo& dev, cudaStream_t stream);
+
+struct PagedAttentionParams {
+  int batch, tokens, heads, group, D;   // group: query heads of a key head
+  int rows;                             // tokens * group: the queries of a sequence that read the same keys
+  int row_blocks;                       // CTAs' worth of them
+  int pages, page_size, max_length, window;
+  const char* q;
+  char* out;
+  long long q_batch, q_token, q_head, out_batch, out_token, out_head;
+  CacheSide kc, vc;
+  const int* table;
+  long long table_stride;               // elements
+  const int* lengths;
+  const float* slopes;
+  float* lse;
+  float alpha, softcap;
+  float* part;                          // partial results, see paged_attention.cuh
+  int ctas;
+  unsigned int* status;
+};
+// How a call is cut: rows of a tile (8 * the row tiles of a warp), row blocks, CTAs, bytes of partial results.
+struct PagedAttentionPlan {
+  int row_tiles, row_blocks, ctas;
+  bool joined;                          // items may be split: a second kernel joins them
+  size_t workspace;
+};
+PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, bool quantized, int max_length, int window, int tokens);
+cudaError_t launch_paged_attention(int dtype, bool quantized, const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream);
+
+}  // namespace comfuse
