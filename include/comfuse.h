@@ -522,7 +522,7 @@ comfuse_status_t comfuse_rotary(const comfuse_rotary_desc_t* desc, const comfuse
 typedef struct {
   void *k, *v;
   float *k_scale, *v_scale;             /* quantized: required; otherwise NULL */
-  int32_t pages, heads, page_size, D;   /* >= 1; page_size <= 65536; D <= 256, a multiple of 8 (quantized: of 16) */
+  int32_t pages, heads, page_size, D;   /* >= 1; page_size <= 65536; pages * page_size < 2^31; D <= 256, a multiple of 8 (quantized: of 16) */
   int32_t dtype;                        /* COMFUSE_DTYPE_BF16 or _F16: what rows are written from and read back to, and, unless quantized, held in */
   int32_t quantized;                    /* 0 or 1 */
   int64_t k_strides[3], v_strides[3];   /* of a page, of a head, of a row */

@@ -51,7 +51,7 @@ comfuse_status_t check_cache(const comfuse_kv_cache_t* c) {
   if (c->pages < 1 || c->heads < 1 || c->page_size < 1 || c->D < 1 || !type_16(c->dtype) || (c->quantized & ~1)) return COMFUSE_ERR_INVALID_ARG;
   if (!c->k || !c->v || (c->quantized ? !c->k_scale || !c->v_scale : c->k_scale || c->v_scale)) return COMFUSE_ERR_INVALID_ARG;
   if (c->D % (c->quantized ? 16 : 8) != 0) return COMFUSE_ERR_ALIGNMENT;
-  if (c->D > 256 || c->page_size > 65536 || c->heads > 65536) return COMFUSE_ERR_UNSUPPORTED;
+  if (c->D > 256 || c->page_size > 65536 || c->heads > 65536 || static_cast<int64_t>(c->pages) * c->page_size > 0x7FFFFFFF) return COMFUSE_ERR_UNSUPPORTED;
   const int64_t d_ = c->D;
   const int bytes = c->quantized ? 1 : 2;
   CHECK_STRIDES(c->k_strides, bytes, c->pages, c->heads, c->page_size);
@@ -110,7 +110,7 @@ comfuse_status_t check_read(const comfuse_cache_read_desc_t* d, const comfuse_kv
   const int64_t d_ = c->D;
   CHECK_STRIDES(d->k_strides, 2, d->tokens, c->heads);
   CHECK_STRIDES(d->v_strides, 2, d->tokens, c->heads);
-  if (static_cast<int64_t>(d->tokens) * c->heads > (int64_t{1} << 32)) return COMFUSE_ERR_UNSUPPORTED;  // (the grid)
+  if (static_cast<int64_t>(d->tokens) * c->heads >= (int64_t{1} << 30)) return COMFUSE_ERR_UNSUPPORTED;  // (rows, of keys and of values, are counted in 32 bits)
   return aligned(k, 16) && aligned(v, 16) && aligned(slots, 8) ? COMFUSE_OK : COMFUSE_ERR_ALIGNMENT;
 }
 
@@ -212,7 +212,7 @@ comfuse_status_t comfuse_rotary(const comfuse_rotary_desc_t* desc, const comfuse
   if (s != COMFUSE_OK) return s;
   RotaryWriteParams p = {};
   p.tokens = desc->tokens; p.q_heads = desc->heads; p.D = desc->D;
-  p.q = rows_side(x, desc->x_strides, out, desc->out_strides, desc->dtype == COMFUSE_DTYPE_F32 ? 4 : 2);
+  p.side[0] = rows_side(x, desc->x_strides, out, desc->out_strides, desc->dtype == COMFUSE_DTYPE_F32 ? 4 : 2);
   fill_rotary(rotary, &p);
   p.status = dev->status_word;
   return launched(launch_rotary_write(desc->dtype, false, false, p, *dev, static_cast<cudaStream_t>(cuda_stream)));
@@ -227,12 +227,12 @@ comfuse_status_t comfuse_cache_write(const comfuse_cache_write_desc_t* desc, con
   if (s != COMFUSE_OK) return s;
   RotaryWriteParams p = {};
   p.tokens = desc->tokens; p.q_heads = desc->q_heads; p.kv_heads = cache->heads; p.D = cache->D;
-  p.q = rows_side(q, desc->q_strides, q_out, desc->q_out_strides, 2);
-  p.k = rows_side(k, desc->k_strides, nullptr, nullptr, 2);
-  p.v = rows_side(v, desc->v_strides, nullptr, nullptr, 2);
+  p.side[0] = rows_side(q, desc->q_strides, q_out, desc->q_out_strides, 2);
+  p.side[1] = rows_side(k, desc->k_strides, nullptr, nullptr, 2);
+  p.side[2] = rows_side(v, desc->v_strides, nullptr, nullptr, 2);
   fill_cache(*cache, &p.kc, &p.vc);
   p.slots = reinterpret_cast<const long long*>(slots);
-  p.page_size = cache->page_size;
+  p.page_size = Divisor(cache->page_size);
   p.capacity = static_cast<long long>(cache->pages) * cache->page_size;
   fill_rotary(rotary, &p);
   p.status = dev->status_word;
@@ -246,7 +246,9 @@ comfuse_status_t comfuse_cache_read(const comfuse_cache_read_desc_t* desc, const
   s = check_device(&dev);
   if (s != COMFUSE_OK) return s;
   CacheReadParams p = {};
-  p.tokens = desc->tokens; p.heads = cache->heads; p.D = cache->D; p.page_size = cache->page_size;
+  p.tokens = desc->tokens; p.heads = cache->heads; p.D = cache->D;
+  p.page_size = Divisor(cache->page_size);
+  p.rows = Divisor(2 * cache->heads);
   fill_cache(*cache, &p.kc, &p.vc);
   p.k = rows_side(nullptr, nullptr, k, desc->k_strides, 2);
   p.v = rows_side(nullptr, nullptr, v, desc->v_strides, 2);

@@ -2,9 +2,10 @@
 //
 //   angle = positions[axis(i)][t] * freqs[i];   (a, b) -> (a cos - b sin, a sin + b cos);   s = max|y| / 127,  code = rint(y / s)
 //
-// Every element is read and written once: the bytes bound it.  The angles of a token are shared by all of its heads: each CTA computes the sines and cosines of its
-// tokens once, into shared memory, and then turns their rows.  A row of D is D / 16 units of two 16-byte pieces (16-bit types), one lane each, so that
-// both halves of a pair are in one lane and a row in 4, 8, 16 or 32 lanes of one warp; the largest value of a row is a few shuffles away.
+// Every element is read and written once: the bytes bound it.  A row of D is D / 16 units of two 16-byte pieces (16-bit types), one lane each, so that both halves of a
+// pair are in one lane and a row in a power of two of lanes of one warp; the largest value of a row is a few shuffles away.  The angles of a token are shared by all of its
+// heads: a warp computes the sines and cosines of its token once, two pairs a lane, and each lane keeps those of its unit while it turns row after row.  Where there are few tokens
+// several warps share one, each with its own sines.
 #include <cstdio>
 
 #include "kv_params.h"
@@ -14,7 +15,7 @@ namespace comfuse {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostAngles = 1024;  // of a CTA's tokens (one of D = 512 has 256)
+constexpr int kMostPairs = 256;  // (D <= 512)
 
 // How a row's pairs lie.  kHalvesWhole: (i, i + pairs), pairs a multiple of 8: a unit is a piece of the first half and its partner.  kAdjacent: (2i, 2i + 1): a unit is
 // 16 elements in line.  kHalves: any other number of pairs: 16 elements in line, and the partners one by one (from the L1).
@@ -57,29 +58,27 @@ __device__ __forceinline__ void unit_pieces(int u, int D, int pairs, int (&at)[2
   at[1] = at[0] + 8 < D ? at[0] + 8 : -1;
 }
 
-// Elements of a unit, turned.  `cs`, `sn`: of the row's token.  `row`: where the partners of kHalves stand.
+// The sines and cosines of a unit's eight pairs, from the token's; pairs behind the last do not turn.
+template <int MODE>
+__device__ __forceinline__ void unit_angles(const float2* angles, int first, int pairs, float2 (&cs)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) cs[i] = first + i < pairs ? angles[first + i] : make_float2(1.f, 0.f);
+}
+
+// Elements of a unit, turned.  `cs`: of its pairs (kHalvesWhole, kAdjacent); `angles`, `row`: the token's, and where the partners of kHalves stand.
 template <int DT, int MODE>
-__device__ __forceinline__ void turn(const Unit<DT>& unit, const char* row, const float* cs, const float* sn, int pairs, float (&y)[2][8]) {
+__device__ __forceinline__ void turn(const Unit<DT>& unit, const float2 (&cs)[8], const char* row, const float2* angles, int pairs, float (&y)[2][8]) {
 #pragma unroll
   for (int k = 0; k < 2; ++k)
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[k][i] = Elem<DT>::of(unit.w[k], i);
   if (MODE == kHalvesWhole) {
     if (unit.at[0] < pairs) {
-      const float4* c4 = reinterpret_cast<const float4*>(cs + unit.at[0]);
-      const float4* s4 = reinterpret_cast<const float4*>(sn + unit.at[0]);
-      float c[8], s[8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float4 a = c4[h], b = s4[h];
-        c[4 * h] = a.x; c[4 * h + 1] = a.y; c[4 * h + 2] = a.z; c[4 * h + 3] = a.w;
-        s[4 * h] = b.x; s[4 * h + 1] = b.y; s[4 * h + 2] = b.z; s[4 * h + 3] = b.w;
-      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float a = y[0][i], b = y[1][i];
-        y[0][i] = a * c[i] - b * s[i];
-        y[1][i] = a * s[i] + b * c[i];
+        y[0][i] = a * cs[i].x - b * cs[i].y;
+        y[1][i] = a * cs[i].y + b * cs[i].x;
       }
     }
   } else if (MODE == kAdjacent) {
@@ -87,11 +86,12 @@ __device__ __forceinline__ void turn(const Unit<DT>& unit, const char* row, cons
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int pair = unit.at[k] / 2 + i;
-        if (unit.at[k] >= 0 && pair < pairs) {
-          const float a = y[k][2 * i], b = y[k][2 * i + 1], c = cs[pair], s = sn[pair];
-          y[k][2 * i] = a * c - b * s;
-          y[k][2 * i + 1] = a * s + b * c;
+        const float a = y[k][2 * i], b = y[k][2 * i + 1];
+        const float2 z = cs[4 * k + i];
+        // (elements behind the pairs stay as they are, whatever they hold)
+        if (unit.at[0] / 2 + 4 * k + i < pairs) {
+          y[k][2 * i] = a * z.x - b * z.y;
+          y[k][2 * i + 1] = a * z.y + b * z.x;
         }
       }
   } else if (MODE == kHalves) {
@@ -103,8 +103,9 @@ __device__ __forceinline__ void turn(const Unit<DT>& unit, const char* row, cons
         if (unit.at[k] >= 0 && e < 2 * pairs) {
           const bool first = e < pairs;
           const int pair = first ? e : e - pairs;
-          const float other = Elem<DT>::get(row, first ? e + pairs : pair), c = cs[pair], s = sn[pair];
-          y[k][i] = first ? y[k][i] * c - other * s : other * s + y[k][i] * c;
+          const float other = Elem<DT>::get(row, first ? e + pairs : pair);
+          const float2 z = angles[pair];
+          y[k][i] = first ? y[k][i] * z.x - other * z.y : other * z.y + y[k][i] * z.x;
         }
       }
   }
@@ -135,177 +136,177 @@ __device__ __forceinline__ float codes_of(const float (&y)[2][8], uint32_t top, 
   return finite ? amax / 127.f : __int_as_float(0x7FFFFFFF);
 }
 
-// Lanes of a row: the power of two that holds its units.
-__host__ __device__ inline int lanes_of(int D, int pairs, int mode) {
+// Lanes of a row: the power of two that holds its units (its logarithm).
+int lanes_log2_of(int D, int pairs, int mode) {
   const int units = mode == kHalvesWhole ? pairs / 8 + (D - 2 * pairs + 15) / 16 : (D + 15) / 16;
-  int lanes = 1;
-  while (lanes < units) lanes *= 2;
-  return lanes;
+  int n = 0;
+  while ((1 << n) < units) ++n;
+  return n;
 }
 
 template <int DT, bool CACHED, bool Q8, int MODE>
-__global__ void __launch_bounds__(kThreads) rotary_write_kernel(const RotaryWriteParams p, const int lanes) {
-  __shared__ __align__(16) float s_cos[kMostAngles], s_sin[kMostAngles];
+__global__ void __launch_bounds__(kThreads, DT == COMFUSE_DTYPE_F32 ? 2 : 3) rotary_write_kernel(const RotaryWriteParams p, const int lanes_log2) {
+  __shared__ float2 s_angles[MODE == kNothing ? 1 : kThreads / 32][MODE == kNothing ? 1 : kMostPairs];
   griddep_launch_dependents();
-  griddep_wait();
-  const int pairs = p.pairs;
-  const int pitch = (pairs + 3) & ~3;  // of a token's angles
-  const int first = blockIdx.x * p.tokens_per_cta;
-  const int mine = min(p.tokens_per_cta, p.tokens - first);
-  if constexpr (MODE != kNothing) {
-    for (int i = threadIdx.x; i < mine * pairs; i += kThreads) {
-      const int t = i / pairs, pair = i - t * pairs;
-      const int axis = (pair >= p.section_end[0]) + (pair >= p.section_end[1]) + (pair >= p.section_end[2]);
-      // Whole turns leave in 64 bits: a position of 2^31 at one radian is 3.4e8 turns, known to 2^-24 of a turn.
-      const double turns = p.positions[axis * p.axis_stride + first + t] * (p.freqs[pair] * 0.15915494309189535);
-      float s, c;
-      sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &s, &c);
-      s_cos[t * pitch + pair] = c;
-      s_sin[t * pitch + pair] = p.sign * s;
-    }
-    __syncthreads();
-  }
-  const int rows = p.q_heads + (CACHED ? 2 * p.kv_heads : 0);
-  const int groups = kThreads / lanes, u = threadIdx.x % lanes;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long item = static_cast<long long>(blockIdx.x) * (kThreads / 32) + warp;
+  const long long token = item >> p.slices_log2;
+  if (token >= p.tokens) return;  // (whole warps, which share nothing with others)
+  const int pairs = p.pairs, lanes = 1 << lanes_log2, u = lane & (lanes - 1);
+  const unsigned rows = p.rows, step = (32u >> lanes_log2) << p.slices_log2;
   int at[2];
   unit_pieces<MODE>(u, p.D, pairs, at);
-  const bool active = at[0] < p.D;
+  const bool active = at[0] < p.D, second = at[1] >= 0;
+  griddep_wait();
 
-  // Two rows a round: their loads are on the way together.
-  int row = threadIdx.x / lanes, t = 0;
-  auto settle = [&](int& r, int& tt) {
-    while (r >= rows && tt < mine) {
-      r -= rows;
-      ++tt;
-    }
-  };
-  settle(row, t);
-  while (__any_sync(0xFFFFFFFFu, t < mine)) {
-    Unit<DT> unit[2];
-    const char* in[2] = {nullptr, nullptr};
-    int rr[2], tt[2];
+  long long place = -1;
+  if constexpr (CACHED) place = p.slots[token];
+  // Two rows a round, whose loads are on the way together.
+  unsigned next = ((static_cast<unsigned>(item) & ((1u << p.slices_log2) - 1)) << (5 - lanes_log2)) + (lane >> lanes_log2);
+  Unit<DT> unit[2];
+  const char* in[2];
+  unsigned row[2], kind[2];
+  bool there[2];
+  auto load = [&]() {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      rr[j] = row;
-      tt[j] = t;
-      unit[j].at[0] = at[0];
-      unit[j].at[1] = at[1];
-      if (t < mine) {
-        const long long token = first + t;
-        const int h = row;
-        in[j] = h < p.q_heads                              ? p.q.in + token * p.q.in_token + h * p.q.in_head
-                : !CACHED || h < p.q_heads + p.kv_heads ? p.k.in + token * p.k.in_token + (h - p.q_heads) * p.k.in_head
-                                                           : p.v.in + token * p.v.in_token + (h - p.q_heads - p.kv_heads) * p.v.in_head;
-        if (active) {
-          load_piece<DT>(in[j], at[0], unit[j].w[0]);
-          if (at[1] >= 0) load_piece<DT>(in[j], at[1], unit[j].w[1]);
+      there[j] = next < rows;
+      row[j] = next;
+      next += step;
+      kind[j] = 0;
+      if constexpr (CACHED) {
+        const unsigned q_heads = p.q_heads, kv_heads = p.kv_heads;
+        if (row[j] >= q_heads) {
+          kind[j] = row[j] >= q_heads + kv_heads ? 2 : 1;
+          row[j] -= kind[j] == 2 ? q_heads + kv_heads : q_heads;
         }
       }
-      if (!(t < mine && active && at[1] >= 0)) {
-#pragma unroll
-        for (int i = 0; i < 2 * Elem<DT>::kBytes; ++i) unit[j].w[1][i] = 0u;
+      const RowsSide& side = p.side[kind[j]];
+      in[j] = side.in + token * side.in_token + row[j] * side.in_head;
+      unit[j].at[0] = at[0];
+      unit[j].at[1] = at[1];
+      if (there[j] && active) {
+        load_piece<DT>(in[j], at[0], unit[j].w[0]);
+        if (second) load_piece<DT>(in[j], at[1], unit[j].w[1]);
       }
-      if (!(t < mine && active)) {
-#pragma unroll
-        for (int i = 0; i < 2 * Elem<DT>::kBytes; ++i) unit[j].w[0][i] = 0u;
-      }
-      row += groups;
-      settle(row, t);
     }
+  };
+  load();
+  float2* angles = s_angles[MODE == kNothing ? 0 : warp];
+  float2 cs[8];
+  if constexpr (MODE != kNothing) {  // (under the first rows' loads)
+    for (int pair = lane; pair < pairs; pair += 32) {
+      const int axis = (pair >= p.section_end[0]) + (pair >= p.section_end[1]) + (pair >= p.section_end[2]);
+      // Whole turns leave in 64 bits: a position of 2^31 at one radian is 3.4e8 turns, known to 2^-24 of a turn.
+      const double turns = p.positions[axis * p.axis_stride + token] * (p.freqs[pair] * 0.15915494309189535);
+      float s, c;
+      sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &s, &c);
+      angles[pair] = make_float2(c, p.sign * s);
+    }
+    __syncwarp();
+    if constexpr (MODE != kHalves) unit_angles<MODE>(angles, MODE == kAdjacent ? 8 * u : at[0], pairs, cs);
+  }
+  const int slot = place >= 0 && place < p.capacity ? static_cast<int>(place) : -1;
+  unsigned page = 0, line = 0;
+  if constexpr (CACHED) {
+    page = p.page_size.of(slot);
+    line = slot - page * p.page_size.d;
+  }
+  while (__any_sync(0xFFFFFFFFu, there[0])) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const bool there = tt[j] < mine, is_q = rr[j] < p.q_heads, is_k = !is_q && rr[j] < p.q_heads + p.kv_heads;
       float y[2][8];
-      if (MODE != kNothing && there && active && (is_q || is_k))
-        turn<DT, MODE>(unit[j], in[j], s_cos + tt[j] * pitch, s_sin + tt[j] * pitch, pairs, y);
-      else {
+      if (MODE != kNothing && (!CACHED || kind[j] < 2)) {
+        if (MODE != kHalves || (there[j] && active)) turn<DT, MODE>(unit[j], cs, in[j], angles, pairs, y);
+      } else {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int i = 0; i < 8; ++i) y[k][i] = Elem<DT>::of(unit[j].w[k], i);
       }
       if (MODE == kHalves) __syncwarp();  // every partner is read before a row is written over itself
-      const long long token = first + tt[j];
-      if (there && is_q) {
-        if (active) {
-          char* out = p.q.out + token * p.q.out_token + rr[j] * p.q.out_head;
-          if (COMFUSE_IN_BOUNDS(token < p.tokens && at[0] + 8 <= p.D && at[1] + 8 <= p.D, p.status)) {
-            store_piece<DT>(out, at[0], y[0]);
-            if (at[1] >= 0) store_piece<DT>(out, at[1], y[1]);
-          }
+      if (kind[j] == 0) {
+        const RowsSide& side = p.side[0];
+        char* out = side.out + token * side.out_token + row[j] * side.out_head;
+        if (there[j] && active && COMFUSE_IN_BOUNDS(token < p.tokens && at[0] + 8 <= p.D && at[1] + 8 <= p.D, p.status)) {
+          store_piece<DT>(out, at[0], y[0]);
+          if (second) store_piece<DT>(out, at[1], y[1]);
         }
       }
       if constexpr (CACHED) {
         uint32_t top = 0u;
         if constexpr (Q8) {
+          if (active) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(y[k][i]) & 0x7FFFFFFFu);
+              for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(y[k][i]) & 0x7FFFFFFFu);
+          }
           for (int o = lanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         }
-        if (there && !is_q) {
-          const long long slot = p.slots[token];
-          if (slot >= 0 && slot < p.capacity) {
-            const CacheSide& c = is_k ? p.kc : p.vc;
-            const long long page = slot / p.page_size, r = slot - page * p.page_size;
-            const int h = is_k ? rr[j] - p.q_heads : rr[j] - p.q_heads - p.kv_heads;
-            char* out = c.rows + page * c.page + h * c.head + r * c.row;
-            if constexpr (Q8) {
-              uint32_t w[2][2];
-              const float scale = codes_of(y, top, w);
-              if (u == 0 && COMFUSE_IN_BOUNDS(h < p.kv_heads && slot < p.capacity, p.status)) c.scale[page * c.scale_page + h * c.scale_head + r * c.scale_row] = scale;
-              if (active && COMFUSE_IN_BOUNDS(h < p.kv_heads && slot < p.capacity && at[0] + 8 <= p.D, p.status)) {
-                if (MODE == kHalvesWhole && at[1] != at[0] + 8) {
-                  st_8(out + at[0], w[0]);
-                  st_8(out + at[1], w[1]);
-                } else {  // 16 elements in line (D is a multiple of 16)
-                  const uint32_t both[4] = {w[0][0], w[0][1], w[1][0], w[1][1]};
-                  st_16(out + at[0], both);
-                }
+        if (kind[j] && there[j] && slot >= 0) {
+          const CacheSide& c = kind[j] == 1 ? p.kc : p.vc;
+          const unsigned h = row[j];
+          char* out = c.rows + page * c.page + h * c.head + line * c.row;
+          if constexpr (Q8) {
+            uint32_t w[2][2];
+            const float scale = codes_of(y, top, w);
+            if (u == 0 && COMFUSE_IN_BOUNDS(h < p.kv_heads && slot < p.capacity, p.status)) c.scale[page * c.scale_page + h * c.scale_head + line * c.scale_row] = scale;
+            if (active && COMFUSE_IN_BOUNDS(h < p.kv_heads && slot < p.capacity && at[0] + 8 <= p.D, p.status)) {
+              if (MODE == kHalvesWhole && at[1] != at[0] + 8) {
+                st_8(out + at[0], w[0]);
+                st_8(out + at[1], w[1]);
+              } else {  // 16 elements in line (D is a multiple of 16)
+                const uint32_t both[4] = {w[0][0], w[0][1], w[1][0], w[1][1]};
+                st_16(out + at[0], both);
               }
-            } else if (active && COMFUSE_IN_BOUNDS(h < p.kv_heads && slot < p.capacity && at[0] + 8 <= p.D, p.status)) {
-              store_piece<DT>(out, at[0], y[0]);
-              if (at[1] >= 0) store_piece<DT>(out, at[1], y[1]);
             }
+          } else if (active && COMFUSE_IN_BOUNDS(h < p.kv_heads && slot < p.capacity && at[0] + 8 <= p.D, p.status)) {
+            store_piece<DT>(out, at[0], y[0]);
+            if (second) store_piece<DT>(out, at[1], y[1]);
           }
         }
       }
     }
+    load();
   }
 }
 
-// A lane of the group of `lanes` that has a token's row of a head (keys, then values) reads and writes 16 elements of it.
-template <int DT, bool Q8>
-__global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadParams p, const int lanes) {
-  constexpr int kRows = 4;  // a lane's rows in flight
+// A lane of the group of `lanes` that has a token's row of a head (keys, then values) reads and writes 16 elements of it.  ROWS: of a lane, in flight together.  Neighbouring groups have the
+// same head of neighbouring tokens, so that a page is read in line; the rows of a few tokens' heads, which lie in line where they go, are still written by one CTA.
+template <int DT, bool Q8, int ROWS>
+__global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadParams p, const int lanes_log2) {
   griddep_launch_dependents();
   griddep_wait();
-  const int groups = kThreads / lanes, u = threadIdx.x % lanes, at = 16 * u;
+  const int groups = kThreads >> lanes_log2, at = 16 * (threadIdx.x & ((1 << lanes_log2) - 1));
   if (at >= p.D) return;
   const bool second = at + 8 < p.D;
-  const int rows = 2 * p.heads;
-  const long long total = static_cast<long long>(p.tokens) * rows;
-  const long long first = static_cast<long long>(blockIdx.x) * groups * kRows + threadIdx.x / lanes;
-  uint32_t w[kRows][8];
-  float scale[kRows];
-  char* out[kRows];
+  const unsigned first = blockIdx.x * (groups * ROWS) + (threadIdx.x >> lanes_log2);
+  uint32_t w[ROWS][8];
+  float scale[ROWS];
+  char* out[ROWS];
+  unsigned token[ROWS], row[ROWS];
+  long long slot[ROWS];
 #pragma unroll
-  for (int j = 0; j < kRows; ++j) {
-    const long long i = first + static_cast<long long>(j) * groups;
+  for (int j = 0; j < ROWS; ++j) {
+    const unsigned i = first + j * groups;
+    const unsigned line = i >> p.tokens_log2, block = p.rows.of(line);
+    row[j] = line - block * p.rows.d;
+    token[j] = (block << p.tokens_log2) + (i & ((1u << p.tokens_log2) - 1));
+    slot[j] = token[j] < static_cast<unsigned>(p.tokens) ? p.slots[token[j]] : -1;
+  }
+#pragma unroll
+  for (int j = 0; j < ROWS; ++j) {
+    const unsigned r = row[j];
     out[j] = nullptr;
-    if (i >= total) continue;
-    const long long token = i / rows;
-    const int r = static_cast<int>(i - token * rows);
-    const long long slot = p.slots[token];
-    if (slot < 0 || slot >= p.capacity) continue;
-    const bool is_k = r < p.heads;
+    if (slot[j] < 0 || slot[j] >= p.capacity) continue;
+    const bool is_k = r < static_cast<unsigned>(p.heads);
     const CacheSide& c = is_k ? p.kc : p.vc;
     const RowsSide& to = is_k ? p.k : p.v;
-    const int h = is_k ? r : r - p.heads;
-    const long long page = slot / p.page_size, line = slot - page * p.page_size;
+    const unsigned h = is_k ? r : r - p.heads, n = static_cast<unsigned>(slot[j]);
+    const long long page = p.page_size.of(n), line = n - page * p.page_size.d;
     const char* in = c.rows + page * c.page + h * c.head + line * c.row;
-    out[j] = to.out + token * to.out_token + h * to.out_head;
+    out[j] = to.out + token[j] * to.out_token + h * to.out_head;
     if constexpr (Q8) {
       ld_16(in + at, w[j]);
       scale[j] = c.scale[page * c.scale_page + h * c.scale_head + line * c.scale_row];
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadPar
     }
   }
 #pragma unroll
-  for (int j = 0; j < kRows; ++j) {
+  for (int j = 0; j < ROWS; ++j) {
     if (!out[j]) continue;
     if constexpr (Q8) {
       float v[2][8];
@@ -336,7 +337,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheReadPar
 }
 
 template <typename Kernel, typename Params>
-cudaError_t launch(Kernel kernel, const Params& p, int lanes, unsigned grid, cudaStream_t stream) {
+cudaError_t launch(Kernel kernel, const Params& p, int lanes_log2, unsigned grid, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
   cfg.gridDim = dim3(grid, 1, 1);
@@ -349,12 +350,12 @@ cudaError_t launch(Kernel kernel, const Params& p, int lanes, unsigned grid, cud
     cfg.numAttrs = 1;
   }
   count_launch();
-  return cudaLaunchKernelEx(&cfg, kernel, p, lanes);
+  return cudaLaunchKernelEx(&cfg, kernel, p, lanes_log2);
 }
 
 template <int DT, bool CACHED, bool Q8>
 cudaError_t launch_mode(int mode, const RotaryWriteParams& p, unsigned grid, cudaStream_t stream) {
-  const int lanes = lanes_of(p.D, p.pairs, mode);
+  const int lanes = lanes_log2_of(p.D, p.pairs, mode);
   switch (mode) {
     case kHalvesWhole: return launch(rotary_write_kernel<DT, CACHED, Q8, kHalvesWhole>, p, lanes, grid, stream);
     case kAdjacent: return launch(rotary_write_kernel<DT, CACHED, Q8, kAdjacent>, p, lanes, grid, stream);
@@ -370,15 +371,14 @@ cudaError_t launch_mode(int mode, const RotaryWriteParams& p, unsigned grid, cud
 cudaError_t launch_rotary_write(int dtype, bool cached, bool quantized, RotaryWriteParams p, const DeviceInfo& dev, cudaStream_t stream) {
   const int mode = !p.positions ? kNothing : p.adjacent ? kAdjacent : p.pairs % 8 == 0 ? kHalvesWhole : kHalves;
   if (mode == kNothing) p.pairs = 0;
-  const int pitch = (p.pairs + 3) & ~3;
-  // Tokens of a CTA: one where there are few, else as many as give its threads two rows each.
-  const int rows = p.q_heads + (cached ? 2 * p.kv_heads : 0), groups = kThreads / lanes_of(p.D, p.pairs, mode);
-  int per = 1;
-  while (2 * per * pitch <= kMostAngles && per * rows < 2 * groups && static_cast<long long>(p.tokens) >= 8ll * per * dev.sm_count) per *= 2;
-  p.tokens_per_cta = per;
-  const unsigned grid = static_cast<unsigned>((static_cast<long long>(p.tokens) + per - 1) / per);
+  p.rows = p.q_heads + (cached ? 2 * p.kv_heads : 0);
+  // Warps of a token: one where there are tokens enough to fill the GPU, else as many as leave each lane two rows.
+  const int groups = 32 >> lanes_log2_of(p.D, p.pairs, mode);
+  while ((static_cast<long long>(p.tokens) << p.slices_log2) < 16ll * dev.sm_count && (2 * groups) << p.slices_log2 < p.rows) ++p.slices_log2;
+  const long long warps = static_cast<long long>(p.tokens) << p.slices_log2;
+  const unsigned grid = static_cast<unsigned>((warps + kThreads / 32 - 1) / (kThreads / 32));
   if (verbose_enabled())
-    std::fprintf(stderr, "comfuse: rotary_write dtype=%d cached=%d quantized=%d mode=%d tokens a CTA=%d\n", dtype, cached, quantized, mode, per);
+    std::fprintf(stderr, "comfuse: rotary_write dtype=%d cached=%d quantized=%d mode=%d warps a token=%d\n", dtype, cached, quantized, mode, 1 << p.slices_log2);
   if (!cached) {
     switch (dtype) {
       case COMFUSE_DTYPE_BF16: return launch_mode<COMFUSE_DTYPE_BF16, false, false>(mode, p, grid, stream);
@@ -391,15 +391,26 @@ cudaError_t launch_rotary_write(int dtype, bool cached, bool quantized, RotaryWr
   return quantized ? launch_mode<COMFUSE_DTYPE_F16, true, true>(mode, p, grid, stream) : launch_mode<COMFUSE_DTYPE_F16, true, false>(mode, p, grid, stream);
 }
 
-cudaError_t launch_cache_read(int dtype, bool quantized, const CacheReadParams& p, const DeviceInfo&, cudaStream_t stream) {
-  const int lanes = lanes_of(p.D, 0, kNothing);
-  const long long rows = 2ll * p.heads * p.tokens, per = 4ll * (kThreads / lanes);
-  const long long grid = (rows + per - 1) / per;
-  if (grid > 0x7FFFFFFF) return cudaErrorInvalidValue;
-  const unsigned n = static_cast<unsigned>(grid);
-  if (dtype == COMFUSE_DTYPE_BF16)
-    return quantized ? launch(cache_read_kernel<COMFUSE_DTYPE_BF16, true>, p, lanes, n, stream) : launch(cache_read_kernel<COMFUSE_DTYPE_BF16, false>, p, lanes, n, stream);
-  return quantized ? launch(cache_read_kernel<COMFUSE_DTYPE_F16, true>, p, lanes, n, stream) : launch(cache_read_kernel<COMFUSE_DTYPE_F16, false>, p, lanes, n, stream);
+namespace {
+template <int DT, bool Q8>
+cudaError_t launch_read(CacheReadParams p, const DeviceInfo& dev, cudaStream_t stream) {
+  const int lanes = lanes_log2_of(p.D, 0, kNothing), groups = kThreads >> lanes;
+  // Eight tokens a block where that leaves no group without one; four rows a lane where they still fill the GPU (32768 x 8 x 128 from 8 bits: 41 us with two, 38 with four, 43
+  // with eight; 500 x 6 x 64: 2.2 us with two, 3.2 with four).
+  while (p.tokens_log2 < 3 && p.tokens % (2 << p.tokens_log2) == 0) ++p.tokens_log2;
+  if (p.tokens >= 64) p.tokens_log2 = 3;
+  const long long blocks = (p.tokens + (1ll << p.tokens_log2) - 1) >> p.tokens_log2, rows = (blocks << p.tokens_log2) * p.rows.d;
+  const bool many = rows >= 8ll * 4 * groups * dev.sm_count;
+  const long long per = (many ? 4ll : 1ll) * groups;
+  const unsigned grid = static_cast<unsigned>((rows + per - 1) / per);
+  if (many) return launch(cache_read_kernel<DT, Q8, 4>, p, lanes, grid, stream);
+  return launch(cache_read_kernel<DT, Q8, 1>, p, lanes, grid, stream);
+}
+}  // namespace
+
+cudaError_t launch_cache_read(int dtype, bool quantized, const CacheReadParams& p, const DeviceInfo& dev, cudaStream_t stream) {
+  if (dtype == COMFUSE_DTYPE_BF16) return quantized ? launch_read<COMFUSE_DTYPE_BF16, true>(p, dev, stream) : launch_read<COMFUSE_DTYPE_BF16, false>(p, dev, stream);
+  return quantized ? launch_read<COMFUSE_DTYPE_F16, true>(p, dev, stream) : launch_read<COMFUSE_DTYPE_F16, false>(p, dev, stream);
 }
 
 }  // namespace comfuse

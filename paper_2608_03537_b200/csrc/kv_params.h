@@ -8,6 +8,17 @@
 
 namespace comfuse {
 
+// Division of 32-bit numbers by a divisor known on the host: the high half of n * ceil(2^64 / d) is n / d for every n < 2^32.
+struct Divisor {
+  unsigned long long inverse;  // 0: d = 1
+  unsigned d;
+  Divisor() = default;
+  explicit Divisor(unsigned by) : inverse(by > 1 ? ~0ull / by + 1 : 0), d(by) {}
+#ifdef __CUDACC__
+  __device__ __forceinline__ unsigned of(unsigned n) const { return inverse ? static_cast<unsigned>(__umul64hi(n, inverse)) : n; }
+#endif
+};
+
 // Where a cached row lies: base + page * page_stride + head * head_stride + row * row_stride.
 struct CacheSide {
   char* rows;
@@ -24,12 +35,13 @@ struct RowsSide {
 
 struct RotaryWriteParams {
   int tokens, q_heads, kv_heads, D;
-  int tokens_per_cta;
-  RowsSide q, k, v;      // (k, v: in only)
+  int rows;              // of a token: what is to turn or store
+  int slices_log2;       // warps that share a token
+  RowsSide side[3];      // queries, keys, values (the latter two: in only)
   CacheSide kc, vc;
   const long long* slots;
-  long long capacity;    // slots of the cache
-  int page_size;
+  long long capacity;    // slots of the cache, below 2^31
+  Divisor page_size;
   const int* positions;  // null: nothing is turned
   const double* freqs;
   long long axis_stride; // elements
@@ -42,7 +54,9 @@ struct RotaryWriteParams {
 cudaError_t launch_rotary_write(int dtype, bool cached, bool quantized, RotaryWriteParams p, const DeviceInfo& dev, cudaStream_t stream);
 
 struct CacheReadParams {
-  int tokens, heads, D, page_size;
+  int tokens, heads, D;
+  Divisor page_size, rows;  // rows: 2 * heads of a token
+  int tokens_log2;          // of a block of tokens, whose rows of one head lie side by side in a warp
   CacheSide kc, vc;
   RowsSide k, v;         // (out only)
   const long long* slots;
