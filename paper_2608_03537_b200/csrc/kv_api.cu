@@ -175,21 +175,22 @@ comfuse_status_t launched(cudaError_t e) { return e == cudaSuccess ? COMFUSE_OK 
 
 }  // namespace
 
-// Row tiles: eight query rows each.  A CTA takes up to four (two for D > 128, whose results would not stay in the registers), more rows are further row blocks, which read the
-// same keys a second time (from the L2).  The partial results' CTAs are those that fit on the GPU's 148 SMs; never more than there may be units.
+// A CTA takes up to 64 query rows, more are further row blocks, which read the same keys a second time (from the L2).  There are as many CTAs as fit on the 148 SMs of the GPU, and never more than
+// there may be units.
 PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, bool quantized, int max_length, int window, int tokens) {
   PagedAttentionPlan plan = {};
-  const int most = D > 128 ? 2 : 4, DH = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-  plan.row_tiles = rows <= 8 ? 1 : rows <= 16 ? 2 : most;
-  plan.row_blocks = (rows + 8 * plan.row_tiles - 1) / (8 * plan.row_tiles);
+  const int DH = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+  plan.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  plan.row_blocks = (rows + plan.rows - 1) / plan.rows;
+  const paged::FormFacts f = quantized ? paged::facts<true>(D, plan.rows) : paged::facts<false>(D, plan.rows);
   int64_t seen = max_length;  // positions of a sequence that may be visible, from the block of the first on
-  if (window > 0) seen = std::min<int64_t>(seen, static_cast<int64_t>(window) + tokens - 1 + paged::kBlock - 1);
-  const int64_t units = std::max<int64_t>(1, (seen + paged::kUnit - 1) / paged::kUnit);
+  if (window > 0) seen = std::min<int64_t>(seen, static_cast<int64_t>(window) + tokens - 1 + f.block - 1);
+  const int64_t units = std::max<int64_t>(1, (seen + f.unit - 1) / f.unit);
   const int64_t items = static_cast<int64_t>(batch) * heads * plan.row_blocks;
-  const int resident = 148 * (DH == 256 && !quantized ? 1 : 2);
-  plan.ctas = static_cast<int>(units >= resident ? resident : std::min<int64_t>(resident, items * units));
+  if (items > 0x7FFFFFFF / units) return plan;  // (units are counted in 32 bits: no CTAs)
+  plan.ctas = static_cast<int>(std::min<int64_t>(148 * f.ctas_per_sm, items * units));
   plan.joined = units > 1 && plan.ctas > 1;
-  plan.workspace = plan.joined ? static_cast<size_t>(plan.ctas) * paged::part_floats(8 * plan.row_tiles, DH) * sizeof(float) : 0;
+  plan.workspace = plan.joined ? static_cast<size_t>(plan.ctas) * paged::part_floats(plan.rows, DH) * sizeof(float) : 0;
   return plan;
 }
 
@@ -262,7 +263,9 @@ comfuse_status_t comfuse_paged_attention_workspace_size(const comfuse_paged_atte
   if (!bytes) return COMFUSE_ERR_INVALID_ARG;
   const comfuse_status_t s = check_attention_sizes(desc, cache);
   if (s != COMFUSE_OK) return s;
-  *bytes = plan_of(desc, cache).workspace;
+  const PagedAttentionPlan plan = plan_of(desc, cache);
+  if (plan.ctas == 0) return COMFUSE_ERR_UNSUPPORTED;
+  *bytes = plan.workspace;
   return COMFUSE_OK;
 }
 
@@ -271,6 +274,7 @@ comfuse_status_t comfuse_paged_attention(const comfuse_paged_attention_desc_t* d
   comfuse_status_t s = check_attention(desc, cache, q, table, lengths, slopes, out, lse);
   if (s != COMFUSE_OK) return s;
   const PagedAttentionPlan plan = plan_of(desc, cache);
+  if (plan.ctas == 0) return COMFUSE_ERR_UNSUPPORTED;
   if (plan.workspace > 0) {
     if (!workspace || workspace_bytes < plan.workspace) return COMFUSE_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return COMFUSE_ERR_ALIGNMENT;
@@ -283,7 +287,7 @@ comfuse_status_t comfuse_paged_attention(const comfuse_paged_attention_desc_t* d
   p.batch = d.batch; p.tokens = d.tokens; p.heads = cache->heads; p.group = d.q_heads / cache->heads; p.D = cache->D;
   p.rows = d.tokens * p.group;
   p.row_blocks = plan.row_blocks;
-  p.pages = cache->pages; p.page_size = cache->page_size;
+  p.pages = cache->pages; p.page_size = Divisor(cache->page_size);
   p.max_length = static_cast<int>(longest(desc, cache));
   p.window = d.window < p.max_length + d.tokens ? d.window : 0;  // (one that hides nothing)
   p.q = static_cast<const char*>(q);

@@ -69,7 +69,8 @@ struct PagedAttentionParams {
   int batch, tokens, heads, group, D;   // group: query heads of a key head
   int rows;                             // tokens * group: the queries of a sequence that read the same keys
   int row_blocks;                       // CTAs' worth of them
-  int pages, page_size, max_length, window;
+  int pages, max_length, window;
+  Divisor page_size;
   const char* q;
   char* out;
   long long q_batch, q_token, q_head, out_batch, out_token, out_head;
@@ -84,9 +85,9 @@ struct PagedAttentionParams {
   int ctas;
   unsigned int* status;
 };
-// How a call is cut: rows of a tile (8 * the row tiles of a warp), row blocks, CTAs, bytes of partial results.
+// How a call is cut: query rows of a CTA (8, 16, 32 or 64), row blocks, CTAs, bytes of partial results.
 struct PagedAttentionPlan {
-  int row_tiles, row_blocks, ctas;
+  int rows, row_blocks, ctas;
   bool joined;                          // items may be split: a second kernel joins them
   size_t workspace;
 };

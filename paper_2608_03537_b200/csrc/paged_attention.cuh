@@ -5,16 +5,17 @@
 // Every visible key and value is read once, and for few queries that is all there is to bound it: 2 D (or 4 D) flops an element of a query row against HBM.  So the
 // kernel is built around loads in flight.
 //
-//   * The call's work is a line of units of 64 positions (sequence by sequence, key head by key head), cut into equal shares, one for each of the CTAs that fit on the
+//   * The call's work is a line of units of some positions (sequence by sequence, key head by key head), cut into equal shares, one for each of the CTAs that fit on the
 //     GPU: whatever the lengths, all finish together.  A CTA finds its share from the lengths themselves.  An item (sequence, key head) that lies in one share is
 //     finished there; one that is cut leaves a partial sum, maximum and weighted values for each share, and a second kernel joins them, in order.
-//   * A unit is four blocks of 16 positions, one for each warp.  A warp is on its own: it fetches its blocks by 16-byte asynchronous copies, several blocks ahead and across the
-//     ends of items, into a ring of its own, and keeps a running maximum, sum and weighted values; no barrier but at the end of an item, where the four are joined.
+//   * A unit is a block of 16 or 32 positions for each of the CTA's key warps.  A key warp is on its own: it fetches its blocks by 16-byte asynchronous copies, several blocks ahead and
+//     across the ends of items, into a ring of its own, and keeps a running maximum, sum and weighted values; no barrier but at the end of an item, where they are joined.  Where there are
+//     more rows of queries than a warp holds, several warps share a ring and its fetching, each with rows of its own, and meet once a block.
 //   * The keys are the 16-row operand of the warp-wide matrix instruction and the queries the 8-column one: S^T = K Q^T, then O^T += V^T P^T.  The queries that share a key head
 //     (tokens x heads of its group) fill eight columns a tile, so that a single query wastes an eighth of what rows of sixteen would.  P^T changes from the accumulators' layout to
 //     the operand's by two 8x8 transposes.
-//   * 8 bits: the codes become fp16 by two permutes and a subtraction for each four, the key's scale is a factor of its score and the value's scale of its weight.  Codes of a row are
-//     taken as they lie in the registers; queries, and the rows of O^T, are permuted alike.
+//   * 8 bits: the first product is one of integers.  A query row is a multiple of a power of two, 22 bits and a sign, in three digits of 8 bits, a product each; the sums are exact.
+//     The key's scale is a factor of its score, the value's scale one of its weight.  The values' codes become fp16 by five instructions for each four.
 //   * The maximum is renewed only when a score is more than 8 (a factor of 256) above it: a vote instead of a reduction in most blocks.
 #pragma once
 
@@ -31,82 +32,88 @@ cudaError_t launch_f16(const PagedAttentionPlan& plan, const PagedAttentionParam
 cudaError_t launch_bf16_q8(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream);
 cudaError_t launch_f16_q8(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream);
 
-namespace {
-
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kBlock = 16;              // positions of a warp's step
-constexpr int kUnit = kBlock * kWarps;  // of a CTA's
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 8.f;           // log2 of what a weight may exceed 1 by
+constexpr float kSlack = 8.f;  // log2 of what a weight may exceed 1 by
+constexpr int kDigits = 3;     // of a query, 8 bits
 
-// Sizes of an instance: D up to DH, NT tiles of eight queries.
-template <bool Q8, int DH, int NT>
+// Sizes of an instance: D up to DH, NT tiles of eight queries a warp, RW warps with rows of their own to a ring.
+template <bool Q8, int DH, int NT, int RW>
 struct Form {
   static constexpr int kRowBytes = DH * (Q8 ? 1 : 2);
-  static constexpr int kPieces = kRowBytes / 16;             // of a row
-  static constexpr int kSide = kBlock * kRowBytes;           // keys, or values, of a block
-  static constexpr int kStage = 2 * kSide + (Q8 ? 128 : 0);  // and their scales
-  static constexpr int kJoinColumns = NT == 4 ? 32 : 64;     // where warps are joined, at a time
-  static constexpr int kPitch = kJoinColumns + 4;            // floats of a row there: a warp's stores fall on all banks
+  static constexpr int kPieces = kRowBytes / 16;                  // of a row
+  static constexpr int kGroups = kRowBytes <= 128 ? 2 : 1;        // of 16 positions, in a block
+  static constexpr int kBlock = 16 * kGroups;
+  static constexpr int kKeyWarps = DH == 256 && RW == 4 ? 2 : 4;  // rings
+  static constexpr int kWarps = kKeyWarps * RW, kThreads = 32 * kWarps;
+  static constexpr int kUnit = kBlock * kKeyWarps;
+  static constexpr int kRows = 8 * NT * RW;                       // of queries
+  static constexpr int kSide = kBlock * kRowBytes;                // keys, or values, of a block
+  static constexpr int kStage = 2 * kSide + (Q8 ? 8 * kBlock : 0);  // and their scales
+  static constexpr int kJoinColumns = NT > 1 ? 32 : 64;          // where warps are joined, at a time
+  static constexpr int kPitch = kJoinColumns + 4;                 // floats of a row there: a warp's stores fall on all banks
   static constexpr int kJoin = kWarps * 8 * kPitch * 4;
-  static constexpr int kQuery = 8 * NT * DH * 2;
-  static constexpr int kSmall = 704 + 64 * 8 * NT;
-  static constexpr int kCtasPerSm = DH == 256 && !Q8 ? 1 : 2;
-  static constexpr int kSmem = (kCtasPerSm == 2 ? 113 : 226) * 1024;  // what a CTA may take
-  static constexpr int kStages = (kSmem - kJoin - kQuery - kSmall) / (kStage * kWarps);
-  static constexpr int kBytes = kStages * kStage * kWarps + kJoin + kQuery + kSmall;
+  static constexpr int kQuery = kRows * DH * (Q8 ? kDigits : 2);
+  static constexpr int kSmall = 256 + 4 * 32 * kKeyWarps + kRows * (8 * kKeyWarps + 24);
+  static constexpr int kCtasPerSm = RW > 1 || DH == 256 ? 1 : 2;
+  static constexpr int kSmem = kCtasPerSm == 2 ? 113 * 1024 : 226 * 1024;  // what a CTA may take
+  static constexpr int kMostStages = (kSmem - kJoin - kQuery - kSmall) / (kStage * kKeyWarps);
+  static constexpr int kStages = kMostStages < 8 ? kMostStages : 8;
+  static constexpr int kBytes = kStages * kStage * kKeyWarps + kJoin + kQuery + kSmall;
 };
 
-// Partial results of CTA c: two slots (of the first item of its share, and of the last), each 8 NT rows of kPartRow floats: D values, the maximum, the sum.
-__host__ __device__ inline long long part_floats(int rows8, int D) { return 2ll * rows8 * (D + 4); }
+// Partial results of CTA c: two slots (of the first item of its share, and of the last), each `rows` rows of D + 4 floats: D values, the maximum, the sum.
+__host__ __device__ inline long long part_floats(int rows, int D) { return 2ll * rows * (D + 4); }
+
+namespace {
 
 // ------------------------------------------------------------------------------------------------ shares
-// The line of units.  Sequence b has units(b) units for each of its `hr` items (key heads x row blocks).
+// The line of units.  Each of a sequence's `hr` items (key heads x row blocks) has the same number of them.
 struct Line {
-  long long total, share, longer;  // the first `longer` CTAs have share + 1 units
-  __device__ long long begin(long long cta) const { return cta * share + (cta < longer ? cta : longer); }
-  __device__ long long owner(long long unit) const {
-    const long long l = longer * (share + 1);
+  unsigned total, share, longer;  // the first `longer` CTAs have share + 1 units
+  __device__ unsigned begin(unsigned cta) const { return cta * share + (cta < longer ? cta : longer); }
+  __device__ unsigned owner(unsigned unit) const {
+    const unsigned l = longer * (share + 1);
     return unit < l ? unit / (share + 1) : longer + (unit - l) / share;
   }
 };
 struct Sequence {
   int length, low, units;  // positions low .. length - 1 are visible to some token; units are counted from low rounded down to a block
 };
+template <typename F>
 __device__ __forceinline__ Sequence sequence_of(const PagedAttentionParams& p, int b) {
   Sequence s;
   s.length = min(max(p.lengths[b], 0), p.max_length);
   s.low = p.window > 0 ? max(0, s.length - p.tokens + 1 - p.window) : 0;
-  s.units = max(1, (s.length - (s.low & ~(kBlock - 1)) + kUnit - 1) / kUnit);  // (an empty sequence has a unit too: its rows are written)
+  s.units = max(1u, static_cast<unsigned>(s.length - (s.low & ~(F::kBlock - 1)) + F::kUnit - 1) / F::kUnit);  // (an empty sequence has a unit too: its rows are written)
   return s;
 }
 struct Place {
   int b, hr, unit;
 };
-// By all of a CTA's threads (the first kThreads of them): the line, and where `n` units given as the function of the line lie.
 struct Scan {
-  long long warp_sum[kWarps];
+  unsigned warp_sum[16];
   Place place;
 };
-template <typename UnitOf>
+// By all threads of a CTA: the line, and where the unit that `unit_of` names lies.
+template <typename F, int THREADS, typename UnitOf>
 __device__ __forceinline__ Line find(const PagedAttentionParams& p, Scan* s, UnitOf unit_of, Place* place) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (p.batch + kThreads - 1) / kThreads;
-  const long long hr = static_cast<long long>(p.heads) * p.row_blocks;
+  const int per = (p.batch + THREADS - 1) / THREADS;
+  const unsigned hr = p.heads * p.row_blocks;
   const int b0 = min(tid * per, p.batch), b1 = min(b0 + per, p.batch);
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += sequence_of(p, b).units;
-  long long upto = mine;
+  unsigned mine = 0;
+  for (int b = b0; b < b1; ++b) mine += sequence_of<F>(p, b).units;
+  unsigned upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+    const unsigned v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
     if (lane >= o) upto += v;
   }
   if (lane == 31) s->warp_sum[warp] = upto;
   __syncthreads();
-  long long before = 0, total = 0;
+  unsigned before = 0, total = 0;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
+  for (int w = 0; w < THREADS / 32; ++w) {
     if (w < warp) before += s->warp_sum[w];
     total += s->warp_sum[w];
   }
@@ -115,15 +122,15 @@ __device__ __forceinline__ Line find(const PagedAttentionParams& p, Scan* s, Uni
   line.total = total * hr;
   line.share = line.total / p.ctas;
   line.longer = line.total - line.share * p.ctas;
-  const long long unit = unit_of(line);
+  const unsigned unit = unit_of(line);
   if (unit >= before * hr && unit < (before + mine) * hr) {
-    long long rest = unit - before * hr;
+    unsigned rest = unit - before * hr;
     for (int b = b0; b < b1; ++b) {
-      const long long n = sequence_of(p, b).units;
+      const unsigned n = sequence_of<F>(p, b).units;
       if (rest < n * hr) {
         s->place.b = b;
-        s->place.hr = static_cast<int>(rest / n);
-        s->place.unit = static_cast<int>(rest - s->place.hr * n);
+        s->place.hr = rest / n;
+        s->place.unit = rest - s->place.hr * n;
         break;
       }
       rest -= n * hr;
@@ -168,6 +175,11 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_s8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 // Two codes of x (chosen by `bytes`, whose even places name them) as fp16: 0x6400 + u is 1024 + u, u = code + 128.
 __device__ __forceinline__ uint32_t codes_f16(uint32_t flipped, uint32_t bytes) {
   const uint32_t raw = __byte_perm(flipped, 0x64646464u, bytes);
@@ -198,182 +210,238 @@ __device__ __forceinline__ int place_of(int r, int c) {
 }
 
 // ------------------------------------------------------------------------------------------------ the kernel
-template <int DT, bool Q8, int DH, int NT>
-__global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attention_kernel(const PagedAttentionParams p) {
-  using F = Form<Q8, DH, NT>;
+template <int DT, bool Q8, int DH, int NT, int RW>
+__global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, NT, RW>::kCtasPerSm) attention_kernel(const PagedAttentionParams p) {
+  using F = Form<Q8, DH, NT, RW>;
   constexpr bool kBf16 = DT == COMFUSE_DTYPE_BF16;  // of queries and outputs
-  constexpr bool kMmaBf16 = kBf16 && !Q8;           // of the products: 8-bit codes are exact in fp16
+  constexpr bool kMmaBf16 = kBf16 && !Q8;           // of the second product: 8-bit codes are exact in fp16
   // A weight in 16 bits is off by half a step of its type, which behind a sum over like terms is as much as the output's own rounding.  So the weights go in twice, rounded and what
   // the rounding left.  fp16 weights of bf16 outputs are eight times as fine as those and go in once.
   constexpr bool kTwice = !(Q8 && kBf16);
-  constexpr int kSteps = DH / 16;
-  constexpr int S = F::kStages;
-  static_assert(S >= 2, "a ring of two blocks at least");
+  constexpr int kSteps = DH / 16, G = F::kGroups, S = F::kStages;
+  static_assert(S >= 2 && S <= 8, "a ring of two blocks at least");
   extern __shared__ __align__(128) char smem[];
-  char* s_ring = smem;
-  float* s_join = reinterpret_cast<float*>(smem + S * F::kStage * kWarps);
-  char* s_query = reinterpret_cast<char*>(s_join) + F::kJoin;
+  float* s_join = reinterpret_cast<float*>(smem + S * F::kStage * F::kKeyWarps);
+  uint32_t* s_query = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s_join) + F::kJoin);
   struct Small {
+    long long out[F::kRows];                                       // where a row's output goes (-1: nowhere)
+    float top[F::kKeyWarps][F::kRows], sum[F::kKeyWarps][F::kRows];
+    float factor[F::kRows];                                        // 8 bits: what a query was divided by
+    float slope[F::kRows];
+    int token[F::kRows];                                           // its new token
+    int lse[F::kRows];
+    unsigned valid[F::kKeyWarps][8];                               // of the blocks in the ring: positions that are there
     Scan scan;
-    unsigned valid[kWarps][32];         // of the blocks in the ring: positions that are there
-    float top[kWarps][8 * NT], sum[kWarps][8 * NT];
-    float factor[8 * NT];               // 8 bits: what a query was divided by
-    float slope[8 * NT];
-    int token[8 * NT];                  // a row's new token
-    long long out[8 * NT];              // where its output goes (-1: nowhere)
-    int lse[8 * NT];
   };
-  static_assert(sizeof(Small) <= F::kSmall && S <= 32, "room for what is small");
-  Small& sm = *reinterpret_cast<Small*>(s_query + F::kQuery);
+  static_assert(sizeof(Small) <= F::kSmall, "room for what is small");
+  Small& sm = *reinterpret_cast<Small*>(reinterpret_cast<char*>(s_query) + F::kQuery);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int kw = RW == 1 ? warp : warp / RW, rw = RW == 1 ? 0 : warp % RW;  // which ring, which rows
   const int g = lane >> 2, c = lane & 3;
 
   griddep_wait();
   griddep_launch_dependents();  // behind the wait: the joining kernel reads the lengths before its own
 
   Place at;
-  const Line line = find(p, &sm.scan, [](const Line& l) { return min(l.begin(blockIdx.x), l.total - 1); }, &at);
-  const long long first_unit = line.begin(blockIdx.x);
-  const int count = static_cast<int>(line.begin(blockIdx.x + 1) - first_unit);
+  const Line line = find<F, F::kThreads>(p, &sm.scan, [](const Line& l) { return min(l.begin(blockIdx.x), l.total - 1); }, &at);
+  const int count = static_cast<int>(line.begin(blockIdx.x + 1) - line.begin(blockIdx.x));
   if (count <= 0) return;
   const int HR = p.heads * p.row_blocks;
 
-  char* ring = s_ring + warp * S * F::kStage;
+  char* ring = smem + kw * S * F::kStage;
   const uint32_t ring_u32 = smem_u32(ring);
+  auto ring_sync = [&]() {  // the warps of a ring
+    if constexpr (RW == 1) __syncwarp();
+    else named_barrier_sync(1 + kw, 32 * RW);
+  };
   if (p.D < DH) {  // pieces behind D are never fetched and stay zeros
-    for (int i = lane; i < S * F::kStage / 16; i += 32) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
-    __syncwarp();
+    for (int i = lane + 32 * rw; i < S * F::kStage / 16; i += 32 * RW) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
+    ring_sync();
   }
 
-  // ---- fetching, several blocks ahead
-  int f_b = at.b, f_hr = at.hr, f_unit = at.unit, f_left = count;
-  Sequence f_seq = sequence_of(p, f_b);
-  int f_page = -1;  // of position (lane & 15) of the block that is next
-  const bool whole_pages = p.page_size % kBlock == 0;  // a block lies in one page
-  auto look_up = [&]() {
-    const int pos = (f_seq.low & ~(kBlock - 1)) + f_unit * kUnit + warp * kBlock + (lane & 15);
-    f_page = -1;
-    if (f_left > 0 && pos >= f_seq.low && pos < f_seq.length) f_page = p.table[f_b * p.table_stride + pos / p.page_size];
+  // ---- fetching, several blocks ahead.  Lane l knows the page and line of position l of the block that is next, and has piece `my_piece` of rows my_row, my_row + kRowStep, ...
+  constexpr int kRowStep = 32 * RW / F::kPieces, kLoads = F::kBlock / kRowStep;
+  static_assert(kLoads >= 1 && kLoads * kRowStep == F::kBlock, "rows of a block over the lanes of a ring's warps");
+  const int my_piece = lane % F::kPieces, my_row = rw * (32 / F::kPieces) + lane / F::kPieces, my_pos = lane & (F::kBlock - 1);
+  const bool my_piece_there = my_piece * 16 < p.D * (Q8 ? 1 : 2);
+  const uint32_t my_dst = ring_u32 + my_row * F::kRowBytes + place_of<F::kPieces>(my_row, my_piece) * 16;
+  const bool whole_pages = p.page_size.d % F::kBlock == 0;  // a block lies in one page
+  int f_b = at.b, f_hr = at.hr, f_unit = at.unit, f_left = count, f_base, f_page, f_line;
+  Sequence f_seq = sequence_of<F>(p, f_b);
+  const int* f_table = p.table + f_b * p.table_stride;
+  const char *f_k, *f_v;  // the head's rows, from this lane's piece on
+  const float *f_ks, *f_vs;
+  auto set_head = [&]() {
+    const int head = p.row_blocks == 1 ? f_hr : f_hr / p.row_blocks;
+    f_k = p.kc.rows + head * p.kc.head + my_piece * 16;
+    f_v = p.vc.rows + head * p.vc.head + my_piece * 16;
+    if constexpr (Q8) {
+      f_ks = p.kc.scale + head * p.kc.scale_head;
+      f_vs = p.vc.scale + head * p.vc.scale_head;
+    }
   };
+  auto look_up = [&]() {
+    f_base = (f_seq.low & ~(F::kBlock - 1)) + f_unit * F::kUnit + kw * F::kBlock;
+    const int pos = f_base + my_pos;
+    f_page = -1;
+    if (pos < f_seq.length) {
+      const unsigned n = p.page_size.of(pos);
+      f_line = pos - n * p.page_size.d;
+      f_page = f_table[n];
+    }
+  };
+  set_head();
   look_up();
-  const int D_bytes = p.D * (Q8 ? 1 : 2);
-  constexpr int kLoads = F::kPieces / 2, kRowsALoad = 32 / F::kPieces;
-  const int my_row = lane / F::kPieces, my_piece = lane % F::kPieces;
-  const bool my_piece_there = my_piece * 16 < D_bytes;
   auto fetch = [&](int stage) {
     if (f_left > 0) {
-      const bool there = f_page >= 0 && f_page < p.pages;
-      const unsigned valid = __ballot_sync(0xFFFFFFFFu, there) & 0xFFFFu;
-      if (lane == 0) sm.valid[warp][stage] = valid;
+      const bool there = f_page >= 0 && f_page < p.pages && f_base + my_pos >= f_seq.low;
+      constexpr unsigned kAll = F::kBlock == 32 ? 0xFFFFFFFFu : 0xFFFFu;
+      const unsigned valid = __ballot_sync(0xFFFFFFFFu, there) & kAll;
+      if (lane == 0) sm.valid[kw][stage] = valid;
       if (valid) {
-        const int head = f_hr / p.row_blocks;
-        const int pos = (f_seq.low & ~(kBlock - 1)) + f_unit * kUnit + warp * kBlock + (lane & 15);
-        const long long page = there ? f_page : 0, row = there ? pos % p.page_size : 0;
-        const uint32_t dst = ring_u32 + stage * F::kStage;
-        const long long k_at = page * p.kc.page + head * p.kc.head + row * p.kc.row, v_at = page * p.vc.page + head * p.vc.head + row * p.vc.row;
-        if (valid == 0xFFFFu && whole_pages) {
-          const char* k = p.kc.rows + __shfl_sync(0xFFFFFFFFu, k_at, 0) + my_row * p.kc.row + my_piece * 16;
-          const char* v = p.vc.rows + __shfl_sync(0xFFFFFFFFu, v_at, 0) + my_row * p.vc.row + my_piece * 16;
+        const uint32_t dst = my_dst + stage * F::kStage;
+        if (valid == kAll && whole_pages) {
+          const int first = f_line - my_pos + my_row;
+          const char* k = f_k + f_page * p.kc.page + first * p.kc.row;
+          const char* v = f_v + f_page * p.vc.page + first * p.vc.row;
+          const long long k_step = kRowStep * p.kc.row, v_step = kRowStep * p.vc.row;
           if (my_piece_there) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-              const int r = i * kRowsALoad + my_row;
-              const uint32_t to = dst + r * F::kRowBytes + place_of<F::kPieces>(r, my_piece) * 16;
-              cp_async_16(to, k + i * kRowsALoad * p.kc.row, true);
-              cp_async_16(to + F::kSide, v + i * kRowsALoad * p.vc.row, true);
+              const uint32_t to = (F::kPieces >= 8 ? dst ^ ((i * kRowStep & 7) << 4) : dst) + i * kRowStep * F::kRowBytes;
+              cp_async_16(to, k, true);
+              cp_async_16(to + F::kSide, v, true);
+              k += k_step;
+              v += v_step;
             }
           }
         } else {
+          const int safe_page = there ? f_page : 0, safe_line = there ? f_line : 0;
 #pragma unroll
           for (int i = 0; i < kLoads; ++i) {
-            const int r = i * kRowsALoad + my_row;
-            const char* k = p.kc.rows + __shfl_sync(0xFFFFFFFFu, k_at, r) + my_piece * 16;
-            const char* v = p.vc.rows + __shfl_sync(0xFFFFFFFFu, v_at, r) + my_piece * 16;
-            const bool ok = (valid >> r) & 1u;
-            const uint32_t to = dst + r * F::kRowBytes + place_of<F::kPieces>(r, my_piece) * 16;
-            if (my_piece_there) {  // (a position that is not there reads as zeros)
-              cp_async_16(to, ok ? k : p.kc.rows, ok);
-              cp_async_16(to + F::kSide, ok ? v : p.vc.rows, ok);
+            const int r = i * kRowStep + my_row;
+            const long long page = __shfl_sync(0xFFFFFFFFu, safe_page, r), row = __shfl_sync(0xFFFFFFFFu, safe_line, r);
+            const bool ok = (valid >> r) & 1u;  // (a position that is not there reads as zeros)
+            const uint32_t to = (F::kPieces >= 8 ? dst ^ ((i * kRowStep & 7) << 4) : dst) + i * kRowStep * F::kRowBytes;
+            if (my_piece_there) {
+              cp_async_16(to, f_k + page * p.kc.page + row * p.kc.row, ok);
+              cp_async_16(to + F::kSide, f_v + page * p.vc.page + row * p.vc.row, ok);
             }
           }
         }
         if constexpr (Q8) {
-          const CacheSide& side = lane < 16 ? p.kc : p.vc;
-          const float* s = side.scale + page * side.scale_page + head * side.scale_head + row * side.scale_row;
-          cp_async_4(dst + 2 * F::kSide + lane * 4, there ? s : side.scale, there);
+          const long long page = there ? f_page : 0, row = there ? f_line : 0;
+          const uint32_t to = ring_u32 + stage * F::kStage + 2 * F::kSide + my_pos * 4;
+          // (16 positions: the upper lanes take the values' scales)
+          if (rw == 0 && (F::kBlock == 32 || lane < 16)) cp_async_4(to, f_ks + page * p.kc.scale_page + row * p.kc.scale_row, there);
+          if (rw == 0 && (F::kBlock == 32 || lane >= 16)) cp_async_4(to + 4 * F::kBlock, f_vs + page * p.vc.scale_page + row * p.vc.scale_row, there);
         }
       }
-      if (--f_left > 0 && ++f_unit == f_seq.units) {
-        f_unit = 0;
-        if (++f_hr == HR) {
-          f_hr = 0;
-          f_seq = sequence_of(p, ++f_b);
+      if (--f_left > 0) {
+        if (++f_unit == f_seq.units) {
+          f_unit = 0;
+          if (++f_hr == HR) {
+            f_hr = 0;
+            f_seq = sequence_of<F>(p, ++f_b);
+            f_table = p.table + f_b * p.table_stride;
+          }
+          set_head();
         }
+        look_up();
       }
-      look_up();
     }
     cp_async_commit();
   };
   for (int s = 0; s < S - 1; ++s) fetch(s);
 
-  // ---- an item's queries: loaded by pieces of 8 elements, kept in shared memory as rows (8 bits: permuted as the codes lie)
-  constexpr int kQueryPieces = DH / 8, kQueryLoads = (8 * NT * kQueryPieces + kThreads - 1) / kThreads;
+  // ---- an item's queries: loaded by pieces of 8 elements, kept in shared memory as the product's operands, eight bytes a lane for each step and tile
+  constexpr int kQueryPieces = DH / 8, kQueryLoads = (F::kRows * kQueryPieces + F::kThreads - 1) / F::kThreads;
+  constexpr int kQuerySteps = Q8 ? DH / 32 : DH / 16, kPlane = kQuerySteps * NT * RW * 64;  // words (of a digit)
   uint32_t q_raw[kQueryLoads][4];
   auto load_queries = [&](int b, int hr) {
-    const int head = hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * 8 * NT;
+    const int head = hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows;
 #pragma unroll
     for (int i = 0; i < kQueryLoads; ++i) {
-      const int n = tid + i * kThreads, r = n / kQueryPieces, piece = n % kQueryPieces, row = row0 + r;
+      const int n = tid + i * F::kThreads, r = n / kQueryPieces, piece = n % kQueryPieces, row = row0 + r;
       q_raw[i][0] = q_raw[i][1] = q_raw[i][2] = q_raw[i][3] = 0u;
-      if (r < 8 * NT && row < p.rows && piece * 8 < p.D) {
-        const int token = row / p.group, h = head * p.group + row % p.group;
+      if (r < F::kRows && row < p.rows && piece * 8 < p.D) {
+        const int token = row / p.group, h = head * p.group + row - token * p.group;
         ld_16(p.q + b * p.q_batch + token * p.q_token + h * p.q_head + piece * 16, q_raw[i]);
       }
     }
   };
   auto keep_queries = [&](int b, int hr) {
-    const int head = hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * 8 * NT;
+    const int head = hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows;
 #pragma unroll
     for (int i = 0; i < kQueryLoads; ++i) {
-      const int n = tid + i * kThreads, r = n / kQueryPieces, piece = n % kQueryPieces;
-      if constexpr (Q8 && kBf16) {
-        // bf16 to fp16: divided by the power of two below its largest element, a row keeps all of its bits down to 2^-14 of that
+      const int n = tid + i * F::kThreads, r = n / kQueryPieces, piece = n % kQueryPieces;
+      uint32_t* to = s_query + (r >> 3) * 64 + (r & 7) * 8;  // (of the step's tiles: this row's lanes)
+      if constexpr (Q8) {
+        // A multiple of 2^-21 of the power of two at or below the row's largest element, in three digits: exact for bf16 down to 2^-14 of that, for fp16 to 2^-11.
         float v[8], most = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           v[j] = Elem<DT>::of(q_raw[i], j);
           most = fmaxf(most, fabsf(v[j]));
         }
+        bool odd = false;  // an infinity or a NaN, which has no digits
+#pragma unroll
+        for (int j = 0; j < 8; ++j) odd |= !isfinite(v[j]);
 #pragma unroll
         for (int o = kQueryPieces / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-        const uint32_t e = __float_as_uint(most) & 0x7F800000u;
-        const bool usual = e >= 0x00800000u * 2 && e < 0x00800000u * 253;
-        const float down = usual ? reciprocal_of_power(__uint_as_float(e)) : 1.f;
-        if (r < 8 * NT && piece == 0) sm.factor[r] = usual ? __uint_as_float(e) : 1.f;
+        odd = __any_sync(0xFFFFFFFFu, odd) && [&] {
+          unsigned row_odd = __ballot_sync(0xFFFFFFFFu, odd);
+          return ((row_odd >> (lane & ~(kQueryPieces - 1) & 31)) & (kQueryPieces >= 32 ? 0xFFFFFFFFu : (1u << (kQueryPieces & 31)) - 1u)) != 0u;
+        }();
+        const uint32_t e = min(max(__float_as_uint(most) & 0x7F800000u, 0x10000000u), 0x7E000000u);  // (2^-95: a row below that is zero beside any other)
+        const float up = reciprocal_of_power(__uint_as_float(e)) * 0x1p21f;
+        if (r < F::kRows && piece == 0) sm.factor[r] = odd ? __int_as_float(0x7FFFFFFF) : __uint_as_float(e) * 0x1p-21f;
+        uint32_t digit[kDigits][2] = {};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q_raw[i][j] = pack_f16x2_rn(v[2 * j] * down, v[2 * j + 1] * down);
-      }
-      if (r < 8 * NT) {
-        // rows of 2 DH bytes, pieces at places as above
-        *reinterpret_cast<uint4*>(s_query + r * DH * 2 + place_of<kQueryPieces>(r, piece) * 16) = make_uint4(q_raw[i][0], q_raw[i][1], q_raw[i][2], q_raw[i][3]);
+        for (int j = 0; j < 8; ++j) {
+          int x = odd ? 0 : __float2int_rn(v[j] * up);
+#pragma unroll
+          for (int d = kDigits - 1; d > 0; --d) {
+            const int low = static_cast<int8_t>(x & 0xFF);
+            digit[d][j >> 2] |= (low & 0xFFu) << (8 * (j & 3));
+            x = (x - low) >> 8;
+          }
+          digit[0][j >> 2] |= (x & 0xFFu) << (8 * (j & 3));
+        }
+        if (r < F::kRows) {
+#pragma unroll
+          for (int d = 0; d < kDigits; ++d)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) to[d * kPlane + (piece >> 2) * NT * RW * 64 + ((piece & 1) * 2 + w) * 2 + ((piece >> 1) & 1)] = digit[d][w];
+        }
+      } else if (r < F::kRows) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) to[(piece >> 1) * NT * RW * 64 + w * 2 + (piece & 1)] = q_raw[i][w];
       }
     }
-    if (tid < 8 * NT) {
+    if (tid < F::kRows) {
       const int row = row0 + tid, token = min(row / p.group, p.tokens - 1), h = head * p.group + row % p.group;
       sm.token[tid] = token;
       sm.slope[tid] = p.slopes && row < p.rows ? p.slopes[h] * kLog2e : 0.f;
       sm.out[tid] = row < p.rows ? b * p.out_batch + token * p.out_token + h * p.out_head : -1;
       sm.lse[tid] = row < p.rows ? (b * p.tokens + token) * p.heads * p.group + h : 0;
-      if constexpr (Q8 && !kBf16) sm.factor[tid] = 1.f;
     }
   };
+  const int tile0 = rw * NT, row_of_mine = 8 * tile0 + 2 * c;  // this warp's tiles; columns 2c, 2c + 1 of the first are this lane's
+  auto query_operand = [&](int digit, int step, int n) {
+    return *reinterpret_cast<const uint2*>(s_query + digit * kPlane + (step * NT * RW + tile0 + n) * 64 + lane * 2);
+  };
+  constexpr bool kHold = NT == 1 && DH <= 128;  // operands of the queries stay in registers
+  uint2 q_held[kHold ? (Q8 ? kDigits : 1) : 1][kHold ? kQuerySteps : 1];
 
   // ---- a warp's running state
   float o[kSteps][NT][4], top[NT][2], sum[NT][2];
   // 8 bits: for each row a power of two that the scales of the values it sees are divided by, so that the largest become 64 .. 128: with e up to 2^8 a weight stays below 2^15, and is a
   // normal number of fp16 down to 2^-20 of the largest.
   float unit_v[NT][2];
-  auto reset = [&]() {
+  float factor[NT][2];  // of a score
+  const SoftcapLog2 cap(p.alpha, p.softcap > 0.f ? p.softcap : 1.f);
+  auto begin_item = [&]() {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       top[n][0] = top[n][1] = -INFINITY;
@@ -381,141 +449,177 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
       unit_v[n][0] = unit_v[n][1] = 0.f;
 #pragma unroll
       for (int k = 0; k < kSteps; ++k) o[k][n][0] = o[k][n][1] = o[k][n][2] = o[k][n][3] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        factor[n][j] = p.softcap > 0.f ? 1.f : p.alpha * kLog2e;
+        if constexpr (Q8) factor[n][j] *= sm.factor[row_of_mine + 8 * n + j];
+      }
     }
-  };
-
-  constexpr bool kHold = NT == 1;  // the queries' operands stay in registers
-  uint32_t q_held[kHold ? kSteps : 1][2];
-  // Operand of step k for tile n.  16 bits: ldmatrix of pieces 2k, 2k + 1.  8 bits: elements 16 k + 4 c .. + 3 of row g.
-  auto query_operand = [&](int k, int n, uint32_t (&b)[2]) {
-    const int r = 8 * n + g;
-    const char* row = s_query + r * DH * 2;
-    if constexpr (Q8) {
-      const uint2 w = *reinterpret_cast<const uint2*>(row + place_of<kQueryPieces>(r, 2 * k + (c >> 1)) * 16 + (c & 1) * 8);
-      b[0] = w.x;
-      b[1] = w.y;
-    } else {
-      b[0] = *reinterpret_cast<const uint32_t*>(row + place_of<kQueryPieces>(r, 2 * k) * 16 + c * 4);
-      b[1] = *reinterpret_cast<const uint32_t*>(row + place_of<kQueryPieces>(r, 2 * k + 1) * 16 + c * 4);
-    }
-  };
-  float factor[NT][2];  // of a score
-  const SoftcapLog2 cap(p.alpha, p.softcap > 0.f ? p.softcap : 1.f);
-  auto begin_item = [&]() {
-    reset();
     if constexpr (kHold) {
 #pragma unroll
-      for (int k = 0; k < kSteps; ++k) query_operand(k, 0, q_held[k]);
+      for (int d = 0; d < (Q8 ? kDigits : 1); ++d)
+#pragma unroll
+        for (int k = 0; k < kQuerySteps; ++k) q_held[d][k] = query_operand(d, k, 0);
     }
+  };
+  auto query = [&](int digit, int step, int n) {
+    if constexpr (kHold) return q_held[digit][step];
+    else return query_operand(digit, step, n);
+  };
+
+  // ---- one block
+  // Where this lane reads of a row's pieces for ldmatrix; piece `k` (even) of the rows is at this address ^ (k << 4), pieces from 8 on 128 bytes further.
+  const int low_row = lane & 15, v_row = Q8 ? low_row : (lane & 7) + ((lane >> 4) << 3), v_piece = Q8 ? lane >> 4 : (lane >> 3) & 1;
+  const uint32_t k_lane = low_row * F::kRowBytes + place_of<F::kPieces>(low_row, lane >> 4) * 16;
+  const uint32_t v_lane = F::kSide + v_row * F::kRowBytes + place_of<F::kPieces>(v_row, v_piece) * 16;
+  auto at_piece = [](uint32_t base, int k) { return (base ^ ((k & 7) << 4)) + (k >> 3) * 128; };
+  auto block = [&](int stage, const Sequence& seq, int base) {
+    const unsigned valid = sm.valid[kw][stage];
+    if (!valid) return;
+    const uint32_t keys = ring_u32 + stage * F::kStage + k_lane, values = ring_u32 + stage * F::kStage + v_lane;
+    float s[G][NT][4];
+    if constexpr (Q8) {
+      uint32_t a[kQuerySteps][G][4];
+#pragma unroll
+      for (int k = 0; k < kQuerySteps; ++k)
+#pragma unroll
+        for (int h = 0; h < G; ++h) ldmatrix_x4(at_piece(keys + h * 16 * F::kRowBytes, 2 * k), a[k][h]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        int sd[kDigits][G][4];
+#pragma unroll
+        for (int d = 0; d < kDigits; ++d)
+#pragma unroll
+          for (int h = 0; h < G; ++h) sd[d][h][0] = sd[d][h][1] = sd[d][h][2] = sd[d][h][3] = 0;
+#pragma unroll
+        for (int k = 0; k < kQuerySteps; ++k)
+#pragma unroll
+          for (int d = 0; d < kDigits; ++d) {
+            const uint2 b = query(d, k, n);
+#pragma unroll
+            for (int h = 0; h < G; ++h) mma_s8(sd[d][h], a[k][h], b.x, b.y);
+          }
+#pragma unroll
+        for (int h = 0; h < G; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)  // (a digit's sum is at most 128 * 128 * 256: the upper two in 32 bits)
+            s[h][n][i] = fmaf(static_cast<float>(sd[0][h][i] * 256 + sd[1][h][i]), 256.f, static_cast<float>(sd[2][h][i]));
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[h][n][0] = s[h][n][1] = s[h][n][2] = s[h][n][3] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kQuerySteps; ++k) {
+        uint32_t a[G][4];
+#pragma unroll
+        for (int h = 0; h < G; ++h) ldmatrix_x4(at_piece(keys + h * 16 * F::kRowBytes, 2 * k), a[h]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint2 b = query(0, k, n);
+#pragma unroll
+          for (int h = 0; h < G; ++h) mma<kMmaBf16>(s[h][n], a[h], b.x, b.y);
+        }
+      }
+    }
+    float ks[G][2], vs[G][2];
+    if constexpr (Q8) {
+      const float* scales = reinterpret_cast<const float*>(ring + stage * F::kStage + 2 * F::kSide);
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          ks[h][i] = scales[16 * h + 8 * i + g];
+          vs[h][i] = scales[F::kBlock + 16 * h + 8 * i + g];
+        }
+    }
+    const int first = seq.length - p.tokens;  // the first new token's position
+    constexpr unsigned kAll = F::kBlock == 32 ? 0xFFFFFFFFu : 0xFFFFu;
+    const bool all = valid == kAll && base + F::kBlock - 1 <= first && (p.window <= 0 || base > seq.length - 1 - p.window);
+    // s: scores in the log2 domain less the running maximum (0 where there is none yet)
+    float ref[NT][2], limit[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        factor[n][j] = p.softcap > 0.f ? 1.f : p.alpha * kLog2e;
-        if constexpr (Q8) factor[n][j] *= sm.factor[8 * n + 2 * c + j];
+        const bool none = top[n][j] == -INFINITY;
+        ref[n][j] = none ? 0.f : top[n][j];
+        limit[n][j] = none ? -INFINITY : kSlack;
       }
-  };
-
-  // ---- one block
-  auto block = [&](int stage, const Sequence& seq, int base) {
-    const unsigned valid = sm.valid[warp][stage];
-    if (!valid) return;
-    const uint32_t keys = ring_u32 + stage * F::kStage, values = keys + F::kSide;
-    float s[NT][4];
+    if (p.softcap > 0.f || p.slopes || !all) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-    if constexpr (Q8) {
+      for (int h = 0; h < G; ++h)
 #pragma unroll
-      for (int k = 0; k < kSteps; k += 2) {
-        uint32_t r[4];
-        const int row = lane & 15, piece = k + (lane >> 4);
-        ldmatrix_x4(keys + row * F::kRowBytes + place_of<F::kPieces>(row, piece) * 16, r);
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t x = r[2 * h] ^ 0x80808080u, y = r[2 * h + 1] ^ 0x80808080u;
-          const uint32_t a[4] = {codes_f16(x, 0x4140), codes_f16(y, 0x4140), codes_f16(x, 0x4342), codes_f16(y, 0x4342)};
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            uint32_t b[2];
-            if constexpr (kHold) b[0] = q_held[k + h][0], b[1] = q_held[k + h][1];
-            else query_operand(k + h, n, b);
-            mma<false>(s[n], a, b[0], b[1]);
+          for (int i = 0; i < 4; ++i) {
+            const int j = i & 1, r = row_of_mine + 8 * n + j, k = 16 * h + g + 8 * (i >> 1);
+            float v = s[h][n][i] * factor[n][j];
+            if constexpr (Q8) v *= ks[h][i >> 1];
+            if (p.softcap > 0.f) v = cap(v);
+            const int gap = base + k - (first + sm.token[r]);
+            if (p.slopes) v = fmaf(sm.slope[r], static_cast<float>(gap), v);
+            const bool hidden = !(((valid >> k) & 1u) && gap <= 0 && (p.window <= 0 || gap > -p.window));
+            s[h][n][i] = hidden ? -INFINITY : v - ref[n][j];
           }
-        }
-      }
     } else {
 #pragma unroll
-      for (int k = 0; k < kSteps; ++k) {
-        uint32_t a[4];
-        const int row = lane & 15, piece = 2 * k + (lane >> 4);
-        ldmatrix_x4(keys + row * F::kRowBytes + place_of<F::kPieces>(row, piece) * 16, a);
+      for (int h = 0; h < G; ++h)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          uint32_t b[2];
-          if constexpr (kHold) b[0] = q_held[k][0], b[1] = q_held[k][1];
-          else query_operand(k, n, b);
-          mma<kMmaBf16>(s[n], a, b[0], b[1]);
-        }
-      }
-    }
-    float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
-    if constexpr (Q8) {
-      const float* scales = reinterpret_cast<const float*>(ring + stage * F::kStage + 2 * F::kSide);
-      ks[0] = scales[g]; ks[1] = scales[g + 8];
-      vs[0] = scales[16 + g]; vs[1] = scales[24 + g];
-    }
-    const int first = seq.length - p.tokens;  // the first new token's position
-    const bool all = valid == 0xFFFFu && base + kBlock - 1 <= first && (p.window <= 0 || base > seq.length - 1 - p.window);
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = i & 1, hi = i >> 1;
-        float v = Q8 ? s[n][i] * (ks[hi] * factor[n][j]) : s[n][i] * factor[n][j];
-        if (p.softcap > 0.f) v = cap(v);
-        s[n][i] = v;
-      }
-    if (p.slopes || !all) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 8 * n + 2 * c + (i & 1), k = g + 8 * (i >> 1);
-          const int gap = base + k - (first + sm.token[r]);
-          if (p.slopes) s[n][i] = fmaf(sm.slope[r], static_cast<float>(gap), s[n][i]);
-          if (!all && !(((valid >> k) & 1u) && gap <= 0 && (p.window <= 0 || gap > -p.window))) s[n][i] = -INFINITY;
-        }
+          for (int i = 0; i < 4; ++i) s[h][n][i] = fmaf(s[h][n][i], Q8 ? factor[n][i & 1] * ks[h][i >> 1] : factor[n][i & 1], -ref[n][i & 1]);
     }
     // the maximum, where a score is well above it
     bool above = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        above |= s[n][i] > top[n][i & 1] + kSlack;
-        if constexpr (Q8) above |= fabsf(vs[i >> 1]) > 128.f * unit_v[n][i & 1] && s[n][i] != -INFINITY;
-      }
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) above |= s[h][n][i] > limit[n][i & 1];
+    if constexpr (Q8) {
+      float least = unit_v[0][0];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) least = fminf(fminf(least, unit_v[n][0]), unit_v[n][1]);
+#pragma unroll
+      for (int h = 0; h < G; ++h) above |= fmaxf(fabsf(vs[h][0]), fabsf(vs[h][1])) > 128.f * least;
+    }
     if (__any_sync(0xFFFFFFFFu, above)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          float m = fmaxf(s[n][j], s[n][j + 2]);
+          float m = -INFINITY, most = 0.f;
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float v = s[h][n][2 * i + j];
+              m = fmaxf(m, v);
+              if constexpr (Q8) most = fmaxf(most, v == -INFINITY ? 0.f : fabsf(vs[h][i]));
+            }
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-          m = fmaxf(m, top[n][j]);
-          const float less = m == top[n][j] ? 1.f : ex2_approx(top[n][j] - m);
-          top[n][j] = m;
+          // (s is relative to ref: the maximum rises by m, where that is positive or there was none)
+          const bool none = top[n][j] == -INFINITY;
+          const float rise = none ? m : fmaxf(m, 0.f), shift = rise == -INFINITY ? 0.f : rise;
+          const float less = none ? 1.f : ex2_approx(-shift);  // (without a maximum there is nothing yet to make less)
+          top[n][j] = none ? rise : top[n][j] + rise;
           sum[n][j] *= less;
           float both = less;
           if constexpr (Q8) {
-            float most = fmaxf(s[n][j] == -INFINITY ? 0.f : fabsf(vs[0]), s[n][j + 2] == -INFINITY ? 0.f : fabsf(vs[1]));
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
             const float unit = fmaxf(unit_v[n][j], __uint_as_float(min(max(__float_as_uint(most) & 0x7F800000u, 0x04000000u), 0x7E000000u) - 0x03000000u));
             both *= unit_v[n][j] / unit;
             unit_v[n][j] = unit;
           }
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[h][n][2 * i + j] -= shift;
 #pragma unroll
           for (int k = 0; k < kSteps; ++k) {
             o[k][n][j] *= both;
@@ -524,29 +628,34 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
         }
     }
     // weights, as the second product's operand
-    uint32_t w[NT][2], rest[NT][2];
+    uint32_t w[G][NT][2], rest[G][NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float e[4];
+      const float inv[2] = {reciprocal_of_power(unit_v[n][0]), reciprocal_of_power(unit_v[n][1])};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float m = top[n][i & 1];
-        e[i] = ex2_approx(s[n][i] - (m == -INFINITY ? 0.f : m));
-      }
-      sum[n][0] += e[0] + e[2];
-      sum[n][1] += e[1] + e[3];
-      if constexpr (Q8) {
-        const float inv[2] = {reciprocal_of_power(unit_v[n][0]), reciprocal_of_power(unit_v[n][1])};
+      for (int h = 0; h < G; ++h) {
+        float e[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) e[i] = s[n][i] == -INFINITY ? 0.f : e[i] * (vs[i >> 1] * inv[i & 1]);  // (a hidden position's scale may be NaN)
-      }
+        for (int i = 0; i < 4; ++i) e[i] = ex2_approx(s[h][n][i]);
+        sum[n][0] += e[0] + e[2];
+        sum[n][1] += e[1] + e[3];
+        if constexpr (Q8) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t x = pack2<kMmaBf16>(e[2 * h], e[2 * h + 1]);
-        w[n][h] = transpose_8x8(x);
-        if constexpr (kTwice) {
-          const float2 r = unpack2<kMmaBf16>(x);
-          rest[n][h] = transpose_8x8(pack2<kMmaBf16>(e[2 * h] - r.x, e[2 * h + 1] - r.y));
+          for (int i = 0; i < 4; ++i) e[i] *= vs[h][i >> 1] * inv[i & 1];
+          if (!all) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (s[h][n][i] == -INFINITY) e[i] = 0.f;  // (a hidden position's scale may be NaN)
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t x = pack2<kMmaBf16>(e[2 * i], e[2 * i + 1]);
+          w[h][n][i] = transpose_8x8(x);
+          if constexpr (kTwice) {
+            const float2 r = unpack2<kMmaBf16>(x);
+            rest[h][n][i] = transpose_8x8(pack2<kMmaBf16>(e[2 * i] - r.x, e[2 * i + 1] - r.y));
+          }
         }
       }
     }
@@ -554,78 +663,82 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
       if (!all && p.tokens > 1) {
         // Some rows see a position and others do not: a value that is not finite must not reach the others as 0 * inf.  Such values are added to the rows that see them, and
         // are zeros for the product.
+        const char* block_v = ring + stage * F::kStage + F::kSide;
         bool odd = false;
         for (int i = lane; i < F::kSide / 16; i += 32) {
-          const uint4 x = *reinterpret_cast<const uint4*>(ring + stage * F::kStage + F::kSide + i * 16);
+          const uint4 x = *reinterpret_cast<const uint4*>(block_v + i * 16);
           const uint32_t y[4] = {x.x, x.y, x.z, x.w};
           constexpr uint32_t e = kBf16 ? 0x7F80u : 0x7C00u;
 #pragma unroll
           for (int j = 0; j < 4; ++j) odd |= (y[j] & e) == e || (y[j] >> 16 & e) == e;
         }
+        // (the warps of a ring find the same, and clear it together)
         if (__any_sync(0xFFFFFFFFu, odd)) {
-          for (int k = 0; k < kBlock; ++k) {
+          for (int k = 0; k < F::kBlock; ++k) {
             const int pos = base + k - first;
 #pragma unroll
             for (int d = 0; d < kSteps; ++d)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 const int e = 16 * d + 8 * h + g;
-                uint16_t* at_v = reinterpret_cast<uint16_t*>(ring + stage * F::kStage + F::kSide + k * F::kRowBytes + place_of<F::kPieces>(k, e >> 3) * 16 + (e & 7) * 2);
-                const float v = Elem<DT>::get(at_v, 0);
+                const float v = Elem<DT>::get(block_v + k * F::kRowBytes + place_of<F::kPieces>(k, e >> 3) * 16 + (e & 7) * 2, 0);
                 if (!isfinite(v)) {
 #pragma unroll
                   for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                      const int gap = pos - sm.token[8 * n + 2 * c + j];
+                      const int gap = pos - sm.token[row_of_mine + 8 * n + j];
                       if (gap <= 0 && (p.window <= 0 || gap > -p.window)) o[d][n][2 * h + j] += v;
                     }
                 }
               }
           }
-          __syncwarp();
+          ring_sync();
           for (int i = lane; i < F::kSide / 2; i += 32) {
             uint16_t* at_v = reinterpret_cast<uint16_t*>(ring + stage * F::kStage + F::kSide) + i;
             if (!isfinite(Elem<DT>::get(at_v, 0))) *at_v = 0;
           }
-          __syncwarp();
+          ring_sync();
         }
       }
     }
-    if constexpr (Q8) {
 #pragma unroll
-      for (int k = 0; k < kSteps; k += 2) {
-        uint32_t r[4];
-        const int row = lane & 15, piece = k + (lane >> 4);
-        ldmatrix_x4_trans(values + row * F::kRowBytes + place_of<F::kPieces>(row, piece) * 16, r);
+    for (int h = 0; h < G; ++h) {
+      const uint32_t rows = values + h * 16 * F::kRowBytes;
+      if constexpr (Q8) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t x = r[2 * h] ^ 0x80808080u, y = r[2 * h + 1] ^ 0x80808080u;
-          const uint32_t a[4] = {codes_f16(x, 0x4240), codes_f16(x, 0x4341), codes_f16(y, 0x4240), codes_f16(y, 0x4341)};
+        for (int k = 0; k < kSteps; k += 2) {
+          uint32_t r[4];
+          ldmatrix_x4_trans(at_piece(rows, k), r);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            mma<false>(o[k + h][n], a, w[n][0], w[n][1]);
-            if constexpr (kTwice) mma<false>(o[k + h][n], a, rest[n][0], rest[n][1]);
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t x = r[2 * i] ^ 0x80808080u, y = r[2 * i + 1] ^ 0x80808080u;
+            const uint32_t a[4] = {codes_f16(x, 0x4240), codes_f16(x, 0x4341), codes_f16(y, 0x4240), codes_f16(y, 0x4341)};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              mma<false>(o[k + i][n], a, w[h][n][0], w[h][n][1]);
+              if constexpr (kTwice) mma<false>(o[k + i][n], a, rest[h][n][0], rest[h][n][1]);
+            }
           }
         }
-      }
-    } else {
+      } else {
 #pragma unroll
-      for (int k = 0; k < kSteps; ++k) {
-        uint32_t a[4];
-        const int row = (lane & 7) + ((lane >> 4) << 3), piece = 2 * k + ((lane >> 3) & 1);
-        ldmatrix_x4_trans(values + row * F::kRowBytes + place_of<F::kPieces>(row, piece) * 16, a);
+        for (int k = 0; k < kSteps; ++k) {
+          uint32_t a[4];
+          ldmatrix_x4_trans(at_piece(rows, 2 * k), a);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          mma<kMmaBf16>(o[k][n], a, w[n][0], w[n][1]);
-          mma<kMmaBf16>(o[k][n], a, rest[n][0], rest[n][1]);
+          for (int n = 0; n < NT; ++n) {
+            mma<kMmaBf16>(o[k][n], a, w[h][n][0], w[h][n][1]);
+            mma<kMmaBf16>(o[k][n], a, rest[h][n][0], rest[h][n][1]);
+          }
         }
       }
     }
   };
 
-  // ---- the end of an item, or of the share: the four warps' results are joined; whole items are finished, cut ones kept
-  constexpr int kMine = 8 * F::kJoinColumns / kThreads;
+  // ---- the end of an item, or of the share: the rings' results are joined; whole items are finished, cut ones kept
+  // A thread adds up kMine columns of every kJoinColumns, of one of the 8 RW rows that a tile of each row warp makes.
+  constexpr int kMine = 8 * RW * F::kJoinColumns / F::kThreads, kAcross = F::kJoinColumns / kMine;
   auto end_item = [&](bool whole, int slot) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -635,8 +748,8 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, d);
         if (g == 0) {
-          sm.top[warp][8 * n + 2 * c + j] = top[n][j];
-          sm.sum[warp][8 * n + 2 * c + j] = t;
+          sm.top[kw][row_of_mine + 8 * n + j] = top[n][j];
+          sm.sum[kw][row_of_mine + 8 * n + j] = t;
         }
       }
     __syncthreads();
@@ -645,27 +758,26 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
       float weight[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int r = 8 * n + 2 * c + j;
+        const int r = row_of_mine + 8 * n + j;
         float m = sm.top[0][r];
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm.top[w][r]);
+        for (int w = 1; w < F::kKeyWarps; ++w) m = fmaxf(m, sm.top[w][r]);
         weight[j] = top[n][j] == -INFINITY && m == -INFINITY ? 1.f : ex2_approx(top[n][j] - m);
         if constexpr (Q8) weight[j] *= unit_v[n][j];
       }
-      // What a thread adds up: columns `col` .. of every kJoinColumns, of row r
-      const int r = tid / 16, col = (tid % 16) * kMine, row = 8 * n + r;
+      const int r = tid / kAcross, col = (tid % kAcross) * kMine, their = r / 8, row = (their * NT + n) * 8 + r % 8;
       float m = sm.top[0][row], l = 0.f;
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm.top[w][row]);
+      for (int w = 1; w < F::kKeyWarps; ++w) m = fmaxf(m, sm.top[w][row]);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) l += sm.sum[w][row] * (sm.top[w][row] == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : ex2_approx(sm.top[w][row] - m));
+      for (int w = 0; w < F::kKeyWarps; ++w) l += sm.sum[w][row] * (sm.top[w][row] == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : ex2_approx(sm.top[w][row] - m));
       const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
       const bool there = sm.out[row] >= 0;
-      float* part = p.part + blockIdx.x * part_floats(8 * NT, DH) + (slot * 8 * NT + row) * (DH + 4);
-      if (there && tid % 16 == 0) {
+      float* part = p.part + blockIdx.x * part_floats(F::kRows, DH) + (slot * F::kRows + row) * (DH + 4);
+      if (there && tid % kAcross == 0) {
         if (whole) {
           if (p.lse && COMFUSE_IN_BOUNDS(sm.lse[row] < p.batch * p.tokens * p.heads * p.group, p.status)) p.lse[sm.lse[row]] = log_sum(m, l);
-        } else if (COMFUSE_IN_BOUNDS(row < 8 * NT && slot < 2, p.status)) {
+        } else if (COMFUSE_IN_BOUNDS(row < F::kRows && slot < 2, p.status)) {
           part[DH] = m;
           part[DH + 1] = l;
         }
@@ -677,7 +789,7 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
         for (int k = 0; k < F::kJoinColumns / 16; ++k)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            float* to = s_join + (warp * 8 + 2 * c + j) * F::kPitch + 16 * k;
+            float* to = s_join + ((kw * RW + rw) * 8 + 2 * c + j) * F::kPitch + 16 * k;
             const float* from = o[first / 16 + k][n];
             if constexpr (Q8) {
               *reinterpret_cast<float2*>(to + 2 * g) = make_float2(from[j] * weight[j], from[2 + j] * weight[j]);
@@ -691,9 +803,9 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
 #pragma unroll
         for (int j = 0; j < kMine; ++j) v[j] = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w)
+        for (int w = 0; w < F::kKeyWarps; ++w)
 #pragma unroll
-          for (int j = 0; j < kMine; ++j) v[j] += s_join[(w * 8 + r) * F::kPitch + col + j];
+          for (int j = 0; j < kMine; ++j) v[j] += s_join[(w * RW * 8 + r) * F::kPitch + col + j];
         const int at = first + col;
         if (!there) continue;
         if (whole) {
@@ -703,12 +815,16 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
             for (int j = 0; j < kMine; ++j) v[j] *= inv;
             Elem<DT>::pack(v, y);
             char* to = p.out + sm.out[row] + 2 * at;
-            if constexpr (kMine == 4) st_8(to, y);
+            if constexpr (kMine == 8) st_16(to, y);
+            else if constexpr (kMine == 4) st_8(to, y);
             else *reinterpret_cast<uint32_t*>(to) = y[0];
           }
-        } else if (COMFUSE_IN_BOUNDS(row < 8 * NT && slot < 2, p.status)) {
-          if constexpr (kMine == 4) st_16(part + at, reinterpret_cast<const uint32_t*>(v));
-          else st_8(part + at, reinterpret_cast<const uint32_t*>(v));
+        } else if (COMFUSE_IN_BOUNDS(row < F::kRows && slot < 2, p.status)) {
+          if constexpr (kMine == 2) st_8(part + at, reinterpret_cast<const uint32_t*>(v));
+          else {
+#pragma unroll
+            for (int j = 0; j < kMine; j += 4) st_16(part + at + j, reinterpret_cast<const uint32_t*>(v) + j);
+          }
         }
       }
     }
@@ -718,16 +834,16 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
   int b = at.b, hr = at.hr, unit = at.unit, stage = 0;
   bool from_start = unit == 0;
   int pieces = 0;
-  Sequence seq = sequence_of(p, b);
+  Sequence seq = sequence_of<F>(p, b);
   load_queries(b, hr);
   keep_queries(b, hr);
   __syncthreads();
   begin_item();
   for (int n = 0; n < count; ++n) {
     cp_async_wait<S - 2>();
-    __syncwarp();
+    ring_sync();
     fetch(stage == 0 ? S - 1 : stage - 1);
-    block(stage, seq, (seq.low & ~(kBlock - 1)) + unit * kUnit + warp * kBlock);
+    block(stage, seq, (seq.low & ~(F::kBlock - 1)) + unit * F::kUnit + kw * F::kBlock);
     stage = stage + 1 == S ? 0 : stage + 1;
     ++unit;
     if (unit == seq.units || n + 1 == count) {
@@ -741,7 +857,7 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
         ++pieces;
         from_start = true;
         unit = 0;
-        if (nb != b) seq = sequence_of(p, nb);
+        if (nb != b) seq = sequence_of<F>(p, nb);
         b = nb;
         hr = nhr;
         keep_queries(b, hr);
@@ -755,28 +871,30 @@ __global__ void __launch_bounds__(kThreads, Form<Q8, DH, NT>::kCtasPerSm) attent
 
 // ------------------------------------------------------------------------------------------------ joining
 // CTA (i, r): row r of the item that is cut behind share i, if that is its first cut.  Partial results are taken in the order of the shares.
-template <int DT, int DH, int NT>
-__global__ void __launch_bounds__(kThreads) join_kernel(const PagedAttentionParams p) {
+constexpr int kJoinThreads = 128;
+template <int DT, bool Q8, int DH, int NT, int RW>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttentionParams p) {
+  using F = Form<Q8, DH, NT, RW>;
   __shared__ Scan scan;
   __shared__ float s_weight[32];
   griddep_launch_dependents();
   Place at;
   // (the lengths are read in front of the wait: the kernel before this one signals behind its own)
-  const Line line = find(p, &scan, [](const Line& l) { return min(l.begin(blockIdx.x + 1), l.total - 1); }, &at);
+  const Line line = find<F, kJoinThreads>(p, &scan, [](const Line& l) { return min(l.begin(blockIdx.x + 1), l.total - 1); }, &at);
   griddep_wait();
-  const long long cut = line.begin(blockIdx.x + 1), item = cut - at.unit;  // the item's first unit
+  const unsigned cut = line.begin(blockIdx.x + 1), item = cut - at.unit;  // the item's first unit
   if (cut >= line.total || at.unit == 0 || item < line.begin(blockIdx.x)) return;
-  const int row0 = (at.hr % p.row_blocks) * 8 * NT, row = row0 + blockIdx.y;
-  if (blockIdx.y >= 8 * NT || row >= p.rows) return;
-  const int units = sequence_of(p, at.b).units;
-  const long long last = line.owner(item + units - 1);
+  const int row0 = (at.hr % p.row_blocks) * F::kRows, row = row0 + blockIdx.y;
+  if (blockIdx.y >= F::kRows || row >= p.rows) return;
+  const int units = sequence_of<F>(p, at.b).units;
+  const unsigned last = line.owner(item + units - 1);
   const int slot = item == line.begin(blockIdx.x) ? 0 : 1;
-  const float* first_part = p.part + blockIdx.x * part_floats(8 * NT, DH) + (slot * 8 * NT + blockIdx.y) * (DH + 4);
-  const float* next_part = p.part + (blockIdx.x + 1) * part_floats(8 * NT, DH) + blockIdx.y * (DH + 4);
+  const float* first_part = p.part + blockIdx.x * part_floats(F::kRows, DH) + (slot * F::kRows + blockIdx.y) * (DH + 4);
+  const float* next_part = p.part + (blockIdx.x + 1) * part_floats(F::kRows, DH) + blockIdx.y * (DH + 4);
   const int n = static_cast<int>(last - blockIdx.x) + 1;
-  auto part = [&](int i) { return i == 0 ? first_part : next_part + (i - 1) * part_floats(8 * NT, DH); };
+  auto part = [&](int i) { return i == 0 ? first_part : next_part + (i - 1) * part_floats(F::kRows, DH); };
 
-  constexpr int kMine = DH > kThreads ? DH / kThreads : 1;
+  constexpr int kMine = DH > kJoinThreads ? DH / kJoinThreads : 1;
   float m = -INFINITY, l = 0.f, v[kMine];
 #pragma unroll
   for (int j = 0; j < kMine; ++j) v[j] = 0.f;
@@ -800,7 +918,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const PagedAttentionPara
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kMine; ++j) {
-      const int d = threadIdx.x + j * kThreads;
+      const int d = threadIdx.x + j * kJoinThreads;
       if (d < DH) {
         float a = v[j] * old;
 #pragma unroll 8
@@ -814,7 +932,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const PagedAttentionPara
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int j = 0; j < kMine; ++j) {
-    const int d = threadIdx.x + j * kThreads;
+    const int d = threadIdx.x + j * kJoinThreads;
     if (d < p.D && COMFUSE_IN_BOUNDS(row < p.rows && at.b < p.batch, p.status)) Elem<DT>::put(out, d, v[j] * inv);
   }
   if (p.lse && threadIdx.x == 0 && COMFUSE_IN_BOUNDS(at.b < p.batch && token < p.tokens, p.status))
@@ -822,23 +940,23 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const PagedAttentionPara
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-template <int DT, bool Q8, int DH, int NT>
+template <int DT, bool Q8, int DH, int NT, int RW>
 cudaError_t launch_instance(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
-  using F = Form<Q8, DH, NT>;
+  using F = Form<Q8, DH, NT, RW>;
   static std::atomic<unsigned long long> ready{0};  // devices on which the kernel may take its shared memory
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
   const unsigned long long bit = 1ull << (device & 63);
   if (device > 63 || !(ready.load(std::memory_order_relaxed) & bit)) {
-    e = cudaFuncSetAttribute(attention_kernel<DT, Q8, DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kBytes);
+    e = cudaFuncSetAttribute(attention_kernel<DT, Q8, DH, NT, RW>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kBytes);
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
   cfg.gridDim = dim3(static_cast<unsigned>(plan.ctas), 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.blockDim = dim3(F::kThreads, 1, 1);
   cfg.dynamicSmemBytes = F::kBytes;
   cfg.stream = stream;
   if (programmatic_launch_enabled()) {
@@ -848,23 +966,50 @@ cudaError_t launch_instance(const PagedAttentionPlan& plan, const PagedAttention
     cfg.numAttrs = 1;
   }
   if (verbose_enabled())
-    std::fprintf(stderr, "comfuse: paged_attention dtype=%d quantized=%d D<=%d row tiles=%d row blocks=%d CTAs=%d stages=%d joined=%d\n", DT, Q8, DH, NT, p.row_blocks, plan.ctas, F::kStages,
+    std::fprintf(stderr, "comfuse: paged_attention dtype=%d quantized=%d D<=%d row tiles=%d x %d row blocks=%d CTAs=%d stages=%d joined=%d\n", DT, Q8, DH, NT, RW, p.row_blocks, plan.ctas, F::kStages,
                  plan.joined);
   count_launch();
-  e = cudaLaunchKernelEx(&cfg, attention_kernel<DT, Q8, DH, NT>, p);
+  e = cudaLaunchKernelEx(&cfg, attention_kernel<DT, Q8, DH, NT, RW>, p);
   if (e != cudaSuccess || !plan.joined) return e;
-  cfg.gridDim = dim3(static_cast<unsigned>(plan.ctas - 1), static_cast<unsigned>(p.rows < 8 * NT ? p.rows : 8 * NT), 1);
+  cfg.gridDim = dim3(static_cast<unsigned>(plan.ctas - 1), static_cast<unsigned>(p.rows < F::kRows ? p.rows : F::kRows), 1);
+  cfg.blockDim = dim3(kJoinThreads, 1, 1);
   cfg.dynamicSmemBytes = 0;
   count_launch();
-  return cudaLaunchKernelEx(&cfg, join_kernel<DT, DH, NT>, p);
+  return cudaLaunchKernelEx(&cfg, join_kernel<DT, Q8, DH, NT, RW>, p);
 }
 
+template <int DT, bool Q8, int DH>
+cudaError_t launch_rows(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
+  constexpr int kMost = DH == 256 ? 2 : 4;  // tiles of a warp
+  if (plan.rows == 8) return launch_instance<DT, Q8, DH, 1, 1>(plan, p, stream);
+  if (plan.rows == 16) return launch_instance<DT, Q8, DH, 2, 1>(plan, p, stream);
+  if (plan.rows == 32) return launch_instance<DT, Q8, DH, 2, 2>(plan, p, stream);
+  return launch_instance<DT, Q8, DH, kMost, 8 / kMost>(plan, p, stream);
+}
 template <int DT, bool Q8>
 cudaError_t launch_type(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
-  const int nt = plan.row_tiles;
-  if (p.D <= 64) return nt == 1 ? launch_instance<DT, Q8, 64, 1>(plan, p, stream) : nt == 2 ? launch_instance<DT, Q8, 64, 2>(plan, p, stream) : launch_instance<DT, Q8, 64, 4>(plan, p, stream);
-  if (p.D <= 128) return nt == 1 ? launch_instance<DT, Q8, 128, 1>(plan, p, stream) : nt == 2 ? launch_instance<DT, Q8, 128, 2>(plan, p, stream) : launch_instance<DT, Q8, 128, 4>(plan, p, stream);
-  return nt == 1 ? launch_instance<DT, Q8, 256, 1>(plan, p, stream) : launch_instance<DT, Q8, 256, 2>(plan, p, stream);
+  if (p.D <= 64) return launch_rows<DT, Q8, 64>(plan, p, stream);
+  if (p.D <= 128) return launch_rows<DT, Q8, 128>(plan, p, stream);
+  return launch_rows<DT, Q8, 256>(plan, p, stream);
+}
+
+// What a plan needs to know of the instance that runs it.
+struct FormFacts {
+  int unit, block, ctas_per_sm;
+};
+template <bool Q8, int DH, int NT, int RW>
+constexpr FormFacts facts_of() {
+  using F = Form<Q8, DH, NT, RW>;
+  return {F::kUnit, F::kBlock, F::kCtasPerSm};
+}
+template <bool Q8, int DH>
+FormFacts facts(int rows) {
+  constexpr int kMost = DH == 256 ? 2 : 4;
+  return rows == 8 ? facts_of<Q8, DH, 1, 1>() : rows == 16 ? facts_of<Q8, DH, 2, 1>() : rows == 32 ? facts_of<Q8, DH, 2, 2>() : facts_of<Q8, DH, kMost, 8 / kMost>();
+}
+template <bool Q8>
+FormFacts facts(int D, int rows) {
+  return D <= 64 ? facts<Q8, 64>(rows) : D <= 128 ? facts<Q8, 128>(rows) : facts<Q8, 256>(rows);
 }
 
 }  // namespace
