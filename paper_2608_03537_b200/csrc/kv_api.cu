@@ -300,6 +300,8 @@ comfuse_status_t comfuse_paged_attention(const comfuse_paged_attention_desc_t* d
   p.alpha = d.alpha; p.softcap = d.softcap;
   p.part = static_cast<float*>(workspace);
   p.ctas = plan.ctas;
+  p.groups = Divisor(p.group);
+  p.shares = Divisor(plan.ctas);
   p.status = dev->status_word;
   return launched(launch_paged_attention(cache->dtype, cache->quantized != 0, plan, p, static_cast<cudaStream_t>(cuda_stream)));
 }

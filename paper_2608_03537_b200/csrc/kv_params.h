@@ -70,7 +70,7 @@ struct PagedAttentionParams {
   int rows;                             // tokens * group: the queries of a sequence that read the same keys
   int row_blocks;                       // CTAs' worth of them
   int pages, max_length, window;
-  Divisor page_size;
+  Divisor page_size, groups, shares;    // groups: divides by `group`, shares: by `ctas`
   const char* q;
   char* out;
   long long q_batch, q_token, q_head, out_batch, out_token, out_head;

@@ -87,58 +87,48 @@ __device__ __forceinline__ Sequence sequence_of(const PagedAttentionParams& p, i
   s.units = max(1u, static_cast<unsigned>(s.length - (s.low & ~(F::kBlock - 1)) + F::kUnit - 1) / F::kUnit);  // (an empty sequence has a unit too: its rows are written)
   return s;
 }
+// By each warp on its own, 32 sequences at a time.  The line; then where a unit lies, or which is the first of an item.
+template <typename F>
+__device__ __forceinline__ Line line_of(const PagedAttentionParams& p, int lane, unsigned* mine) {
+  unsigned total = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    const unsigned n = b0 + lane < p.batch ? sequence_of<F>(p, b0 + lane).units : 0u;
+    if (b0 == 0) *mine = n;  // (most calls have no more)
+    total += n;
+  }
+  Line line;
+  line.total = __reduce_add_sync(0xFFFFFFFFu, total) * static_cast<unsigned>(p.heads * p.row_blocks);
+  line.share = p.shares.of(line.total);
+  line.longer = line.total - line.share * p.ctas;
+  return line;
+}
 struct Place {
   int b, hr, unit;
 };
-struct Scan {
-  unsigned warp_sum[16];
-  Place place;
-};
-// By all threads of a CTA: the line, and where the unit that `unit_of` names lies.
-template <typename F, int THREADS, typename UnitOf>
-__device__ __forceinline__ Line find(const PagedAttentionParams& p, Scan* s, UnitOf unit_of, Place* place) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (p.batch + THREADS - 1) / THREADS;
+template <typename F>
+__device__ __forceinline__ Place place_of_unit(const PagedAttentionParams& p, int lane, unsigned mine, unsigned unit) {
   const unsigned hr = p.heads * p.row_blocks;
-  const int b0 = min(tid * per, p.batch), b1 = min(b0 + per, p.batch);
-  unsigned mine = 0;
-  for (int b = b0; b < b1; ++b) mine += sequence_of<F>(p, b).units;
-  unsigned upto = mine;
+  unsigned before = 0;  // units of the sequences in front, of one item each
+  for (int b0 = 0;; b0 += 32) {
+    const unsigned n = b0 == 0 ? mine : b0 + lane < p.batch ? sequence_of<F>(p, b0 + lane).units : 0u;
+    unsigned upto = n;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-    if (lane >= o) upto += v;
-  }
-  if (lane == 31) s->warp_sum[warp] = upto;
-  __syncthreads();
-  unsigned before = 0, total = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) {
-    if (w < warp) before += s->warp_sum[w];
-    total += s->warp_sum[w];
-  }
-  before += upto - mine;
-  Line line;
-  line.total = total * hr;
-  line.share = line.total / p.ctas;
-  line.longer = line.total - line.share * p.ctas;
-  const unsigned unit = unit_of(line);
-  if (unit >= before * hr && unit < (before + mine) * hr) {
-    unsigned rest = unit - before * hr;
-    for (int b = b0; b < b1; ++b) {
-      const unsigned n = sequence_of<F>(p, b).units;
-      if (rest < n * hr) {
-        s->place.b = b;
-        s->place.hr = rest / n;
-        s->place.unit = rest - s->place.hr * n;
-        break;
-      }
-      rest -= n * hr;
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      if (lane >= o) upto += v;
     }
+    const unsigned found = __ballot_sync(0xFFFFFFFFu, unit < (before + upto) * hr);
+    if (found || b0 + 32 >= p.batch) {
+      const int i = found ? __ffs(found) - 1 : 0;
+      const unsigned units = __shfl_sync(0xFFFFFFFFu, n, i), rest = unit - (before + __shfl_sync(0xFFFFFFFFu, upto, i) - units) * hr;
+      Place at;
+      at.b = b0 + i;
+      at.hr = rest / units;
+      at.unit = rest - at.hr * units;
+      return at;
+    }
+    before += __shfl_sync(0xFFFFFFFFu, upto, 31);
   }
-  __syncthreads();
-  *place = s->place;
-  return line;
 }
 
 // ------------------------------------------------------------------------------------------------ instructions
@@ -231,7 +221,6 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
     int token[F::kRows];                                           // its new token
     int lse[F::kRows];
     unsigned valid[F::kKeyWarps][8];                               // of the blocks in the ring: positions that are there
-    Scan scan;
   };
   static_assert(sizeof(Small) <= F::kSmall, "room for what is small");
   Small& sm = *reinterpret_cast<Small*>(reinterpret_cast<char*>(s_query) + F::kQuery);
@@ -242,11 +231,31 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   griddep_wait();
   griddep_launch_dependents();  // behind the wait: the joining kernel reads the lengths before its own
 
-  Place at;
-  const Line line = find<F, F::kThreads>(p, &sm.scan, [](const Line& l) { return min(l.begin(blockIdx.x), l.total - 1); }, &at);
-  const int count = static_cast<int>(line.begin(blockIdx.x + 1) - line.begin(blockIdx.x));
+  unsigned lane_units;
+  const Line line = line_of<F>(p, lane, &lane_units);
+  const unsigned first_unit = line.begin(blockIdx.x);
+  const int count = static_cast<int>(line.begin(blockIdx.x + 1) - first_unit);
   if (count <= 0) return;
+  const Place at = place_of_unit<F>(p, lane, lane_units, first_unit);
   const int HR = p.heads * p.row_blocks;
+
+  // ---- an item's queries: loaded by pieces of 8 elements, kept in shared memory as the product's operands, eight bytes a lane for each step and tile
+  constexpr int kQueryPieces = DH / 8, kQueryLoads = (F::kRows * kQueryPieces + F::kThreads - 1) / F::kThreads;
+  constexpr int kQuerySteps = Q8 ? DH / 32 : DH / 16, kPlane = kQuerySteps * NT * RW * 64;  // words (of a digit)
+  uint32_t q_raw[kQueryLoads][4];
+  auto load_queries = [&](int b, int hr) {
+    const int head = p.row_blocks == 1 ? hr : hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows;
+#pragma unroll
+    for (int i = 0; i < kQueryLoads; ++i) {
+      const int n = tid + i * F::kThreads, r = n / kQueryPieces, piece = n % kQueryPieces, row = row0 + r;
+      q_raw[i][0] = q_raw[i][1] = q_raw[i][2] = q_raw[i][3] = 0u;
+      if (r < F::kRows && row < p.rows && piece * 8 < p.D) {
+        const int token = p.groups.of(row), h = head * p.group + row - token * p.group;
+        ld_16(p.q + b * p.q_batch + token * p.q_token + h * p.q_head + piece * 16, q_raw[i]);
+      }
+    }
+  };
+  load_queries(at.b, at.hr);
 
   char* ring = smem + kw * S * F::kStage;
   const uint32_t ring_u32 = smem_u32(ring);
@@ -268,6 +277,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   const bool whole_pages = p.page_size.d % F::kBlock == 0;  // a block lies in one page
   int f_b = at.b, f_hr = at.hr, f_unit = at.unit, f_left = count, f_base, f_page, f_line;
   Sequence f_seq = sequence_of<F>(p, f_b);
+  const Sequence first_seq = f_seq;
   const int* f_table = p.table + f_b * p.table_stride;
   const char *f_k, *f_v;  // the head's rows, from this lane's piece on
   const float *f_ks, *f_vs;
@@ -352,26 +362,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
     }
     cp_async_commit();
   };
-  for (int s = 0; s < S - 1; ++s) fetch(s);
-
-  // ---- an item's queries: loaded by pieces of 8 elements, kept in shared memory as the product's operands, eight bytes a lane for each step and tile
-  constexpr int kQueryPieces = DH / 8, kQueryLoads = (F::kRows * kQueryPieces + F::kThreads - 1) / F::kThreads;
-  constexpr int kQuerySteps = Q8 ? DH / 32 : DH / 16, kPlane = kQuerySteps * NT * RW * 64;  // words (of a digit)
-  uint32_t q_raw[kQueryLoads][4];
-  auto load_queries = [&](int b, int hr) {
-    const int head = hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows;
-#pragma unroll
-    for (int i = 0; i < kQueryLoads; ++i) {
-      const int n = tid + i * F::kThreads, r = n / kQueryPieces, piece = n % kQueryPieces, row = row0 + r;
-      q_raw[i][0] = q_raw[i][1] = q_raw[i][2] = q_raw[i][3] = 0u;
-      if (r < F::kRows && row < p.rows && piece * 8 < p.D) {
-        const int token = row / p.group, h = head * p.group + row - token * p.group;
-        ld_16(p.q + b * p.q_batch + token * p.q_token + h * p.q_head + piece * 16, q_raw[i]);
-      }
-    }
-  };
   auto keep_queries = [&](int b, int hr) {
-    const int head = hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows;
+    const int head = p.row_blocks == 1 ? hr : hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows;
 #pragma unroll
     for (int i = 0; i < kQueryLoads; ++i) {
       const int n = tid + i * F::kThreads, r = n / kQueryPieces, piece = n % kQueryPieces;
@@ -420,19 +412,24 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
       }
     }
     if (tid < F::kRows) {
-      const int row = row0 + tid, token = min(row / p.group, p.tokens - 1), h = head * p.group + row % p.group;
+      const int row = row0 + tid, turn = p.groups.of(row), token = min(turn, p.tokens - 1), h = head * p.group + row - turn * p.group;
       sm.token[tid] = token;
       sm.slope[tid] = p.slopes && row < p.rows ? p.slopes[h] * kLog2e : 0.f;
       sm.out[tid] = row < p.rows ? b * p.out_batch + token * p.out_token + h * p.out_head : -1;
       sm.lse[tid] = row < p.rows ? (b * p.tokens + token) * p.heads * p.group + h : 0;
     }
   };
-  const int tile0 = rw * NT, row_of_mine = 8 * tile0 + 2 * c;  // this warp's tiles; columns 2c, 2c + 1 of the first are this lane's
+  // Tile n of a warp is tile n RW + rw of the CTA, so that few rows are spread over its warps; columns 2c, 2c + 1 are this lane's.  Tiles behind the rows are left out.
+  const int row_of_mine = 8 * rw + 2 * c;
+  int tiles = NT;
+  auto has = [&](int n) { return NT * RW == 1 || n < tiles; };
   auto query_operand = [&](int digit, int step, int n) {
-    return *reinterpret_cast<const uint2*>(s_query + digit * kPlane + (step * NT * RW + tile0 + n) * 64 + lane * 2);
+    return *reinterpret_cast<const uint2*>(s_query + digit * kPlane + (step * NT * RW + n * RW + rw) * 64 + lane * 2);
   };
   constexpr bool kHold = NT == 1 && DH <= 128;  // operands of the queries stay in registers
   uint2 q_held[kHold ? (Q8 ? kDigits : 1) : 1][kHold ? kQuerySteps : 1];
+
+  int b = at.b, hr = at.hr, unit = at.unit;  // where the blocks are
 
   // ---- a warp's running state
   float o[kSteps][NT][4], top[NT][2], sum[NT][2];
@@ -442,6 +439,10 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   float factor[NT][2];  // of a score
   const SoftcapLog2 cap(p.alpha, p.softcap > 0.f ? p.softcap : 1.f);
   auto begin_item = [&]() {
+    if constexpr (NT * RW > 1) {
+      const int here = p.row_blocks == 1 ? p.rows : min(F::kRows, p.rows - (hr - hr / p.row_blocks * p.row_blocks) * F::kRows);
+      tiles = max(0, min(NT, (here - 8 * rw + 8 * RW - 1) / (8 * RW)));
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       top[n][0] = top[n][1] = -INFINITY;
@@ -452,7 +453,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         factor[n][j] = p.softcap > 0.f ? 1.f : p.alpha * kLog2e;
-        if constexpr (Q8) factor[n][j] *= sm.factor[row_of_mine + 8 * n + j];
+        if constexpr (Q8) factor[n][j] *= sm.factor[row_of_mine + 8 * RW * n + j];
       }
     }
     if constexpr (kHold) {
@@ -476,8 +477,61 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   auto block = [&](int stage, const Sequence& seq, int base) {
     const unsigned valid = sm.valid[kw][stage];
     if (!valid) return;
+    const int first = seq.length - p.tokens;  // the first new token's position
+    constexpr unsigned kAll = F::kBlock == 32 ? 0xFFFFFFFFu : 0xFFFFu;
+    const bool all = valid == kAll && base + F::kBlock - 1 <= first && (p.window <= 0 || base > seq.length - 1 - p.window);
+    if constexpr (!Q8) {
+      if (!all && p.tokens > 1) {
+        // Some rows see a position and others do not: a value that is not finite must not reach the others as 0 * inf.  Such values are added to the rows that see them, and
+        // are zeros for the product.
+        const char* block_v = ring + stage * F::kStage + F::kSide;
+        bool odd = false;
+        for (int i = lane; i < F::kSide / 16; i += 32) {
+          const uint4 x = *reinterpret_cast<const uint4*>(block_v + i * 16);
+          const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+          constexpr uint32_t e = kBf16 ? 0x7F80u : 0x7C00u;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) odd |= (y[j] & e) == e || (y[j] >> 16 & e) == e;
+        }
+        // (all warps of a ring come here, find the same, and clear it together)
+        if (__any_sync(0xFFFFFFFFu, odd)) {
+          for (int k = 0; k < F::kBlock; ++k) {
+            const int pos = base + k - first;
+#pragma unroll
+            for (int d = 0; d < kSteps; ++d)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int e = 16 * d + 8 * h + g;
+                const float v = Elem<DT>::get(block_v + k * F::kRowBytes + place_of<F::kPieces>(k, e >> 3) * 16 + (e & 7) * 2, 0);
+                if (!isfinite(v)) {
+#pragma unroll
+                  for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                      const int gap = pos - sm.token[row_of_mine + 8 * RW * n + j];
+                      if (gap <= 0 && (p.window <= 0 || gap > -p.window)) o[d][n][2 * h + j] += v;
+                    }
+                }
+              }
+          }
+          ring_sync();
+          for (int i = lane; i < F::kSide / 2; i += 32) {
+            uint16_t* at_v = reinterpret_cast<uint16_t*>(ring + stage * F::kStage + F::kSide) + i;
+            if (!isfinite(Elem<DT>::get(at_v, 0))) *at_v = 0;
+          }
+          ring_sync();
+        }
+      }
+    }
+    if (NT * RW > 1 && tiles == 0) return;
     const uint32_t keys = ring_u32 + stage * F::kStage + k_lane, values = ring_u32 + stage * F::kStage + v_lane;
     float s[G][NT][4];
+    if constexpr (NT > 1) {
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[h][n][0] = s[h][n][1] = s[h][n][2] = s[h][n][3] = 0.f;
+    }
     if constexpr (Q8) {
       uint32_t a[kQuerySteps][G][4];
 #pragma unroll
@@ -486,6 +540,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         for (int h = 0; h < G; ++h) ldmatrix_x4(at_piece(keys + h * 16 * F::kRowBytes, 2 * k), a[k][h]);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
+        if (!has(n)) continue;
         int sd[kDigits][G][4];
 #pragma unroll
         for (int d = 0; d < kDigits; ++d)
@@ -517,6 +572,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         for (int h = 0; h < G; ++h) ldmatrix_x4(at_piece(keys + h * 16 * F::kRowBytes, 2 * k), a[h]);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+          if (!has(n)) continue;
           const uint2 b = query(0, k, n);
 #pragma unroll
           for (int h = 0; h < G; ++h) mma<kMmaBf16>(s[h][n], a[h], b.x, b.y);
@@ -534,9 +590,6 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
           vs[h][i] = scales[F::kBlock + 16 * h + 8 * i + g];
         }
     }
-    const int first = seq.length - p.tokens;  // the first new token's position
-    constexpr unsigned kAll = F::kBlock == 32 ? 0xFFFFFFFFu : 0xFFFFu;
-    const bool all = valid == kAll && base + F::kBlock - 1 <= first && (p.window <= 0 || base > seq.length - 1 - p.window);
     // s: scores in the log2 domain less the running maximum (0 where there is none yet)
     float ref[NT][2], limit[NT][2];
 #pragma unroll
@@ -554,7 +607,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int j = i & 1, r = row_of_mine + 8 * n + j, k = 16 * h + g + 8 * (i >> 1);
+            const int j = i & 1, r = row_of_mine + 8 * RW * n + j, k = 16 * h + g + 8 * (i >> 1);
             float v = s[h][n][i] * factor[n][j];
             if constexpr (Q8) v *= ks[h][i >> 1];
             if (p.softcap > 0.f) v = cap(v);
@@ -659,49 +712,6 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         }
       }
     }
-    if constexpr (!Q8) {
-      if (!all && p.tokens > 1) {
-        // Some rows see a position and others do not: a value that is not finite must not reach the others as 0 * inf.  Such values are added to the rows that see them, and
-        // are zeros for the product.
-        const char* block_v = ring + stage * F::kStage + F::kSide;
-        bool odd = false;
-        for (int i = lane; i < F::kSide / 16; i += 32) {
-          const uint4 x = *reinterpret_cast<const uint4*>(block_v + i * 16);
-          const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-          constexpr uint32_t e = kBf16 ? 0x7F80u : 0x7C00u;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) odd |= (y[j] & e) == e || (y[j] >> 16 & e) == e;
-        }
-        // (the warps of a ring find the same, and clear it together)
-        if (__any_sync(0xFFFFFFFFu, odd)) {
-          for (int k = 0; k < F::kBlock; ++k) {
-            const int pos = base + k - first;
-#pragma unroll
-            for (int d = 0; d < kSteps; ++d)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int e = 16 * d + 8 * h + g;
-                const float v = Elem<DT>::get(block_v + k * F::kRowBytes + place_of<F::kPieces>(k, e >> 3) * 16 + (e & 7) * 2, 0);
-                if (!isfinite(v)) {
-#pragma unroll
-                  for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                      const int gap = pos - sm.token[row_of_mine + 8 * n + j];
-                      if (gap <= 0 && (p.window <= 0 || gap > -p.window)) o[d][n][2 * h + j] += v;
-                    }
-                }
-              }
-          }
-          ring_sync();
-          for (int i = lane; i < F::kSide / 2; i += 32) {
-            uint16_t* at_v = reinterpret_cast<uint16_t*>(ring + stage * F::kStage + F::kSide) + i;
-            if (!isfinite(Elem<DT>::get(at_v, 0))) *at_v = 0;
-          }
-          ring_sync();
-        }
-      }
-    }
 #pragma unroll
     for (int h = 0; h < G; ++h) {
       const uint32_t rows = values + h * 16 * F::kRowBytes;
@@ -716,6 +726,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
             const uint32_t a[4] = {codes_f16(x, 0x4240), codes_f16(x, 0x4341), codes_f16(y, 0x4240), codes_f16(y, 0x4341)};
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
+              if (!has(n)) continue;
               mma<false>(o[k + i][n], a, w[h][n][0], w[h][n][1]);
               if constexpr (kTwice) mma<false>(o[k + i][n], a, rest[h][n][0], rest[h][n][1]);
             }
@@ -728,6 +739,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
           ldmatrix_x4_trans(at_piece(rows, 2 * k), a);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
+            if (!has(n)) continue;
             mma<kMmaBf16>(o[k][n], a, w[h][n][0], w[h][n][1]);
             mma<kMmaBf16>(o[k][n], a, rest[h][n][0], rest[h][n][1]);
           }
@@ -748,8 +760,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, d);
         if (g == 0) {
-          sm.top[kw][row_of_mine + 8 * n + j] = top[n][j];
-          sm.sum[kw][row_of_mine + 8 * n + j] = t;
+          sm.top[kw][row_of_mine + 8 * RW * n + j] = top[n][j];
+          sm.sum[kw][row_of_mine + 8 * RW * n + j] = t;
         }
       }
     __syncthreads();
@@ -758,14 +770,14 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
       float weight[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int r = row_of_mine + 8 * n + j;
+        const int r = row_of_mine + 8 * RW * n + j;
         float m = sm.top[0][r];
 #pragma unroll
         for (int w = 1; w < F::kKeyWarps; ++w) m = fmaxf(m, sm.top[w][r]);
         weight[j] = top[n][j] == -INFINITY && m == -INFINITY ? 1.f : ex2_approx(top[n][j] - m);
         if constexpr (Q8) weight[j] *= unit_v[n][j];
       }
-      const int r = tid / kAcross, col = (tid % kAcross) * kMine, their = r / 8, row = (their * NT + n) * 8 + r % 8;
+      const int r = tid / kAcross, col = (tid % kAcross) * kMine, row = n * 8 * RW + r;
       float m = sm.top[0][row], l = 0.f;
 #pragma unroll
       for (int w = 1; w < F::kKeyWarps; ++w) m = fmaxf(m, sm.top[w][row]);
@@ -830,19 +842,24 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
     }
   };
 
-  // ---- the share
-  int b = at.b, hr = at.hr, unit = at.unit, stage = 0;
-  bool from_start = unit == 0;
+  // ---- the share: S - 1 rounds that only fetch, then a block each
+  int stage = 0;
+  bool from_start = unit == 0, fresh = true;
   int pieces = 0;
-  Sequence seq = sequence_of<F>(p, b);
-  load_queries(b, hr);
-  keep_queries(b, hr);
-  __syncthreads();
-  begin_item();
-  for (int n = 0; n < count; ++n) {
-    cp_async_wait<S - 2>();
-    ring_sync();
-    fetch(stage == 0 ? S - 1 : stage - 1);
+  Sequence seq = first_seq;
+  for (int n = 1 - S; n < count; ++n) {
+    if (n >= 0) {
+      if (fresh) {
+        keep_queries(b, hr);
+        __syncthreads();
+        begin_item();
+        fresh = false;
+      }
+      cp_async_wait<S - 2>();
+      ring_sync();
+    }
+    fetch(n < 0 ? n + S - 1 : stage == 0 ? S - 1 : stage - 1);
+    if (n < 0) continue;
     block(stage, seq, (seq.low & ~(F::kBlock - 1)) + unit * F::kUnit + kw * F::kBlock);
     stage = stage + 1 == S ? 0 : stage + 1;
     ++unit;
@@ -855,14 +872,11 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
       if (more) {
         __syncthreads();  // everyone has read the last item's rows
         ++pieces;
-        from_start = true;
+        fresh = from_start = true;
         unit = 0;
         if (nb != b) seq = sequence_of<F>(p, nb);
         b = nb;
         hr = nhr;
-        keep_queries(b, hr);
-        __syncthreads();
-        begin_item();
       }
     }
   }
@@ -870,72 +884,93 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
 }
 
 // ------------------------------------------------------------------------------------------------ joining
-// CTA (i, r): row r of the item that is cut behind share i, if that is its first cut.  Partial results are taken in the order of the shares.
-constexpr int kJoinThreads = 128;
+// CTA (i, r): row r of item i (few items), or of the item that is cut behind share i, if that is its first cut.  Partial results are added up in the order of the shares.
+constexpr int kJoinThreads = 256;
 template <int DT, bool Q8, int DH, int NT, int RW>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttentionParams p) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttentionParams p, const int by_item) {
   using F = Form<Q8, DH, NT, RW>;
-  __shared__ Scan scan;
-  __shared__ float s_weight[32];
+  constexpr int kAcross = DH / 4, kStripes = kJoinThreads / kAcross;  // threads of a row, four columns each; every kStripes-th part is one stripe's
+  constexpr int kMost = 296;                                          // parts
+  __shared__ float s_weight[kMost];
+  __shared__ float4 s_sum[kStripes][kAcross];
   griddep_launch_dependents();
-  Place at;
+  const int tid = threadIdx.x, lane = tid & 31;
   // (the lengths are read in front of the wait: the kernel before this one signals behind its own)
-  const Line line = find<F, kJoinThreads>(p, &scan, [](const Line& l) { return min(l.begin(blockIdx.x + 1), l.total - 1); }, &at);
+  unsigned lane_units;
+  const Line line = line_of<F>(p, lane, &lane_units);
+  Place at;
+  unsigned item, first, units;  // the item's first unit, its first share
+  bool cut;
+  if (by_item) {
+    const int HR = p.heads * p.row_blocks;
+    at.b = blockIdx.x / HR;
+    at.hr = blockIdx.x - at.b * HR;
+    unsigned before = 0;
+    for (int b0 = 0; b0 < at.b; b0 += 32) before += b0 + lane < at.b ? (b0 == 0 ? lane_units : sequence_of<F>(p, b0 + lane).units) : 0u;
+    units = sequence_of<F>(p, at.b).units;
+    item = __reduce_add_sync(0xFFFFFFFFu, before) * HR + at.hr * units;
+    first = line.owner(item);
+    cut = line.owner(item + units - 1) != first;
+  } else {
+    const unsigned behind = line.begin(blockIdx.x + 1);
+    at = place_of_unit<F>(p, lane, lane_units, min(behind, line.total - 1));
+    units = sequence_of<F>(p, at.b).units;
+    item = behind - at.unit;
+    first = blockIdx.x;
+    cut = behind < line.total && at.unit > 0 && item >= line.begin(blockIdx.x);
+  }
   griddep_wait();
-  const unsigned cut = line.begin(blockIdx.x + 1), item = cut - at.unit;  // the item's first unit
-  if (cut >= line.total || at.unit == 0 || item < line.begin(blockIdx.x)) return;
-  const int row0 = (at.hr % p.row_blocks) * F::kRows, row = row0 + blockIdx.y;
-  if (blockIdx.y >= F::kRows || row >= p.rows) return;
-  const int units = sequence_of<F>(p, at.b).units;
-  const unsigned last = line.owner(item + units - 1);
-  const int slot = item == line.begin(blockIdx.x) ? 0 : 1;
-  const float* first_part = p.part + blockIdx.x * part_floats(F::kRows, DH) + (slot * F::kRows + blockIdx.y) * (DH + 4);
-  const float* next_part = p.part + (blockIdx.x + 1) * part_floats(F::kRows, DH) + blockIdx.y * (DH + 4);
-  const int n = static_cast<int>(last - blockIdx.x) + 1;
+  const int r = blockIdx.y, row = (at.hr % p.row_blocks) * F::kRows + r;
+  if (!cut || row >= p.rows) return;
+  const int n = static_cast<int>(line.owner(item + units - 1) - first) + 1;  // parts
+  const int slot = item == line.begin(first) ? 0 : 1;
+  const float* first_part = p.part + first * part_floats(F::kRows, DH) + (slot * F::kRows + r) * (DH + 4);
+  const float* next_part = p.part + (first + 1) * part_floats(F::kRows, DH) + r * (DH + 4);
   auto part = [&](int i) { return i == 0 ? first_part : next_part + (i - 1) * part_floats(F::kRows, DH); };
 
-  constexpr int kMine = DH > kJoinThreads ? DH / kJoinThreads : 1;
-  float m = -INFINITY, l = 0.f, v[kMine];
+  // the first parts of this thread's stripe are on their way while the weights are worked out
+  constexpr int kEarly = 4;
+  const int stripe = tid / kAcross, col = (tid % kAcross) * 4;
+  float4 early[kEarly];
 #pragma unroll
-  for (int j = 0; j < kMine; ++j) v[j] = 0.f;
-  for (int i0 = 0; i0 < n; i0 += 32) {  // 32 parts at a time: their weights first
-    const int k = min(32, n - i0);
-    const int lane = threadIdx.x & 31;
-    const float pm = lane < k ? part(i0 + lane)[DH] : -INFINITY, pl = lane < k ? part(i0 + lane)[DH + 1] : 0.f;
-    float most = pm;
+  for (int i = 0; i < kEarly; ++i) early[i] = stripe + i * kStripes < n ? *reinterpret_cast<const float4*>(part(stripe + i * kStripes) + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+  float m = -INFINITY, l = 0.f;
+  for (int i = lane; i < n; i += 32) m = fmaxf(m, part(i)[DH]);
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
-    most = fmaxf(most, m);
-    const float old = m == -INFINITY ? (most == -INFINITY ? 1.f : 0.f) : ex2_approx(m - most);
-    const float mine = pm == -INFINITY ? (most == -INFINITY ? 1.f : 0.f) : ex2_approx(pm - most);
-    float t = pl * mine;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, d);
-    l = l * old + t;
-    m = most;
-    __syncthreads();
-    if (threadIdx.x < 32) s_weight[lane] = mine;
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const int d = threadIdx.x + j * kJoinThreads;
-      if (d < DH) {
-        float a = v[j] * old;
-#pragma unroll 8
-        for (int i = 0; i < k; ++i) a = fmaf(part(i0 + i)[d], s_weight[i], a);
-        v[j] = a;
-      }
-    }
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+  for (int i = lane; i < n; i += 32) {
+    const float pm = part(i)[DH], w = pm == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : ex2_approx(pm - m);
+    l += part(i)[DH + 1] * w;
+    if (tid < 32) s_weight[i] = w;
   }
-  const int head = at.hr / p.row_blocks, token = row / p.group, h = head * p.group + row % p.group;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
+  __syncthreads();
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float4& x, float w) {
+    v.x = fmaf(x.x, w, v.x); v.y = fmaf(x.y, w, v.y); v.z = fmaf(x.z, w, v.z); v.w = fmaf(x.w, w, v.w);
+  };
+#pragma unroll
+  for (int i = 0; i < kEarly; ++i)
+    if (stripe + i * kStripes < n) add(early[i], s_weight[stripe + i * kStripes]);
+#pragma unroll 4
+  for (int i = stripe + kEarly * kStripes; i < n; i += kStripes) add(*reinterpret_cast<const float4*>(part(i) + col), s_weight[i]);
+  s_sum[stripe][tid % kAcross] = v;
+  __syncthreads();
+  if (stripe > 0) return;
+#pragma unroll
+  for (int i = 1; i < kStripes; ++i) {
+    const float4 x = s_sum[i][tid];
+    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+  }
+  const int head = at.hr / p.row_blocks, token = p.groups.of(row), h = head * p.group + row - token * p.group;
   char* out = p.out + at.b * p.out_batch + token * p.out_token + h * p.out_head;
   const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int j = 0; j < kMine; ++j) {
-    const int d = threadIdx.x + j * kJoinThreads;
-    if (d < p.D && COMFUSE_IN_BOUNDS(row < p.rows && at.b < p.batch, p.status)) Elem<DT>::put(out, d, v[j] * inv);
-  }
-  if (p.lse && threadIdx.x == 0 && COMFUSE_IN_BOUNDS(at.b < p.batch && token < p.tokens, p.status))
+  const float y[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
+  uint32_t packed[2];
+  Elem<DT>::pack(y, packed);
+  if (col < p.D && COMFUSE_IN_BOUNDS(col + 4 <= p.D && row < p.rows && at.b < p.batch, p.status)) st_8(out + 2 * col, packed);
+  if (p.lse && tid == 0 && COMFUSE_IN_BOUNDS(at.b < p.batch && token < p.tokens, p.status))
     p.lse[(static_cast<long long>(at.b) * p.tokens + token) * p.heads * p.group + h] = log_sum(m, l);
 }
 
@@ -971,11 +1006,13 @@ cudaError_t launch_instance(const PagedAttentionPlan& plan, const PagedAttention
   count_launch();
   e = cudaLaunchKernelEx(&cfg, attention_kernel<DT, Q8, DH, NT, RW>, p);
   if (e != cudaSuccess || !plan.joined) return e;
-  cfg.gridDim = dim3(static_cast<unsigned>(plan.ctas - 1), static_cast<unsigned>(p.rows < F::kRows ? p.rows : F::kRows), 1);
+  const long long items = static_cast<long long>(p.batch) * p.heads * p.row_blocks;
+  const int by_item = items < plan.ctas - 1;
+  cfg.gridDim = dim3(static_cast<unsigned>(by_item ? items : plan.ctas - 1), static_cast<unsigned>(p.rows < F::kRows ? p.rows : F::kRows), 1);
   cfg.blockDim = dim3(kJoinThreads, 1, 1);
   cfg.dynamicSmemBytes = 0;
   count_launch();
-  return cudaLaunchKernelEx(&cfg, join_kernel<DT, Q8, DH, NT, RW>, p);
+  return cudaLaunchKernelEx(&cfg, join_kernel<DT, Q8, DH, NT, RW>, p, by_item);
 }
 
 template <int DT, bool Q8, int DH>
