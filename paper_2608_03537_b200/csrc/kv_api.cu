@@ -187,8 +187,8 @@ PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, b
   if (window > 0) seen = std::min<int64_t>(seen, static_cast<int64_t>(window) + tokens - 1 + f.block - 1);
   const int64_t units = std::max<int64_t>(1, (seen + f.unit - 1) / f.unit);
   const int64_t items = static_cast<int64_t>(batch) * heads * plan.row_blocks;
-  if (items > 0x7FFFFFFF / units) return plan;  // (units are counted in 32 bits: no CTAs)
-  plan.ctas = static_cast<int>(std::min<int64_t>(148 * f.ctas_per_sm, items * units));
+  if (items > 0x7FFFFFFF / (units + f.set_up)) return plan;  // (units are counted in 32 bits: no CTAs)
+  plan.ctas = static_cast<int>(std::min<int64_t>(148 * f.ctas_per_sm, items * (units + f.set_up)));
   plan.joined = units > 1 && plan.ctas > 1;
   plan.workspace = plan.joined ? static_cast<size_t>(plan.ctas) * paged::part_floats(plan.rows, DH) * sizeof(float) : 0;
   return plan;

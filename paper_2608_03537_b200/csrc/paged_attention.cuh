@@ -41,20 +41,22 @@ template <bool Q8, int DH, int NT, int RW>
 struct Form {
   static constexpr int kRowBytes = DH * (Q8 ? 1 : 2);
   static constexpr int kPieces = kRowBytes / 16;                  // of a row
-  static constexpr int kGroups = kRowBytes <= 128 ? 2 : 1;        // of 16 positions, in a block
+  static constexpr int kGroups = kRowBytes <= 128 && !(Q8 && DH == 128 && RW > 1) ? 2 : 1;  // of 16 positions, in a block
   static constexpr int kBlock = 16 * kGroups;
-  static constexpr int kKeyWarps = DH == 256 && RW == 4 ? 2 : 4;  // rings
+  static constexpr int kKeyWarps = RW == 4 ? 2 : 4;               // rings
   static constexpr int kWarps = kKeyWarps * RW, kThreads = 32 * kWarps;
   static constexpr int kUnit = kBlock * kKeyWarps;
   static constexpr int kRows = 8 * NT * RW;                       // of queries
+  static constexpr int kSetUp = 2;                                // what beginning and ending an item costs, in units
   static constexpr int kSide = kBlock * kRowBytes;                // keys, or values, of a block
   static constexpr int kStage = 2 * kSide + (Q8 ? 8 * kBlock : 0);  // and their scales
-  static constexpr int kJoinColumns = NT > 1 ? 32 : 64;          // where warps are joined, at a time
+  static constexpr int kJoinColumns = NT > 1 && RW == 1 ? 32 : 64;  // where warps are joined, at a time
   static constexpr int kPitch = kJoinColumns + 4;                 // floats of a row there: a warp's stores fall on all banks
   static constexpr int kJoin = kWarps * 8 * kPitch * 4;
-  static constexpr int kQuery = kRows * DH * (Q8 ? kDigits : 2);
+  static constexpr int kQueryStep = 8 * kRows + (Q8 ? 8 : 0);     // words of a step of all rows (8 bits: steps of a row on other banks)
+  static constexpr int kQuery = DH / (Q8 ? 32 : 16) * kQueryStep * 4 * (Q8 ? kDigits : 1);
   static constexpr int kSmall = 256 + 4 * 32 * kKeyWarps + kRows * (8 * kKeyWarps + 24);
-  static constexpr int kCtasPerSm = RW > 1 || DH == 256 ? 1 : 2;
+  static constexpr int kCtasPerSm = DH == 256 || (DH == 128 && RW > 1) ? 1 : 2;
   static constexpr int kSmem = kCtasPerSm == 2 ? 113 * 1024 : 226 * 1024;  // what a CTA may take
   static constexpr int kMostStages = (kSmem - kJoin - kQuery - kSmall) / (kStage * kKeyWarps);
   static constexpr int kStages = kMostStages < 8 ? kMostStages : 8;
@@ -67,9 +69,10 @@ __host__ __device__ inline long long part_floats(int rows, int D) { return 2ll *
 namespace {
 
 // ------------------------------------------------------------------------------------------------ shares
-// The line of units.  Each of a sequence's `hr` items (key heads x row blocks) has the same number of them.
+// The line of units.  Each of a sequence's `hr` items (key heads x row blocks) has the same number of them, and kSetUp more in front that stand for the work of beginning and ending an
+// item: shares are equal in both together (64 sequences of 20 .. 1000 positions, 8 heads of 128: the CTA with the most items, 14 of a unit each, took twice as long as the others).
 struct Line {
-  unsigned total, share, longer;  // the first `longer` CTAs have share + 1 units
+  unsigned total, share, longer;  // the first `longer` CTAs have share + 1
   __device__ unsigned begin(unsigned cta) const { return cta * share + (cta < longer ? cta : longer); }
   __device__ unsigned owner(unsigned unit) const {
     const unsigned l = longer * (share + 1);
@@ -92,7 +95,7 @@ template <typename F>
 __device__ __forceinline__ Line line_of(const PagedAttentionParams& p, int lane, unsigned* mine) {
   unsigned total = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
-    const unsigned n = b0 + lane < p.batch ? sequence_of<F>(p, b0 + lane).units : 0u;
+    const unsigned n = b0 + lane < p.batch ? sequence_of<F>(p, b0 + lane).units + F::kSetUp : 0u;
     if (b0 == 0) *mine = n;  // (most calls have no more)
     total += n;
   }
@@ -103,14 +106,15 @@ __device__ __forceinline__ Line line_of(const PagedAttentionParams& p, int lane,
   return line;
 }
 struct Place {
-  int b, hr, unit;
+  int b, hr, at;   // place in the item, kSetUp in front of the first unit
+  unsigned real;   // units in front of it, of all items
 };
 template <typename F>
 __device__ __forceinline__ Place place_of_unit(const PagedAttentionParams& p, int lane, unsigned mine, unsigned unit) {
   const unsigned hr = p.heads * p.row_blocks;
-  unsigned before = 0;  // units of the sequences in front, of one item each
+  unsigned before = 0;  // of the sequences in front, one item each
   for (int b0 = 0;; b0 += 32) {
-    const unsigned n = b0 == 0 ? mine : b0 + lane < p.batch ? sequence_of<F>(p, b0 + lane).units : 0u;
+    const unsigned n = b0 == 0 ? mine : b0 + lane < p.batch ? sequence_of<F>(p, b0 + lane).units + F::kSetUp : 0u;
     unsigned upto = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -124,7 +128,8 @@ __device__ __forceinline__ Place place_of_unit(const PagedAttentionParams& p, in
       Place at;
       at.b = b0 + i;
       at.hr = rest / units;
-      at.unit = rest - at.hr * units;
+      at.at = rest - at.hr * units;
+      at.real = unit - at.at - F::kSetUp * (at.b * hr + at.hr) + max(0, at.at - F::kSetUp);
       return at;
     }
     before += __shfl_sync(0xFFFFFFFFu, upto, 31);
@@ -233,25 +238,36 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
 
   unsigned lane_units;
   const Line line = line_of<F>(p, lane, &lane_units);
-  const unsigned first_unit = line.begin(blockIdx.x);
-  const int count = static_cast<int>(line.begin(blockIdx.x + 1) - first_unit);
-  if (count <= 0) return;
-  const Place at = place_of_unit<F>(p, lane, lane_units, first_unit);
+  const unsigned share_begin = line.begin(blockIdx.x), share_end = line.begin(blockIdx.x + 1);
+  if (share_begin >= share_end) return;
+  const Place at = place_of_unit<F>(p, lane, lane_units, share_begin);
+  // (the line's last place is a unit: the one behind it has one more in front)
+  const Place end = place_of_unit<F>(p, lane, lane_units, min(share_end, line.total - 1));
+  const int count = static_cast<int>(end.real - at.real) + (share_end == line.total);
+  if (count <= 0) return;  // (nothing but the front of an item)
+  const int first_at = max(0, at.at - F::kSetUp);
   const int HR = p.heads * p.row_blocks;
 
-  // ---- an item's queries: loaded by pieces of 8 elements, kept in shared memory as the product's operands, eight bytes a lane for each step and tile
-  constexpr int kQueryPieces = DH / 8, kQueryLoads = (F::kRows * kQueryPieces + F::kThreads - 1) / F::kThreads;
-  constexpr int kQuerySteps = Q8 ? DH / 32 : DH / 16, kPlane = kQuerySteps * NT * RW * 64;  // words (of a digit)
-  uint32_t q_raw[kQueryLoads][4];
+  // ---- an item's queries, kept in shared memory as the product's operands, eight bytes a lane for each step and tile: a step (16 elements; of 8 bits 32) of a row is 32 bytes in line (in
+  // each of the digits' planes).  A thread brings a step of a row; of 16 bits neighbours have neighbouring rows, of 8 bits the steps of one, whose largest element they need.
+  constexpr int kStepPieces = Q8 ? 4 : 2, kQuerySteps = DH / (8 * kStepPieces), kQueryLoads = (F::kRows * kQuerySteps + F::kThreads - 1) / F::kThreads;
+  constexpr int kStepWords = F::kQueryStep, kPlane = kQuerySteps * kStepWords;  // (of a digit)
+  uint32_t q_raw[kQueryLoads][kStepPieces][4];
+  auto query_row = [&](int i) { return Q8 ? (tid + i * F::kThreads) / kQuerySteps : (tid + i * F::kThreads) % F::kRows; };
+  auto query_step = [&](int i) { return Q8 ? (tid + i * F::kThreads) % kQuerySteps : (tid + i * F::kThreads) / F::kRows; };
   auto load_queries = [&](int b, int hr) {
     const int head = p.row_blocks == 1 ? hr : hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows;
 #pragma unroll
     for (int i = 0; i < kQueryLoads; ++i) {
-      const int n = tid + i * F::kThreads, r = n / kQueryPieces, piece = n % kQueryPieces, row = row0 + r;
-      q_raw[i][0] = q_raw[i][1] = q_raw[i][2] = q_raw[i][3] = 0u;
-      if (r < F::kRows && row < p.rows && piece * 8 < p.D) {
-        const int token = p.groups.of(row), h = head * p.group + row - token * p.group;
-        ld_16(p.q + b * p.q_batch + token * p.q_token + h * p.q_head + piece * 16, q_raw[i]);
+      const int r = query_row(i), step = query_step(i), row = row0 + r;
+      const bool there = r < F::kRows && step < kQuerySteps && row < p.rows;
+      const int token = p.groups.of(row), h = head * p.group + row - token * p.group;
+      const char* from = p.q + b * p.q_batch + token * p.q_token + h * p.q_head;
+#pragma unroll
+      for (int j = 0; j < kStepPieces; ++j) {
+        const int piece = step * kStepPieces + j;
+        q_raw[i][j][0] = q_raw[i][j][1] = q_raw[i][j][2] = q_raw[i][j][3] = 0u;
+        if (there && piece * 8 < p.D) ld_16(from + piece * 16, q_raw[i][j]);
       }
     }
   };
@@ -275,7 +291,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   const bool my_piece_there = my_piece * 16 < p.D * (Q8 ? 1 : 2);
   const uint32_t my_dst = ring_u32 + my_row * F::kRowBytes + place_of<F::kPieces>(my_row, my_piece) * 16;
   const bool whole_pages = p.page_size.d % F::kBlock == 0;  // a block lies in one page
-  int f_b = at.b, f_hr = at.hr, f_unit = at.unit, f_left = count, f_base, f_page, f_line;
+  int f_b = at.b, f_hr = at.hr, f_unit = first_at, f_left = count, f_base, f_page, f_line;
   Sequence f_seq = sequence_of<F>(p, f_b);
   const Sequence first_seq = f_seq;
   const int* f_table = p.table + f_b * p.table_stride;
@@ -366,49 +382,51 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
     const int head = p.row_blocks == 1 ? hr : hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows;
 #pragma unroll
     for (int i = 0; i < kQueryLoads; ++i) {
-      const int n = tid + i * F::kThreads, r = n / kQueryPieces, piece = n % kQueryPieces;
-      uint32_t* to = s_query + (r >> 3) * 64 + (r & 7) * 8;  // (of the step's tiles: this row's lanes)
+      const int r = query_row(i), step = query_step(i);
+      const bool mine = r < F::kRows && step < kQuerySteps;
+      uint32_t* to = s_query + step * kStepWords + r * 8;
       if constexpr (Q8) {
         // A multiple of 2^-21 of the power of two at or below the row's largest element, in three digits: exact for bf16 down to 2^-14 of that, for fp16 to 2^-11.
-        float v[8], most = 0.f;
+        uint32_t top = 0u;  // of the bits: infinities and NaNs are above every number
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          v[j] = Elem<DT>::of(q_raw[i], j);
-          most = fmaxf(most, fabsf(v[j]));
-        }
-        bool odd = false;  // an infinity or a NaN, which has no digits
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) odd |= !isfinite(v[j]);
+          for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(Elem<DT>::of(q_raw[i][j], e)) & 0x7FFFFFFFu);
 #pragma unroll
-        for (int o = kQueryPieces / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-        odd = __any_sync(0xFFFFFFFFu, odd) && [&] {
-          unsigned row_odd = __ballot_sync(0xFFFFFFFFu, odd);
-          return ((row_odd >> (lane & ~(kQueryPieces - 1) & 31)) & (kQueryPieces >= 32 ? 0xFFFFFFFFu : (1u << (kQueryPieces & 31)) - 1u)) != 0u;
-        }();
-        const uint32_t e = min(max(__float_as_uint(most) & 0x7F800000u, 0x10000000u), 0x7E000000u);  // (2^-95: a row below that is zero beside any other)
+        for (int o = kQuerySteps / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        const bool odd = top >= 0x7F800000u;  // (such a row has no digits: NaN)
+        const uint32_t e = min(max(top & 0x7F800000u, 0x10000000u), 0x7E000000u);  // (2^-95: a row below that is zero beside any other)
         const float up = reciprocal_of_power(__uint_as_float(e)) * 0x1p21f;
-        if (r < F::kRows && piece == 0) sm.factor[r] = odd ? __int_as_float(0x7FFFFFFF) : __uint_as_float(e) * 0x1p-21f;
-        uint32_t digit[kDigits][2] = {};
+        if (mine && step == 0) sm.factor[r] = odd ? __int_as_float(0x7FFFFFFF) : __uint_as_float(e) * 0x1p-21f;
+        // elements 4w .. 4w + 3 of the step are word 2 (w mod 4) + w / 4 of its row: lane c's first four, and 16 further its second
+        uint32_t digit[kDigits][8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          int x = odd ? 0 : __float2int_rn(v[j] * up);
+        for (int w = 0; w < 8; ++w) {
+          uint32_t word[kDigits] = {};
 #pragma unroll
-          for (int d = kDigits - 1; d > 0; --d) {
-            const int low = static_cast<int8_t>(x & 0xFF);
-            digit[d][j >> 2] |= (low & 0xFFu) << (8 * (j & 3));
-            x = (x - low) >> 8;
+          for (int j = 0; j < 4; ++j) {
+            const int n = 4 * w + j;
+            int x = odd ? 0 : __float2int_rn(Elem<DT>::of(q_raw[i][n >> 3], n & 7) * up);
+#pragma unroll
+            for (int d = kDigits - 1; d > 0; --d) {
+              const int low = static_cast<int8_t>(x & 0xFF);
+              word[d] |= (low & 0xFFu) << (8 * j);
+              x = (x - low) >> 8;
+            }
+            word[0] |= (x & 0xFFu) << (8 * j);
           }
-          digit[0][j >> 2] |= (x & 0xFFu) << (8 * (j & 3));
+#pragma unroll
+          for (int d = 0; d < kDigits; ++d) digit[d][2 * (w & 3) + (w >> 2)] = word[d];
         }
-        if (r < F::kRows) {
+        if (mine) {
 #pragma unroll
           for (int d = 0; d < kDigits; ++d)
 #pragma unroll
-            for (int w = 0; w < 2; ++w) to[d * kPlane + (piece >> 2) * NT * RW * 64 + ((piece & 1) * 2 + w) * 2 + ((piece >> 1) & 1)] = digit[d][w];
+            for (int w = 0; w < 8; w += 4) *reinterpret_cast<uint4*>(to + d * kPlane + w) = make_uint4(digit[d][w], digit[d][w + 1], digit[d][w + 2], digit[d][w + 3]);
         }
-      } else if (r < F::kRows) {
+      } else if (mine) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) to[(piece >> 1) * NT * RW * 64 + w * 2 + (piece & 1)] = q_raw[i][w];
+        for (int w = 0; w < 4; w += 2) *reinterpret_cast<uint4*>(to + 2 * w) = make_uint4(q_raw[i][0][w], q_raw[i][1][w], q_raw[i][0][w + 1], q_raw[i][1][w + 1]);
       }
     }
     if (tid < F::kRows) {
@@ -424,12 +442,12 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   int tiles = NT;
   auto has = [&](int n) { return NT * RW == 1 || n < tiles; };
   auto query_operand = [&](int digit, int step, int n) {
-    return *reinterpret_cast<const uint2*>(s_query + digit * kPlane + (step * NT * RW + n * RW + rw) * 64 + lane * 2);
+    return *reinterpret_cast<const uint2*>(s_query + digit * kPlane + step * kStepWords + (n * RW + rw) * 64 + lane * 2);
   };
   constexpr bool kHold = NT == 1 && DH <= 128;  // operands of the queries stay in registers
   uint2 q_held[kHold ? (Q8 ? kDigits : 1) : 1][kHold ? kQuerySteps : 1];
 
-  int b = at.b, hr = at.hr, unit = at.unit;  // where the blocks are
+  int b = at.b, hr = at.hr, unit = first_at;  // where the blocks are
 
   // ---- a warp's running state
   float o[kSteps][NT][4], top[NT][2], sum[NT][2];
@@ -526,7 +544,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
     if (NT * RW > 1 && tiles == 0) return;
     const uint32_t keys = ring_u32 + stage * F::kStage + k_lane, values = ring_u32 + stage * F::kStage + v_lane;
     float s[G][NT][4];
-    if constexpr (NT > 1) {
+    if constexpr (Q8 && NT > 1) {
 #pragma unroll
       for (int h = 0; h < G; ++h)
 #pragma unroll
@@ -899,31 +917,31 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttention
   unsigned lane_units;
   const Line line = line_of<F>(p, lane, &lane_units);
   Place at;
-  unsigned item, first, units;  // the item's first unit, its first share
+  unsigned item, first, units;  // where the item begins, its first share
   bool cut;
   if (by_item) {
     const int HR = p.heads * p.row_blocks;
     at.b = blockIdx.x / HR;
     at.hr = blockIdx.x - at.b * HR;
     unsigned before = 0;
-    for (int b0 = 0; b0 < at.b; b0 += 32) before += b0 + lane < at.b ? (b0 == 0 ? lane_units : sequence_of<F>(p, b0 + lane).units) : 0u;
+    for (int b0 = 0; b0 < at.b; b0 += 32) before += b0 + lane < at.b ? (b0 == 0 ? lane_units : sequence_of<F>(p, b0 + lane).units + F::kSetUp) : 0u;
     units = sequence_of<F>(p, at.b).units;
-    item = __reduce_add_sync(0xFFFFFFFFu, before) * HR + at.hr * units;
-    first = line.owner(item);
-    cut = line.owner(item + units - 1) != first;
+    item = __reduce_add_sync(0xFFFFFFFFu, before) * HR + at.hr * (units + F::kSetUp);
+    first = line.owner(item + F::kSetUp);
+    cut = line.owner(item + F::kSetUp + units - 1) != first;
   } else {
     const unsigned behind = line.begin(blockIdx.x + 1);
     at = place_of_unit<F>(p, lane, lane_units, min(behind, line.total - 1));
     units = sequence_of<F>(p, at.b).units;
-    item = behind - at.unit;
+    item = behind - at.at;
     first = blockIdx.x;
-    cut = behind < line.total && at.unit > 0 && item >= line.begin(blockIdx.x);
+    cut = behind < line.total && at.at > F::kSetUp && item + F::kSetUp >= line.begin(blockIdx.x);
   }
   griddep_wait();
   const int r = blockIdx.y, row = (at.hr % p.row_blocks) * F::kRows + r;
   if (!cut || row >= p.rows) return;
-  const int n = static_cast<int>(line.owner(item + units - 1) - first) + 1;  // parts
-  const int slot = item == line.begin(first) ? 0 : 1;
+  const int n = static_cast<int>(line.owner(item + F::kSetUp + units - 1) - first) + 1;  // parts
+  const int slot = item <= line.begin(first) ? 0 : 1;  // (a share that begins in front of the item has some of another's first)
   const float* first_part = p.part + first * part_floats(F::kRows, DH) + (slot * F::kRows + r) * (DH + 4);
   const float* next_part = p.part + (first + 1) * part_floats(F::kRows, DH) + r * (DH + 4);
   auto part = [&](int i) { return i == 0 ? first_part : next_part + (i - 1) * part_floats(F::kRows, DH); };
@@ -1017,11 +1035,10 @@ cudaError_t launch_instance(const PagedAttentionPlan& plan, const PagedAttention
 
 template <int DT, bool Q8, int DH>
 cudaError_t launch_rows(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
-  constexpr int kMost = DH == 256 ? 2 : 4;  // tiles of a warp
   if (plan.rows == 8) return launch_instance<DT, Q8, DH, 1, 1>(plan, p, stream);
   if (plan.rows == 16) return launch_instance<DT, Q8, DH, 2, 1>(plan, p, stream);
   if (plan.rows == 32) return launch_instance<DT, Q8, DH, 2, 2>(plan, p, stream);
-  return launch_instance<DT, Q8, DH, kMost, 8 / kMost>(plan, p, stream);
+  return launch_instance<DT, Q8, DH, 2, 4>(plan, p, stream);
 }
 template <int DT, bool Q8>
 cudaError_t launch_type(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
@@ -1032,17 +1049,16 @@ cudaError_t launch_type(const PagedAttentionPlan& plan, const PagedAttentionPara
 
 // What a plan needs to know of the instance that runs it.
 struct FormFacts {
-  int unit, block, ctas_per_sm;
+  int unit, block, ctas_per_sm, set_up;
 };
 template <bool Q8, int DH, int NT, int RW>
 constexpr FormFacts facts_of() {
   using F = Form<Q8, DH, NT, RW>;
-  return {F::kUnit, F::kBlock, F::kCtasPerSm};
+  return {F::kUnit, F::kBlock, F::kCtasPerSm, F::kSetUp};
 }
 template <bool Q8, int DH>
 FormFacts facts(int rows) {
-  constexpr int kMost = DH == 256 ? 2 : 4;
-  return rows == 8 ? facts_of<Q8, DH, 1, 1>() : rows == 16 ? facts_of<Q8, DH, 2, 1>() : rows == 32 ? facts_of<Q8, DH, 2, 2>() : facts_of<Q8, DH, kMost, 8 / kMost>();
+  return rows == 8 ? facts_of<Q8, DH, 1, 1>() : rows == 16 ? facts_of<Q8, DH, 2, 1>() : rows == 32 ? facts_of<Q8, DH, 2, 2>() : facts_of<Q8, DH, 2, 4>();
 }
 template <bool Q8>
 FormFacts facts(int D, int rows) {

@@ -171,7 +171,7 @@ def test_workspace_is_bounded():
         heads, group = int(r.randint(1, 17)), int(r.randint(1, 33))
         q8 = bool(r.randint(2))
         D = int(r.choice([16, 64, 80, 128, 256]))
-        st, n = _attention(size=True, **(QUANTIZED if q8 else {}), D=D, heads=heads, q_heads=heads * group, tokens=int(r.randint(1, 65)), batch=int(2 ** r.uniform(0, 8)), table_width=int(2 ** r.uniform(0, 20)),
+        st, n = _attention(size=True, **(QUANTIZED if q8 else {}), D=D, heads=heads, q_heads=heads * group, tokens=int(r.randint(1, 65)), batch=int(2 ** r.uniform(0, 8)), table_width=int(2 ** r.uniform(0, 14)),
                            window=int(r.choice([0, 100])), table_stride=1 << 20)
         assert st == cf.OK and 0 <= n <= cf.PAGED_ATTENTION_WORKSPACE_BYTES and n % 16 == 0
 
