@@ -1,6 +1,7 @@
 // C entry points of the key-value cache: argument checks, choice of the form.
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "kv_params.h"
 #include "paged_attention.cuh"
@@ -114,6 +115,16 @@ comfuse_status_t check_read(const comfuse_cache_read_desc_t* d, const comfuse_kv
   return aligned(k, 16) && aligned(v, 16) && aligned(slots, 8) ? COMFUSE_OK : COMFUSE_ERR_ALIGNMENT;
 }
 
+// COMFUSE_ATTENTION_CLUSTER: CTAs of an item (1, 2, 4, 8, 16), 0 = equal shares and a second kernel; otherwise the sizes decide.
+int forced_cluster() {
+  static const int n = [] {
+    const char* e = std::getenv("COMFUSE_ATTENTION_CLUSTER");
+    const int v = e ? std::atoi(e) : -1;
+    return v == 0 || v == 1 || v == 2 || v == 4 || v == 8 || v == 16 ? v : -1;
+  }();
+  return n;
+}
+
 // The longest sequence a call may meet, 0 where that is out of range.
 int64_t longest(const comfuse_paged_attention_desc_t* d, const comfuse_kv_cache_t* c) {
   const int64_t room = static_cast<int64_t>(d->table_width) * c->page_size;
@@ -188,7 +199,22 @@ PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, b
   const int64_t units = std::max<int64_t>(1, (seen + f.unit - 1) / f.unit);
   const int64_t items = static_cast<int64_t>(batch) * heads * plan.row_blocks;
   if (items > 0x7FFFFFFF / (units + f.set_up)) return plan;  // (units are counted in 32 bits: no CTAs)
-  plan.ctas = static_cast<int>(std::min<int64_t>(148 * f.ctas_per_sm, items * (units + f.set_up)));
+  const int64_t slots = 148 * f.ctas_per_sm;
+  // Items by clusters, or equal shares and a second kernel?  By estimated times.  In us: a CTA's start and end take 2.5, a unit 0.6 or what its bytes take at the CTA's part of 6.5 TB/s, a
+  // cluster's joining 0.6, the second kernel 2.8.  Clusters of 8 and 16 leave some SMs of the GPU's processing clusters idle.
+  auto unit_us = [&](int64_t ctas) { return std::max(0.6, f.unit_bytes * static_cast<double>(std::min(ctas, slots)) / 6.5e6); };
+  double best = 5.3 + static_cast<double>(items * (units + f.set_up)) / static_cast<double>(slots) * unit_us(items * units);
+  for (int c = 1; c <= 16 && (c == 1 || c <= units); c *= 2) {
+    const int64_t ctas = items * c, fit = f.ctas_per_sm * (c == 16 ? 112 : c == 8 ? 128 : 148);
+    const double us = static_cast<double>((ctas + fit - 1) / fit) * (2.5 + static_cast<double>((units + c - 1) / c) * unit_us(std::min(ctas, fit))) + (c > 1 ? 0.6 : 0.0);
+    if (us < best && ctas <= 0x7FFFFFFF) plan.cluster = c, best = us;
+  }
+  if (forced_cluster() >= 0 && items * 16 <= 0x7FFFFFFF) plan.cluster = forced_cluster();
+  if (plan.cluster > 0) {
+    plan.ctas = static_cast<int>(items * plan.cluster);
+    return plan;
+  }
+  plan.ctas = static_cast<int>(std::min<int64_t>(slots, items * (units + f.set_up)));
   plan.joined = units > 1 && plan.ctas > 1;
   plan.workspace = plan.joined ? static_cast<size_t>(plan.ctas) * paged::part_floats(plan.rows, DH) * sizeof(float) : 0;
   return plan;
@@ -300,6 +326,7 @@ comfuse_status_t comfuse_paged_attention(const comfuse_paged_attention_desc_t* d
   p.alpha = d.alpha; p.softcap = d.softcap;
   p.part = static_cast<float*>(workspace);
   p.ctas = plan.ctas;
+  p.cluster = plan.cluster;
   p.groups = Divisor(p.group);
   p.shares = Divisor(plan.ctas);
   p.status = dev->status_word;

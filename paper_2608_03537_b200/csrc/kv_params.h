@@ -82,13 +82,14 @@ struct PagedAttentionParams {
   float* lse;
   float alpha, softcap;
   float* part;                          // partial results, see paged_attention.cuh
-  int ctas;
+  int ctas, cluster;                    // cluster: CTAs of an item (0: shares)
   unsigned int* status;
 };
 // How a call is cut: query rows of a CTA (8, 16, 32 or 64), row blocks, CTAs, bytes of partial results.
 struct PagedAttentionPlan {
   int rows, row_blocks, ctas;
-  bool joined;                          // items may be split: a second kernel joins them
+  int cluster;                          // CTAs of an item, 0: items are cut where equal shares end
+  bool joined;                          // items may be cut: a second kernel joins them
   size_t workspace;
 };
 PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, bool quantized, int max_length, int window, int tokens);

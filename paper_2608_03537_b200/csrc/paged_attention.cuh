@@ -8,6 +8,8 @@
 //   * The call's work is a line of units of some positions (sequence by sequence, key head by key head), cut into equal shares, one for each of the CTAs that fit on the
 //     GPU: whatever the lengths, all finish together.  A CTA finds its share from the lengths themselves.  An item (sequence, key head) that lies in one share is
 //     finished there; one that is cut leaves a partial sum, maximum and weighted values for each share, and a second kernel joins them, in order.
+//   * Calls of few positions, whose time is latency, take clusters instead: each item is one cluster's, its units in equal parts the CTAs', which read one another's results through
+//     distributed shared memory.  One kernel, no shares to find, no partial results in memory.
 //   * A unit is a block of 16 or 32 positions for each of the CTA's key warps.  A key warp is on its own: it fetches its blocks by 16-byte asynchronous copies, several blocks ahead and
 //     across the ends of items, into a ring of its own, and keeps a running maximum, sum and weighted values; no barrier but at the end of an item, where they are joined.  Where there are
 //     more rows of queries than a warp holds, several warps share a ring and its fetching, each with rows of its own, and meet once a block.
@@ -193,6 +195,16 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
 }
 // 1 / x for x = 2^n, |n| < 127; anything for 0
 __device__ __forceinline__ float reciprocal_of_power(float x) { return __uint_as_float(0x7F000000u - __float_as_uint(x)); }
+__device__ __forceinline__ float2 ld_cluster_f32x2(uint32_t at) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
 // log of a sum whose terms were divided by 2^m; nothing: -inf
 __device__ __forceinline__ float log_sum(float m, float l) {
   if (m == -INFINITY) return l == 0.f ? -INFINITY : l;  // (else a NaN)
@@ -205,7 +217,7 @@ __device__ __forceinline__ int place_of(int r, int c) {
 }
 
 // ------------------------------------------------------------------------------------------------ the kernel
-template <int DT, bool Q8, int DH, int NT, int RW>
+template <int DT, bool Q8, int DH, int NT, int RW, bool CLUSTER>
 __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, NT, RW>::kCtasPerSm) attention_kernel(const PagedAttentionParams p) {
   using F = Form<Q8, DH, NT, RW>;
   constexpr bool kBf16 = DT == COMFUSE_DTYPE_BF16;  // of queries and outputs
@@ -228,6 +240,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
     unsigned valid[F::kKeyWarps][8];                               // of the blocks in the ring: positions that are there
   };
   static_assert(sizeof(Small) <= F::kSmall, "room for what is small");
+  static_assert(F::kRows * (DH + 4) * 4 <= S * F::kStage * F::kKeyWarps, "a cluster's CTA keeps its results where its rings were");
   Small& sm = *reinterpret_cast<Small*>(reinterpret_cast<char*>(s_query) + F::kQuery);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int kw = RW == 1 ? warp : warp / RW, rw = RW == 1 ? 0 : warp % RW;  // which ring, which rows
@@ -236,17 +249,29 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   griddep_wait();
   griddep_launch_dependents();  // behind the wait: the joining kernel reads the lengths before its own
 
-  unsigned lane_units;
-  const Line line = line_of<F>(p, lane, &lane_units);
-  const unsigned share_begin = line.begin(blockIdx.x), share_end = line.begin(blockIdx.x + 1);
-  if (share_begin >= share_end) return;
-  const Place at = place_of_unit<F>(p, lane, lane_units, share_begin);
-  // (the line's last place is a unit: the one behind it has one more in front)
-  const Place end = place_of_unit<F>(p, lane, lane_units, min(share_end, line.total - 1));
-  const int count = static_cast<int>(end.real - at.real) + (share_end == line.total);
-  if (count <= 0) return;  // (nothing but the front of an item)
-  const int first_at = max(0, at.at - F::kSetUp);
   const int HR = p.heads * p.row_blocks;
+  Place at;
+  int count, first_at;
+  const int rank = CLUSTER ? blockIdx.x % p.cluster : 0;
+  if constexpr (CLUSTER) {
+    const int item = blockIdx.x / p.cluster;
+    at.b = item / HR;
+    at.hr = item - at.b * HR;
+    const long long units = sequence_of<F>(p, at.b).units;
+    first_at = static_cast<int>(units * rank / p.cluster);
+    count = static_cast<int>(units * (rank + 1) / p.cluster) - first_at;
+  } else {
+    unsigned lane_units;
+    const Line line = line_of<F>(p, lane, &lane_units);
+    const unsigned share_begin = line.begin(blockIdx.x), share_end = line.begin(blockIdx.x + 1);
+    if (share_begin >= share_end) return;
+    at = place_of_unit<F>(p, lane, lane_units, share_begin);
+    // (the line's last place is a unit: the one behind it has one more in front)
+    const Place end = place_of_unit<F>(p, lane, lane_units, min(share_end, line.total - 1));
+    count = static_cast<int>(end.real - at.real) + (share_end == line.total);
+    if (count <= 0) return;  // (nothing but the front of an item)
+    first_at = max(0, at.at - F::kSetUp);
+  }
 
   // ---- an item's queries, kept in shared memory as the product's operands, eight bytes a lane for each step and tile: a step (16 elements; of 8 bits 32) of a row is 32 bytes in line (in
   // each of the digits' planes).  A thread brings a step of a row; of 16 bits neighbours have neighbouring rows, of 8 bits the steps of one, whose largest element they need.
@@ -317,7 +342,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
     }
   };
   set_head();
-  look_up();
+  if (count > 0) look_up();
   auto fetch = [&](int stage) {
     if (f_left > 0) {
       const bool there = f_page >= 0 && f_page < p.pages && f_base + my_pos >= f_seq.low;
@@ -769,7 +794,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   // ---- the end of an item, or of the share: the rings' results are joined; whole items are finished, cut ones kept
   // A thread adds up kMine columns of every kJoinColumns, of one of the 8 RW rows that a tile of each row warp makes.
   constexpr int kMine = 8 * RW * F::kJoinColumns / F::kThreads, kAcross = F::kJoinColumns / kMine;
-  auto end_item = [&](bool whole, int slot) {
+  // `part`: where the rows of a cut item go (a cluster: into its own shared memory).
+  auto end_item = [&](bool whole, float* parts) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -803,11 +829,11 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
       for (int w = 0; w < F::kKeyWarps; ++w) l += sm.sum[w][row] * (sm.top[w][row] == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : ex2_approx(sm.top[w][row] - m));
       const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
       const bool there = sm.out[row] >= 0;
-      float* part = p.part + blockIdx.x * part_floats(F::kRows, DH) + (slot * F::kRows + row) * (DH + 4);
+      float* part = parts + row * (DH + 4);
       if (there && tid % kAcross == 0) {
         if (whole) {
           if (p.lse && COMFUSE_IN_BOUNDS(sm.lse[row] < p.batch * p.tokens * p.heads * p.group, p.status)) p.lse[sm.lse[row]] = log_sum(m, l);
-        } else if (COMFUSE_IN_BOUNDS(row < F::kRows && slot < 2, p.status)) {
+        } else if (COMFUSE_IN_BOUNDS(row < F::kRows, p.status)) {
           part[DH] = m;
           part[DH + 1] = l;
         }
@@ -849,12 +875,9 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
             else if constexpr (kMine == 4) st_8(to, y);
             else *reinterpret_cast<uint32_t*>(to) = y[0];
           }
-        } else if (COMFUSE_IN_BOUNDS(row < F::kRows && slot < 2, p.status)) {
-          if constexpr (kMine == 2) st_8(part + at, reinterpret_cast<const uint32_t*>(v));
-          else {
+        } else if (COMFUSE_IN_BOUNDS(row < F::kRows, p.status)) {
 #pragma unroll
-            for (int j = 0; j < kMine; j += 4) st_16(part + at + j, reinterpret_cast<const uint32_t*>(v) + j);
-          }
+          for (int j = 0; j < kMine; j += 2) *reinterpret_cast<float2*>(part + at + j) = make_float2(v[j], v[j + 1]);
         }
       }
     }
@@ -865,7 +888,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   bool from_start = unit == 0, fresh = true;
   int pieces = 0;
   Sequence seq = first_seq;
-  for (int n = 1 - S; n < count; ++n) {
+  for (int n = 1 - S; n < (CLUSTER ? max(count, 1) : count); ++n) {
     if (n >= 0) {
       if (fresh) {
         keep_queries(b, hr);
@@ -878,15 +901,54 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
     }
     fetch(n < 0 ? n + S - 1 : stage == 0 ? S - 1 : stage - 1);
     if (n < 0) continue;
-    block(stage, seq, (seq.low & ~(F::kBlock - 1)) + unit * F::kUnit + kw * F::kBlock);
+    if (!CLUSTER || count > 0) block(stage, seq, (seq.low & ~(F::kBlock - 1)) + unit * F::kUnit + kw * F::kBlock);
     stage = stage + 1 == S ? 0 : stage + 1;
     ++unit;
+    if constexpr (CLUSTER) {
+      if (n + 1 < count) continue;
+      if (p.cluster == 1) {
+        end_item(true, nullptr);
+        break;
+      }
+      // The cluster's results: each CTA's in its own shared memory (the rings are done with), read by all for some of the outputs each.
+      cp_async_wait<0>();
+      __syncthreads();
+      float* mine = reinterpret_cast<float*>(smem);
+      end_item(false, mine);
+      cluster_sync_all();
+      const uint32_t mine_u32 = smem_u32(mine);
+      const int head = p.row_blocks == 1 ? hr : hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows, here = min(F::kRows, p.rows - row0);
+      for (int i = rank + p.cluster * tid; i < here * (DH / 4); i += p.cluster * F::kThreads) {
+        const int r = i / (DH / 4), col = (i % (DH / 4)) * 4;
+        const uint32_t stats = mine_u32 + (r * (DH + 4) + DH) * 4, values = mine_u32 + (r * (DH + 4) + col) * 4;
+        float m = -INFINITY;
+        for (int k = 0; k < p.cluster; ++k) m = fmaxf(m, ld_cluster_f32x2(map_to_cta(stats, k)).x);
+        float l = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < p.cluster; ++k) {
+          const float2 s = ld_cluster_f32x2(map_to_cta(stats, k));
+          const float4 x = ld_cluster_f32x4(map_to_cta(values, k));
+          const float w = s.x == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : ex2_approx(s.x - m);
+          l = fmaf(s.y, w, l);
+          v.x = fmaf(x.x, w, v.x); v.y = fmaf(x.y, w, v.y); v.z = fmaf(x.z, w, v.z); v.w = fmaf(x.w, w, v.w);
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float y[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
+        uint32_t packed[2];
+        Elem<DT>::pack(y, packed);
+        if (col < p.D && COMFUSE_IN_BOUNDS(col + 4 <= p.D && r < here, p.status)) st_8(p.out + sm.out[r] + 2 * col, packed);
+        if (p.lse && col == 0 && COMFUSE_IN_BOUNDS(sm.lse[r] < p.batch * p.tokens * p.heads * p.group, p.status)) p.lse[sm.lse[r]] = log_sum(m, l);
+      }
+      cluster_sync_all();  // (nobody reads another CTA's shared memory behind it)
+      break;
+    }
     if (unit == seq.units || n + 1 == count) {
       const bool whole = from_start && unit == seq.units, more = n + 1 < count;
       int nb = b, nhr = hr + 1;
       if (nhr == HR) nhr = 0, ++nb;
       if (more) load_queries(nb, nhr);  // on their way under the joining
-      end_item(whole, pieces ? 1 : 0);
+      end_item(whole, p.part + blockIdx.x * part_floats(F::kRows, DH) + (pieces ? F::kRows * (DH + 4) : 0));
       if (more) {
         __syncthreads();  // everyone has read the last item's rows
         ++pieces;
@@ -993,52 +1055,68 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttention
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-template <int DT, bool Q8, int DH, int NT, int RW>
-cudaError_t launch_instance(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
-  using F = Form<Q8, DH, NT, RW>;
-  static std::atomic<unsigned long long> ready{0};  // devices on which the kernel may take its shared memory
+// Dynamic shared memory, and clusters of 16, are asked for once a device.
+cudaError_t make_ready(const void* kernel, int bytes, bool clusters, std::atomic<unsigned long long>* ready) {
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
   const unsigned long long bit = 1ull << (device & 63);
-  if (device > 63 || !(ready.load(std::memory_order_relaxed) & bit)) {
-    e = cudaFuncSetAttribute(attention_kernel<DT, Q8, DH, NT, RW>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kBytes);
-    if (e != cudaSuccess) return e;
-    ready.fetch_or(bit, std::memory_order_relaxed);
-  }
+  if (device < 64 && (ready->load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && clusters) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) ready->fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+template <int DT, bool Q8, int DH, int NT, int RW, bool CLUSTER>
+cudaError_t launch_instance(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
+  using F = Form<Q8, DH, NT, RW>;
+  static std::atomic<unsigned long long> ready{0};
+  const auto kernel = attention_kernel<DT, Q8, DH, NT, RW, CLUSTER>;
+  cudaError_t e = make_ready(reinterpret_cast<const void*>(kernel), F::kBytes, CLUSTER, &ready);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   cfg.gridDim = dim3(static_cast<unsigned>(plan.ctas), 1, 1);
   cfg.blockDim = dim3(F::kThreads, 1, 1);
   cfg.dynamicSmemBytes = F::kBytes;
   cfg.stream = stream;
+  cfg.attrs = attr;
   if (programmatic_launch_enabled()) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
     cfg.numAttrs = 1;
   }
+  if (CLUSTER && plan.cluster > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = static_cast<unsigned>(plan.cluster);
+    attr[cfg.numAttrs].val.clusterDim.y = 1;
+    attr[cfg.numAttrs++].val.clusterDim.z = 1;
+  }
   if (verbose_enabled())
-    std::fprintf(stderr, "comfuse: paged_attention dtype=%d quantized=%d D<=%d row tiles=%d x %d row blocks=%d CTAs=%d stages=%d joined=%d\n", DT, Q8, DH, NT, RW, p.row_blocks, plan.ctas, F::kStages,
-                 plan.joined);
+    std::fprintf(stderr, "comfuse: paged_attention dtype=%d quantized=%d D<=%d row tiles=%d x %d row blocks=%d CTAs=%d cluster=%d stages=%d joined=%d\n", DT, Q8, DH, NT, RW, p.row_blocks, plan.ctas,
+                 plan.cluster, F::kStages, plan.joined);
   count_launch();
-  e = cudaLaunchKernelEx(&cfg, attention_kernel<DT, Q8, DH, NT, RW>, p);
-  if (e != cudaSuccess || !plan.joined) return e;
-  const long long items = static_cast<long long>(p.batch) * p.heads * p.row_blocks;
-  const int by_item = items < plan.ctas - 1;
-  cfg.gridDim = dim3(static_cast<unsigned>(by_item ? items : plan.ctas - 1), static_cast<unsigned>(p.rows < F::kRows ? p.rows : F::kRows), 1);
-  cfg.blockDim = dim3(kJoinThreads, 1, 1);
-  cfg.dynamicSmemBytes = 0;
-  count_launch();
-  return cudaLaunchKernelEx(&cfg, join_kernel<DT, Q8, DH, NT, RW>, p, by_item);
+  e = cudaLaunchKernelEx(&cfg, kernel, p);
+  if constexpr (!CLUSTER) {
+    if (e != cudaSuccess || !plan.joined) return e;
+    const long long items = static_cast<long long>(p.batch) * p.heads * p.row_blocks;
+    const int by_item = items < plan.ctas - 1;
+    cfg.gridDim = dim3(static_cast<unsigned>(by_item ? items : plan.ctas - 1), static_cast<unsigned>(p.rows < F::kRows ? p.rows : F::kRows), 1);
+    cfg.blockDim = dim3(kJoinThreads, 1, 1);
+    cfg.dynamicSmemBytes = 0;
+    count_launch();
+    e = cudaLaunchKernelEx(&cfg, join_kernel<DT, Q8, DH, NT, RW>, p, by_item);
+  }
+  return e;
 }
 
 template <int DT, bool Q8, int DH>
 cudaError_t launch_rows(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
-  if (plan.rows == 8) return launch_instance<DT, Q8, DH, 1, 1>(plan, p, stream);
-  if (plan.rows == 16) return launch_instance<DT, Q8, DH, 2, 1>(plan, p, stream);
-  if (plan.rows == 32) return launch_instance<DT, Q8, DH, 2, 2>(plan, p, stream);
-  return launch_instance<DT, Q8, DH, 2, 4>(plan, p, stream);
+  if (plan.rows == 8) return plan.cluster ? launch_instance<DT, Q8, DH, 1, 1, true>(plan, p, stream) : launch_instance<DT, Q8, DH, 1, 1, false>(plan, p, stream);
+  if (plan.rows == 16) return plan.cluster ? launch_instance<DT, Q8, DH, 2, 1, true>(plan, p, stream) : launch_instance<DT, Q8, DH, 2, 1, false>(plan, p, stream);
+  if (plan.rows == 32) return plan.cluster ? launch_instance<DT, Q8, DH, 2, 2, true>(plan, p, stream) : launch_instance<DT, Q8, DH, 2, 2, false>(plan, p, stream);
+  return plan.cluster ? launch_instance<DT, Q8, DH, 2, 4, true>(plan, p, stream) : launch_instance<DT, Q8, DH, 2, 4, false>(plan, p, stream);
 }
 template <int DT, bool Q8>
 cudaError_t launch_type(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
@@ -1049,12 +1127,12 @@ cudaError_t launch_type(const PagedAttentionPlan& plan, const PagedAttentionPara
 
 // What a plan needs to know of the instance that runs it.
 struct FormFacts {
-  int unit, block, ctas_per_sm, set_up;
+  int unit, block, ctas_per_sm, set_up, unit_bytes;
 };
 template <bool Q8, int DH, int NT, int RW>
 constexpr FormFacts facts_of() {
   using F = Form<Q8, DH, NT, RW>;
-  return {F::kUnit, F::kBlock, F::kCtasPerSm, F::kSetUp};
+  return {F::kUnit, F::kBlock, F::kCtasPerSm, F::kSetUp, F::kStage * F::kKeyWarps};
 }
 template <bool Q8, int DH>
 FormFacts facts(int rows) {

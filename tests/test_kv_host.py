@@ -153,12 +153,13 @@ def test_attention_refuses():
     for kw in (dict(q=None), dict(table=None), dict(lengths=None), dict(out=None), dict(batch=0), dict(tokens=0), dict(q_heads=0), dict(q_heads=7), dict(table_width=0), dict(max_length=-1), dict(window=-1),
                dict(alpha=float("inf")), dict(softcap=-1.0), dict(softcap=float("nan")), dict(table_stride=9), dict(q_strides=(1024, 512, 0)), dict(out_strides=(1024, 512, 56))):
         assert _attention(**kw) == cf.ERR_INVALID_ARG, kw
-    for kw in (dict(q=ODD), dict(out=ODD), dict(table=OFF4), dict(lengths=OFF4), dict(slopes=OFF4), dict(lse=OFF4), dict(workspace=ODD), dict(q_strides=(1028, 512, 64))):
+    long = dict(table_width=4096, table_stride=4096)   # room for sequences that are cut
+    for kw in (dict(q=ODD), dict(out=ODD), dict(table=OFF4), dict(lengths=OFF4), dict(slopes=OFF4), dict(lse=OFF4), dict(long, workspace=ODD), dict(q_strides=(1028, 512, 64))):
         assert _attention(**kw) == cf.ERR_ALIGNMENT, kw
     for kw in (dict(tokens=65), dict(table_width=2 ** 28, table_stride=2 ** 28), dict(batch=2 ** 30)):
         assert _attention(**kw) == cf.ERR_UNSUPPORTED, kw
-    need = _attention(size=True)[1]
-    for kw in (dict(workspace=None), dict(bytes=need - 1)):
+    need = _attention(size=True, **long)[1]
+    for kw in (dict(long, workspace=None), dict(long, bytes=need - 1)):
         assert _attention(**kw) == cf.ERR_WORKSPACE, kw
     assert L.comfuse_paged_attention_workspace_size(None, ref(_cache_of()), ref(ctypes.c_size_t())) == cf.ERR_INVALID_ARG
     assert _attention(size=True, q_heads=7)[0] == cf.ERR_INVALID_ARG
