@@ -49,7 +49,7 @@ struct Form {
   static constexpr int kWarps = kKeyWarps * RW, kThreads = 32 * kWarps;
   static constexpr int kUnit = kBlock * kKeyWarps;
   static constexpr int kRows = 8 * NT * RW;                       // of queries
-  static constexpr int kSetUp = 2;                                // what beginning and ending an item costs, in units
+  static constexpr int kSetUp = kUnit < 64 ? 4 : 2;               // what beginning and ending an item costs, in units
   static constexpr int kSide = kBlock * kRowBytes;                // keys, or values, of a block
   static constexpr int kStage = 2 * kSide + (Q8 ? 8 * kBlock : 0);  // and their scales
   static constexpr int kJoinColumns = NT > 1 && RW == 1 ? 32 : 64;  // where warps are joined, at a time
