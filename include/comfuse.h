@@ -525,7 +525,7 @@ typedef struct {
   int32_t pages, heads, page_size, D;   /* >= 1; page_size <= 65536; pages * page_size < 2^31; D <= 256, a multiple of 8 (quantized: of 16) */
   int32_t dtype;                        /* COMFUSE_DTYPE_BF16 or _F16: what rows are written from and read back to, and, unless quantized, held in */
   int32_t quantized;                    /* 0 or 1 */
-  int64_t k_strides[3], v_strides[3];   /* of a page, of a head, of a row */
+  int64_t k_strides[3], v_strides[3];   /* of a page, of a head, of a row; a page's and a row's below 2^31 bytes */
   int64_t k_scale_strides[3], v_scale_strides[3];
 } comfuse_kv_cache_t;
 

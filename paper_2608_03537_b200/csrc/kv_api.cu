@@ -58,6 +58,9 @@ comfuse_status_t check_cache(const comfuse_kv_cache_t* c) {
   CHECK_STRIDES(c->k_strides, bytes, c->pages, c->heads, c->page_size);
   CHECK_STRIDES(c->v_strides, bytes, c->pages, c->heads, c->page_size);
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) return COMFUSE_ERR_ALIGNMENT;
+  // (offsets within a page, and of pages, are products of 32-bit numbers)
+  for (const int64_t* s : {c->k_strides, c->v_strides})
+    if ((c->pages > 1 && s[0] * bytes > 0x7FFFFFFF) || (c->page_size > 1 && s[2] * bytes > 0x7FFFFFFF)) return COMFUSE_ERR_UNSUPPORTED;
   if (c->quantized) {
     const int64_t sizes[] = {c->pages, c->heads, c->page_size};
     if (!strides_ok(c->k_scale_strides, sizes, 1) || !strides_ok(c->v_scale_strides, sizes, 1)) return COMFUSE_ERR_INVALID_ARG;
@@ -171,8 +174,9 @@ void fill_rotary(const comfuse_rotary_t* r, RotaryWriteParams* p) {
 }
 void fill_cache(const comfuse_kv_cache_t& c, CacheSide* k, CacheSide* v) {
   const int bytes = c.quantized ? 1 : 2;
-  *k = {static_cast<char*>(c.k), c.k_scale, c.k_strides[0] * bytes, c.k_strides[1] * bytes, c.k_strides[2] * bytes, c.k_scale_strides[0], c.k_scale_strides[1], c.k_scale_strides[2]};
-  *v = {static_cast<char*>(c.v), c.v_scale, c.v_strides[0] * bytes, c.v_strides[1] * bytes, c.v_strides[2] * bytes, c.v_scale_strides[0], c.v_scale_strides[1], c.v_scale_strides[2]};
+  auto used = [](int64_t stride, int64_t size) { return size > 1 ? stride : 0; };  // (of a dimension of one element: anything)
+  *k = {static_cast<char*>(c.k), c.k_scale, used(c.k_strides[0], c.pages) * bytes, used(c.k_strides[1], c.heads) * bytes, used(c.k_strides[2], c.page_size) * bytes, c.k_scale_strides[0], c.k_scale_strides[1], c.k_scale_strides[2]};
+  *v = {static_cast<char*>(c.v), c.v_scale, used(c.v_strides[0], c.pages) * bytes, used(c.v_strides[1], c.heads) * bytes, used(c.v_strides[2], c.page_size) * bytes, c.v_scale_strides[0], c.v_scale_strides[1], c.v_scale_strides[2]};
 }
 RowsSide rows_side(const void* in, const int64_t* in_strides, void* out, const int64_t* out_strides, int bytes) {
   RowsSide r = {};

@@ -316,6 +316,11 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   const bool my_piece_there = my_piece * 16 < p.D * (Q8 ? 1 : 2);
   const uint32_t my_dst = ring_u32 + my_row * F::kRowBytes + place_of<F::kPieces>(my_row, my_piece) * 16;
   const bool whole_pages = p.page_size.d % F::kBlock == 0;  // a block lies in one page
+  const bool same_strides = p.kc.page == p.vc.page && p.kc.row == p.vc.row;
+  // (the strides of pages and rows fit in 32 bits)
+  auto offset = [](unsigned page, unsigned row, const CacheSide& c) {
+    return static_cast<long long>(static_cast<unsigned long long>(page) * static_cast<unsigned>(c.page) + static_cast<unsigned long long>(row) * static_cast<unsigned>(c.row));
+  };
   int f_b = at.b, f_hr = at.hr, f_unit = first_at, f_left = count, f_base, f_page, f_line;
   Sequence f_seq = sequence_of<F>(p, f_b);
   const Sequence first_seq = f_seq;
@@ -353,8 +358,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         const uint32_t dst = my_dst + stage * F::kStage;
         if (valid == kAll && whole_pages) {
           const int first = f_line - my_pos + my_row;
-          const char* k = f_k + f_page * p.kc.page + first * p.kc.row;
-          const char* v = f_v + f_page * p.vc.page + first * p.vc.row;
+          const char* k = f_k + offset(f_page, first, p.kc);
+          const char* v = f_v + offset(f_page, first, p.vc);
           const long long k_step = kRowStep * p.kc.row, v_step = kRowStep * p.vc.row;
           if (my_piece_there) {
 #pragma unroll
@@ -367,16 +372,19 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
             }
           }
         } else {
-          const int safe_page = there ? f_page : 0, safe_line = there ? f_line : 0;
+          // each position's offset by the lane that knows it, then to those that fetch it
+          const long long k_mine = there ? offset(f_page, f_line, p.kc) : 0, v_mine = same_strides ? k_mine : there ? offset(f_page, f_line, p.vc) : 0;
 #pragma unroll
           for (int i = 0; i < kLoads; ++i) {
             const int r = i * kRowStep + my_row;
-            const long long page = __shfl_sync(0xFFFFFFFFu, safe_page, r), row = __shfl_sync(0xFFFFFFFFu, safe_line, r);
+            const long long k_at = __shfl_sync(0xFFFFFFFFu, k_mine, r);
+            long long v_at = k_at;
+            if (!same_strides) v_at = __shfl_sync(0xFFFFFFFFu, v_mine, r);
             const bool ok = (valid >> r) & 1u;  // (a position that is not there reads as zeros)
             const uint32_t to = (F::kPieces >= 8 ? dst ^ ((i * kRowStep & 7) << 4) : dst) + i * kRowStep * F::kRowBytes;
             if (my_piece_there) {
-              cp_async_16(to, f_k + page * p.kc.page + row * p.kc.row, ok);
-              cp_async_16(to + F::kSide, f_v + page * p.vc.page + row * p.vc.row, ok);
+              cp_async_16(to, f_k + k_at, ok);
+              cp_async_16(to + F::kSide, f_v + v_at, ok);
             }
           }
         }
@@ -643,22 +651,13 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         ref[n][j] = none ? 0.f : top[n][j];
         limit[n][j] = none ? -INFINITY : kSlack;
       }
-    if (p.softcap > 0.f || p.slopes || !all) {
+    if (p.softcap > 0.f) {
 #pragma unroll
       for (int h = 0; h < G; ++h)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int j = i & 1, r = row_of_mine + 8 * RW * n + j, k = 16 * h + g + 8 * (i >> 1);
-            float v = s[h][n][i] * factor[n][j];
-            if constexpr (Q8) v *= ks[h][i >> 1];
-            if (p.softcap > 0.f) v = cap(v);
-            const int gap = base + k - (first + sm.token[r]);
-            if (p.slopes) v = fmaf(sm.slope[r], static_cast<float>(gap), v);
-            const bool hidden = !(((valid >> k) & 1u) && gap <= 0 && (p.window <= 0 || gap > -p.window));
-            s[h][n][i] = hidden ? -INFINITY : v - ref[n][j];
-          }
+          for (int i = 0; i < 4; ++i) s[h][n][i] = cap(Q8 ? s[h][n][i] * (factor[n][i & 1] * ks[h][i >> 1]) : s[h][n][i]) - ref[n][i & 1];
     } else {
 #pragma unroll
       for (int h = 0; h < G; ++h)
@@ -666,6 +665,34 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[h][n][i] = fmaf(s[h][n][i], Q8 ? factor[n][i & 1] * ks[h][i >> 1] : factor[n][i & 1], -ref[n][i & 1]);
+    }
+    if (p.slopes) {  // slope (n - m), from the distance of the block's first position on
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = row_of_mine + 8 * RW * n + j;
+          const float slope = sm.slope[r], from = static_cast<float>(base + g - (first + sm.token[r])) * slope;
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[h][n][2 * i + j] += fmaf(slope, static_cast<float>(16 * h + 8 * i), from);
+        }
+    }
+    if (!all) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int last = first + sm.token[row_of_mine + 8 * RW * n + j] - base;  // the row sees positions of the block up to this one
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int k = 16 * h + 8 * i + g;
+              if (!((valid >> k) & 1u) || k > last || (p.window > 0 && k <= last - p.window)) s[h][n][2 * i + j] = -INFINITY;
+            }
+        }
     }
     // the maximum, where a score is well above it
     bool above = false;
