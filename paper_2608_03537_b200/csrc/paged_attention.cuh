@@ -22,6 +22,7 @@
 #pragma once
 
 #include <cstdio>
+#include <type_traits>
 
 #include "kv_params.h"
 #include "q8_common.cuh"
@@ -129,7 +130,9 @@ __device__ __forceinline__ Place place_of_unit(const PagedAttentionParams& p, in
       const unsigned units = __shfl_sync(0xFFFFFFFFu, n, i), rest = unit - (before + __shfl_sync(0xFFFFFFFFu, upto, i) - units) * hr;
       Place at;
       at.b = b0 + i;
-      at.hr = rest / units;
+      at.hr = static_cast<int>(__fdividef(static_cast<float>(rest), static_cast<float>(units)));  // (off by one at most)
+      if (at.hr * units > rest) --at.hr;
+      if ((at.hr + 1) * units <= rest) ++at.hr;
       at.at = rest - at.hr * units;
       at.real = unit - at.at - F::kSetUp * (at.b * hr + at.hr) + max(0, at.at - F::kSetUp);
       return at;
@@ -473,7 +476,6 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   // Tile n of a warp is tile n RW + rw of the CTA, so that few rows are spread over its warps; columns 2c, 2c + 1 are this lane's.  Tiles behind the rows are left out.
   const int row_of_mine = 8 * rw + 2 * c;
   int tiles = NT;
-  auto has = [&](int n) { return NT * RW == 1 || n < tiles; };
   auto query_operand = [&](int digit, int step, int n) {
     return *reinterpret_cast<const uint2*>(s_query + digit * kPlane + step * kStepWords + (n * RW + rw) * 64 + lane * 2);
   };
@@ -490,7 +492,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   float factor[NT][2];  // of a score
   const SoftcapLog2 cap(p.alpha, p.softcap > 0.f ? p.softcap : 1.f);
   auto begin_item = [&]() {
-    if constexpr (NT * RW > 1) {
+    if constexpr (RW > 1) {
       const int here = p.row_blocks == 1 ? p.rows : min(F::kRows, p.rows - (hr - hr / p.row_blocks * p.row_blocks) * F::kRows);
       tiles = max(0, min(NT, (here - 8 * rw + 8 * RW - 1) / (8 * RW)));
     }
@@ -525,6 +527,242 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   const uint32_t k_lane = low_row * F::kRowBytes + place_of<F::kPieces>(low_row, lane >> 4) * 16;
   const uint32_t v_lane = F::kSide + v_row * F::kRowBytes + place_of<F::kPieces>(v_row, v_piece) * 16;
   auto at_piece = [](uint32_t base, int k) { return (base ^ ((k & 7) << 4)) + (k >> 3) * 128; };
+  // The products and the softmax of a block, for this warp's first TN tiles.
+  auto products = [&](auto tn, int stage, const Sequence& seq, int base, unsigned valid, bool all) {
+    constexpr int TN = decltype(tn)::value;
+    const int first = seq.length - p.tokens;  // the first new token's position
+    const uint32_t keys = ring_u32 + stage * F::kStage + k_lane, values = ring_u32 + stage * F::kStage + v_lane;
+    float s[G][TN][4];
+    if constexpr (Q8) {
+      uint32_t a[kQuerySteps][G][4];
+#pragma unroll
+      for (int k = 0; k < kQuerySteps; ++k)
+#pragma unroll
+        for (int h = 0; h < G; ++h) ldmatrix_x4(at_piece(keys + h * 16 * F::kRowBytes, 2 * k), a[k][h]);
+#pragma unroll
+      for (int n = 0; n < TN; ++n) {
+        int sd[kDigits][G][4];
+#pragma unroll
+        for (int d = 0; d < kDigits; ++d)
+#pragma unroll
+          for (int h = 0; h < G; ++h) sd[d][h][0] = sd[d][h][1] = sd[d][h][2] = sd[d][h][3] = 0;
+#pragma unroll
+        for (int k = 0; k < kQuerySteps; ++k)
+#pragma unroll
+          for (int d = 0; d < kDigits; ++d) {
+            const uint2 b = query(d, k, n);
+#pragma unroll
+            for (int h = 0; h < G; ++h) mma_s8(sd[d][h], a[k][h], b.x, b.y);
+          }
+#pragma unroll
+        for (int h = 0; h < G; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)  // (a digit's sum is at most 128 * 128 * 256: the upper two in 32 bits)
+            s[h][n][i] = fmaf(static_cast<float>(sd[0][h][i] * 256 + sd[1][h][i]), 256.f, static_cast<float>(sd[2][h][i]));
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int n = 0; n < TN; ++n) s[h][n][0] = s[h][n][1] = s[h][n][2] = s[h][n][3] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kQuerySteps; ++k) {
+        uint32_t a[G][4];
+#pragma unroll
+        for (int h = 0; h < G; ++h) ldmatrix_x4(at_piece(keys + h * 16 * F::kRowBytes, 2 * k), a[h]);
+#pragma unroll
+        for (int n = 0; n < TN; ++n) {
+            const uint2 b = query(0, k, n);
+#pragma unroll
+          for (int h = 0; h < G; ++h) mma<kMmaBf16>(s[h][n], a[h], b.x, b.y);
+        }
+      }
+    }
+    float ks[G][2], vs[G][2];
+    if constexpr (Q8) {
+      const float* scales = reinterpret_cast<const float*>(ring + stage * F::kStage + 2 * F::kSide);
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          ks[h][i] = scales[16 * h + 8 * i + g];
+          vs[h][i] = scales[F::kBlock + 16 * h + 8 * i + g];
+        }
+    }
+    // s: scores in the log2 domain less the running maximum (0 where there is none yet)
+    float ref[TN][2], limit[TN][2];
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const bool none = top[n][j] == -INFINITY;
+        ref[n][j] = none ? 0.f : top[n][j];
+        limit[n][j] = none ? -INFINITY : kSlack;
+      }
+    if (p.softcap > 0.f) {
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[h][n][i] = cap(Q8 ? s[h][n][i] * (factor[n][i & 1] * ks[h][i >> 1]) : s[h][n][i]) - ref[n][i & 1];
+    } else {
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[h][n][i] = fmaf(s[h][n][i], Q8 ? factor[n][i & 1] * ks[h][i >> 1] : factor[n][i & 1], -ref[n][i & 1]);
+    }
+    if (p.slopes) {  // slope (n - m), from the distance of the block's first position on
+#pragma unroll
+      for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = row_of_mine + 8 * RW * n + j;
+          const float slope = sm.slope[r], from = static_cast<float>(base + g - (first + sm.token[r])) * slope;
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[h][n][2 * i + j] += fmaf(slope, static_cast<float>(16 * h + 8 * i), from);
+        }
+    }
+    if (!all) {
+#pragma unroll
+      for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int last = first + sm.token[row_of_mine + 8 * RW * n + j] - base;  // the row sees positions of the block up to this one
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int k = 16 * h + 8 * i + g;
+              if (!((valid >> k) & 1u) || k > last || (p.window > 0 && k <= last - p.window)) s[h][n][2 * i + j] = -INFINITY;
+            }
+        }
+    }
+    // the maximum, where a score is well above it
+    bool above = false;
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+      for (int h = 0; h < G; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) above |= s[h][n][i] > limit[n][i & 1];
+    if constexpr (Q8) {
+      float least = unit_v[0][0];
+#pragma unroll
+      for (int n = 0; n < TN; ++n) least = fminf(fminf(least, unit_v[n][0]), unit_v[n][1]);
+#pragma unroll
+      for (int h = 0; h < G; ++h) above |= fmaxf(fabsf(vs[h][0]), fabsf(vs[h][1])) > 128.f * least;
+    }
+    if (__any_sync(0xFFFFFFFFu, above)) {
+#pragma unroll
+      for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float m = -INFINITY, most = 0.f;
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float v = s[h][n][2 * i + j];
+              m = fmaxf(m, v);
+              if constexpr (Q8) most = fmaxf(most, v == -INFINITY ? 0.f : fabsf(vs[h][i]));
+            }
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+          // (s is relative to ref: the maximum rises by m, where that is positive or there was none)
+          const bool none = top[n][j] == -INFINITY;
+          const float rise = none ? m : fmaxf(m, 0.f), shift = rise == -INFINITY ? 0.f : rise;
+          const float less = none ? 1.f : ex2_approx(-shift);  // (without a maximum there is nothing yet to make less)
+          top[n][j] = none ? rise : top[n][j] + rise;
+          sum[n][j] *= less;
+          float both = less;
+          if constexpr (Q8) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+            const float unit = fmaxf(unit_v[n][j], __uint_as_float(min(max(__float_as_uint(most) & 0x7F800000u, 0x04000000u), 0x7E000000u) - 0x03000000u));
+            both *= unit_v[n][j] / unit;
+            unit_v[n][j] = unit;
+          }
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[h][n][2 * i + j] -= shift;
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k) {
+            o[k][n][j] *= both;
+            o[k][n][j + 2] *= both;
+          }
+        }
+    }
+    // weights, as the second product's operand
+    uint32_t w[G][TN][2], rest[G][TN][2];
+#pragma unroll
+    for (int n = 0; n < TN; ++n) {
+      const float inv[2] = {reciprocal_of_power(unit_v[n][0]), reciprocal_of_power(unit_v[n][1])};
+#pragma unroll
+      for (int h = 0; h < G; ++h) {
+        float e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = ex2_approx(s[h][n][i]);
+        sum[n][0] += e[0] + e[2];
+        sum[n][1] += e[1] + e[3];
+        if constexpr (Q8) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e[i] *= vs[h][i >> 1] * inv[i & 1];
+          if (!all) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (s[h][n][i] == -INFINITY) e[i] = 0.f;  // (a hidden position's scale may be NaN)
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t x = pack2<kMmaBf16>(e[2 * i], e[2 * i + 1]);
+          w[h][n][i] = transpose_8x8(x);
+          if constexpr (kTwice) {
+            const float2 r = unpack2<kMmaBf16>(x);
+            rest[h][n][i] = transpose_8x8(pack2<kMmaBf16>(e[2 * i] - r.x, e[2 * i + 1] - r.y));
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      const uint32_t rows = values + h * 16 * F::kRowBytes;
+      if constexpr (Q8) {
+#pragma unroll
+        for (int k = 0; k < kSteps; k += 2) {
+          uint32_t r[4];
+          ldmatrix_x4_trans(at_piece(rows, k), r);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t x = r[2 * i] ^ 0x80808080u, y = r[2 * i + 1] ^ 0x80808080u;
+            const uint32_t a[4] = {codes_f16(x, 0x4240), codes_f16(x, 0x4341), codes_f16(y, 0x4240), codes_f16(y, 0x4341)};
+#pragma unroll
+            for (int n = 0; n < TN; ++n) {
+                    mma<false>(o[k + i][n], a, w[h][n][0], w[h][n][1]);
+              if constexpr (kTwice) mma<false>(o[k + i][n], a, rest[h][n][0], rest[h][n][1]);
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+          uint32_t a[4];
+          ldmatrix_x4_trans(at_piece(rows, 2 * k), a);
+#pragma unroll
+          for (int n = 0; n < TN; ++n) {
+                mma<kMmaBf16>(o[k][n], a, w[h][n][0], w[h][n][1]);
+            mma<kMmaBf16>(o[k][n], a, rest[h][n][0], rest[h][n][1]);
+          }
+        }
+      }
+    }
+  };
   auto block = [&](int stage, const Sequence& seq, int base) {
     const unsigned valid = sm.valid[kw][stage];
     if (!valid) return;
@@ -574,248 +812,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         }
       }
     }
-    if (NT * RW > 1 && tiles == 0) return;
-    const uint32_t keys = ring_u32 + stage * F::kStage + k_lane, values = ring_u32 + stage * F::kStage + v_lane;
-    float s[G][NT][4];
-    if constexpr (Q8 && NT > 1) {
-#pragma unroll
-      for (int h = 0; h < G; ++h)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) s[h][n][0] = s[h][n][1] = s[h][n][2] = s[h][n][3] = 0.f;
-    }
-    if constexpr (Q8) {
-      uint32_t a[kQuerySteps][G][4];
-#pragma unroll
-      for (int k = 0; k < kQuerySteps; ++k)
-#pragma unroll
-        for (int h = 0; h < G; ++h) ldmatrix_x4(at_piece(keys + h * 16 * F::kRowBytes, 2 * k), a[k][h]);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        if (!has(n)) continue;
-        int sd[kDigits][G][4];
-#pragma unroll
-        for (int d = 0; d < kDigits; ++d)
-#pragma unroll
-          for (int h = 0; h < G; ++h) sd[d][h][0] = sd[d][h][1] = sd[d][h][2] = sd[d][h][3] = 0;
-#pragma unroll
-        for (int k = 0; k < kQuerySteps; ++k)
-#pragma unroll
-          for (int d = 0; d < kDigits; ++d) {
-            const uint2 b = query(d, k, n);
-#pragma unroll
-            for (int h = 0; h < G; ++h) mma_s8(sd[d][h], a[k][h], b.x, b.y);
-          }
-#pragma unroll
-        for (int h = 0; h < G; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)  // (a digit's sum is at most 128 * 128 * 256: the upper two in 32 bits)
-            s[h][n][i] = fmaf(static_cast<float>(sd[0][h][i] * 256 + sd[1][h][i]), 256.f, static_cast<float>(sd[2][h][i]));
-      }
-    } else {
-#pragma unroll
-      for (int h = 0; h < G; ++h)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) s[h][n][0] = s[h][n][1] = s[h][n][2] = s[h][n][3] = 0.f;
-#pragma unroll
-      for (int k = 0; k < kQuerySteps; ++k) {
-        uint32_t a[G][4];
-#pragma unroll
-        for (int h = 0; h < G; ++h) ldmatrix_x4(at_piece(keys + h * 16 * F::kRowBytes, 2 * k), a[h]);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          if (!has(n)) continue;
-          const uint2 b = query(0, k, n);
-#pragma unroll
-          for (int h = 0; h < G; ++h) mma<kMmaBf16>(s[h][n], a[h], b.x, b.y);
-        }
-      }
-    }
-    float ks[G][2], vs[G][2];
-    if constexpr (Q8) {
-      const float* scales = reinterpret_cast<const float*>(ring + stage * F::kStage + 2 * F::kSide);
-#pragma unroll
-      for (int h = 0; h < G; ++h)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          ks[h][i] = scales[16 * h + 8 * i + g];
-          vs[h][i] = scales[F::kBlock + 16 * h + 8 * i + g];
-        }
-    }
-    // s: scores in the log2 domain less the running maximum (0 where there is none yet)
-    float ref[NT][2], limit[NT][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const bool none = top[n][j] == -INFINITY;
-        ref[n][j] = none ? 0.f : top[n][j];
-        limit[n][j] = none ? -INFINITY : kSlack;
-      }
-    if (p.softcap > 0.f) {
-#pragma unroll
-      for (int h = 0; h < G; ++h)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[h][n][i] = cap(Q8 ? s[h][n][i] * (factor[n][i & 1] * ks[h][i >> 1]) : s[h][n][i]) - ref[n][i & 1];
-    } else {
-#pragma unroll
-      for (int h = 0; h < G; ++h)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[h][n][i] = fmaf(s[h][n][i], Q8 ? factor[n][i & 1] * ks[h][i >> 1] : factor[n][i & 1], -ref[n][i & 1]);
-    }
-    if (p.slopes) {  // slope (n - m), from the distance of the block's first position on
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int r = row_of_mine + 8 * RW * n + j;
-          const float slope = sm.slope[r], from = static_cast<float>(base + g - (first + sm.token[r])) * slope;
-#pragma unroll
-          for (int h = 0; h < G; ++h)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) s[h][n][2 * i + j] += fmaf(slope, static_cast<float>(16 * h + 8 * i), from);
-        }
-    }
-    if (!all) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int last = first + sm.token[row_of_mine + 8 * RW * n + j] - base;  // the row sees positions of the block up to this one
-#pragma unroll
-          for (int h = 0; h < G; ++h)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int k = 16 * h + 8 * i + g;
-              if (!((valid >> k) & 1u) || k > last || (p.window > 0 && k <= last - p.window)) s[h][n][2 * i + j] = -INFINITY;
-            }
-        }
-    }
-    // the maximum, where a score is well above it
-    bool above = false;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int h = 0; h < G; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) above |= s[h][n][i] > limit[n][i & 1];
-    if constexpr (Q8) {
-      float least = unit_v[0][0];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) least = fminf(fminf(least, unit_v[n][0]), unit_v[n][1]);
-#pragma unroll
-      for (int h = 0; h < G; ++h) above |= fmaxf(fabsf(vs[h][0]), fabsf(vs[h][1])) > 128.f * least;
-    }
-    if (__any_sync(0xFFFFFFFFu, above)) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float m = -INFINITY, most = 0.f;
-#pragma unroll
-          for (int h = 0; h < G; ++h)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float v = s[h][n][2 * i + j];
-              m = fmaxf(m, v);
-              if constexpr (Q8) most = fmaxf(most, v == -INFINITY ? 0.f : fabsf(vs[h][i]));
-            }
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-          // (s is relative to ref: the maximum rises by m, where that is positive or there was none)
-          const bool none = top[n][j] == -INFINITY;
-          const float rise = none ? m : fmaxf(m, 0.f), shift = rise == -INFINITY ? 0.f : rise;
-          const float less = none ? 1.f : ex2_approx(-shift);  // (without a maximum there is nothing yet to make less)
-          top[n][j] = none ? rise : top[n][j] + rise;
-          sum[n][j] *= less;
-          float both = less;
-          if constexpr (Q8) {
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
-            const float unit = fmaxf(unit_v[n][j], __uint_as_float(min(max(__float_as_uint(most) & 0x7F800000u, 0x04000000u), 0x7E000000u) - 0x03000000u));
-            both *= unit_v[n][j] / unit;
-            unit_v[n][j] = unit;
-          }
-#pragma unroll
-          for (int h = 0; h < G; ++h)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) s[h][n][2 * i + j] -= shift;
-#pragma unroll
-          for (int k = 0; k < kSteps; ++k) {
-            o[k][n][j] *= both;
-            o[k][n][j + 2] *= both;
-          }
-        }
-    }
-    // weights, as the second product's operand
-    uint32_t w[G][NT][2], rest[G][NT][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const float inv[2] = {reciprocal_of_power(unit_v[n][0]), reciprocal_of_power(unit_v[n][1])};
-#pragma unroll
-      for (int h = 0; h < G; ++h) {
-        float e[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e[i] = ex2_approx(s[h][n][i]);
-        sum[n][0] += e[0] + e[2];
-        sum[n][1] += e[1] + e[3];
-        if constexpr (Q8) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) e[i] *= vs[h][i >> 1] * inv[i & 1];
-          if (!all) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (s[h][n][i] == -INFINITY) e[i] = 0.f;  // (a hidden position's scale may be NaN)
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t x = pack2<kMmaBf16>(e[2 * i], e[2 * i + 1]);
-          w[h][n][i] = transpose_8x8(x);
-          if constexpr (kTwice) {
-            const float2 r = unpack2<kMmaBf16>(x);
-            rest[h][n][i] = transpose_8x8(pack2<kMmaBf16>(e[2 * i] - r.x, e[2 * i + 1] - r.y));
-          }
-        }
-      }
-    }
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-      const uint32_t rows = values + h * 16 * F::kRowBytes;
-      if constexpr (Q8) {
-#pragma unroll
-        for (int k = 0; k < kSteps; k += 2) {
-          uint32_t r[4];
-          ldmatrix_x4_trans(at_piece(rows, k), r);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t x = r[2 * i] ^ 0x80808080u, y = r[2 * i + 1] ^ 0x80808080u;
-            const uint32_t a[4] = {codes_f16(x, 0x4240), codes_f16(x, 0x4341), codes_f16(y, 0x4240), codes_f16(y, 0x4341)};
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              if (!has(n)) continue;
-              mma<false>(o[k + i][n], a, w[h][n][0], w[h][n][1]);
-              if constexpr (kTwice) mma<false>(o[k + i][n], a, rest[h][n][0], rest[h][n][1]);
-            }
-          }
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-          uint32_t a[4];
-          ldmatrix_x4_trans(at_piece(rows, 2 * k), a);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            if (!has(n)) continue;
-            mma<kMmaBf16>(o[k][n], a, w[h][n][0], w[h][n][1]);
-            mma<kMmaBf16>(o[k][n], a, rest[h][n][0], rest[h][n][1]);
-          }
-        }
-      }
-    }
+    if (RW == 1 || tiles == NT) products(std::integral_constant<int, NT>(), stage, seq, base, valid, all);
+    else if (NT > 1 && tiles > 0) products(std::integral_constant<int, 1>(), stage, seq, base, valid, all);
   };
 
   // ---- the end of an item, or of the share: the rings' results are joined; whole items are finished, cut ones kept
