@@ -370,6 +370,7 @@ enum { WIDE_NONE, WIDE_I32, WIDE_I64, WIDE_F64 };
 typedef struct {
   Geometry g;
   int type, wide;
+  int bytes;       // of an element; 0 = not asked for
   int64_t device;  // -1 = host
   const void* p;
 } Described;
@@ -394,6 +395,7 @@ static int describe(PyObject* t, Described* d) {
                 : code == 0 && bits == 8  ? TYPE_I8
                                           : TYPE_OTHER;
       d->wide = v.dtype.lanes != 1 ? WIDE_NONE : code == 0 && bits == 32 ? WIDE_I32 : code == 0 && bits == 64 ? WIDE_I64 : code == 2 && bits == 64 ? WIDE_F64 : WIDE_NONE;
+      d->bytes = (bits * v.dtype.lanes + 7) / 8;
       d->device = v.device.type == 2 ? v.device.id : v.device.type == 1 ? -1 : -2;
       d->p = (const char*)v.data + v.byte_offset;
       return 1;
@@ -405,6 +407,7 @@ static int describe(PyObject* t, Described* d) {
   if (!type) return 0;
   Py_DECREF(type);  // (a tensor's type outlives it)
   d->type = type == t_bf16 ? TYPE_BF16 : type == t_f16 ? TYPE_F16 : type == t_f32 ? TYPE_F32 : type == t_i8 ? TYPE_I8 : TYPE_OTHER;
+  d->bytes = 0;
   d->wide = type == t_i32 ? WIDE_I32 : type == t_i64 ? WIDE_I64 : type == t_f64 ? WIDE_F64 : WIDE_NONE;
   return shape_of(t, &d->g) && tuple_i64(PyObject_CallMethodNoArgs(t, s_stride), d->g.stride, &n) && method_i64(t, s_get_device, &d->device) && pointer(t, &d->p);
 }
@@ -554,8 +557,7 @@ static paged_attention_fn f_paged_attention;
 static paged_attention_size_fn f_paged_attention_size;
 
 // A tensor of n dimensions with the given element type (or, type < 0, wide type) and, where they are given (>= 0), sizes; its last dimension is dense.
-static int tensor(PyObject* t, int type, int wide, int64_t device, int n, const int64_t* sizes, const char* what, Described* d) {
-  if (!describe(t, d)) return 0;
+static int shaped(Described* d, int type, int wide, int64_t device, int n, const int64_t* sizes, const char* what) {
   if (type >= 0 ? d->type != type : d->wide != wide) return refuse(what, "has another element type than the call takes");
   int same = d->g.n == n;
   for (int i = 0; same && i < n; ++i) same = sizes[i] < 0 ? d->g.size[i] <= INT32_MAX : d->g.size[i] == sizes[i];
@@ -563,6 +565,9 @@ static int tensor(PyObject* t, int type, int wide, int64_t device, int n, const 
   if (d->device != device) return refuse(what, "is not on the current device");
   if (n > 0 && d->g.stride[n - 1] != 1 && d->g.size[n - 1] != 1) return refuse(what, "must be dense in its last dimension");
   return 1;
+}
+static int tensor(PyObject* t, int type, int wide, int64_t device, int n, const int64_t* sizes, const char* what, Described* d) {
+  return describe(t, d) && shaped(d, type, wide, device, n, sizes, what);
 }
 static int dense(const Described* d, const char* what) {
   int64_t want = 1;
@@ -572,11 +577,10 @@ static int dense(const Described* d, const char* what) {
   }
   return 1;
 }
-static int type_16(PyObject* t, const char* what, int* type) {
-  Described d;
-  if (!describe(t, &d)) return 0;
-  *type = d.type;
-  return d.type == TYPE_BF16 || d.type == TYPE_F16 ? 1 : refuse(what, "has another element type than the call takes");
+static int type_16(PyObject* t, const char* what, Described* d, int* type) {
+  if (!describe(t, d)) return 0;
+  *type = d->type;
+  return d->type == TYPE_BF16 || d->type == TYPE_F16 ? 1 : refuse(what, "has another element type than the call takes");
 }
 static int no_negative_strides(const Described* d, const char* what) {
   for (int i = 0; i < d->g.n; ++i)
@@ -592,7 +596,7 @@ static int fill_rotary(PyObject* const* a, int64_t device, int64_t tokens, comfu
   if (!tensor(a[1], -1, WIDE_F64, device, 1, any, "freqs", &freqs) || !describe(a[0], &pos)) return 0;
   const int axes = pos.g.n == 2 ? (int)(pos.g.size[0] <= 4 ? pos.g.size[0] : 5) : 1;
   const int64_t one[1] = {tokens}, more[2] = {-1, tokens};
-  if (!tensor(a[0], -1, WIDE_I32, device, pos.g.n == 2 ? 2 : 1, pos.g.n == 2 ? more : one, "positions", &pos) || !no_negative_strides(&pos, "positions")) return 0;
+  if (!shaped(&pos, -1, WIDE_I32, device, pos.g.n == 2 ? 2 : 1, pos.g.n == 2 ? more : one, "positions") || !no_negative_strides(&pos, "positions")) return 0;
   if (!require(axes <= 4, "positions has more than 4 axes")) return 0;
   r->positions = pos.p;
   r->axis_stride = axes > 1 ? pos.g.stride[0] : 0;
@@ -626,7 +630,7 @@ static int fill_cache(PyObject* const* a, int type, int64_t device, comfuse_kv_c
   memset(c, 0, sizeof(*c));
   if (!describe(a[0], &k)) return 0;
   const int held = k.type == TYPE_I8 ? TYPE_I8 : type;
-  if (!tensor(a[0], held, 0, device, 4, any, "k_cache", &k) || !tensor(a[1], held, 0, device, 4, k.g.size, "v_cache", &v) || !no_negative_strides(&k, "k_cache") ||
+  if (!shaped(&k, held, 0, device, 4, any, "k_cache") || !tensor(a[1], held, 0, device, 4, k.g.size, "v_cache", &v) || !no_negative_strides(&k, "k_cache") ||
       !no_negative_strides(&v, "v_cache"))
     return 0;
   c->k = (void*)k.p;
@@ -658,12 +662,15 @@ static int fill_cache(PyObject* const* a, int type, int64_t device, comfuse_kv_c
   return 1;
 }
 // Rows [tokens, heads, D]
-static int rows_of(PyObject* t, int type, int64_t device, int64_t tokens, int64_t heads, int64_t D, const char* what, int64_t* strides, Described* d) {
+static int rows_described(Described* d, int type, int64_t device, int64_t tokens, int64_t heads, int64_t D, const char* what, int64_t* strides) {
   const int64_t sizes[3] = {tokens, heads, D};
-  if (!tensor(t, type, 0, device, 3, sizes, what, d) || !no_negative_strides(d, what)) return 0;
+  if (!shaped(d, type, 0, device, 3, sizes, what) || !no_negative_strides(d, what)) return 0;
   strides[0] = d->g.stride[0];
   strides[1] = d->g.stride[1];
   return 1;
+}
+static int rows_of(PyObject* t, int type, int64_t device, int64_t tokens, int64_t heads, int64_t D, const char* what, int64_t* strides, Described* d) {
+  return describe(t, d) && rows_described(d, type, device, tokens, heads, D, what, strides);
 }
 static int slots_of(PyObject* t, int64_t device, int64_t tokens, Described* d) {
   const int64_t sizes[1] = {tokens};
@@ -680,7 +687,7 @@ static PyObject* py_rotary(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   int type;
   memset(&d, 0, sizeof(d));
   if (!fixed_args(n, 9, "rotary") || !to_i64(a[7], &device) || !describe(a[0], &x) || !float_type(&x, "x", &type)) return NULL;
-  if (!rows_of(a[0], type, device, -1, -1, -1, "x", d.x_strides, &x) || !fill_rotary(a + 1, device, x.g.size[0], &r) ||
+  if (!rows_described(&x, type, device, -1, -1, -1, "x", d.x_strides) || !fill_rotary(a + 1, device, x.g.size[0], &r) ||
       !rows_of(a[6], type, device, x.g.size[0], x.g.size[1], x.g.size[2], "out", d.out_strides, &out) || !stream_on(a[8], device, &stream))
     return NULL;
   d.tokens = (int32_t)x.g.size[0];
@@ -705,8 +712,8 @@ static PyObject* py_cache_write(PyObject* self, PyObject* const* a, Py_ssize_t n
   int type;
   memset(&d, 0, sizeof(d));
   q.p = q_out.p = NULL;
-  if (!fixed_args(n, 16, "cache_write") || !to_i64(a[14], &device) || !type_16(a[0], "k", &type) || !fill_cache(a + 2, type, device, &c)) return NULL;
-  if (!rows_of(a[0], type, device, -1, c.heads, c.D, "k", d.k_strides, &k)) return NULL;
+  if (!fixed_args(n, 16, "cache_write") || !to_i64(a[14], &device) || !type_16(a[0], "k", &k, &type) || !fill_cache(a + 2, type, device, &c)) return NULL;
+  if (!rows_described(&k, type, device, -1, c.heads, c.D, "k", d.k_strides)) return NULL;
   const int64_t tokens = k.g.size[0];
   if (!rows_of(a[1], type, device, tokens, c.heads, c.D, "v", d.v_strides, &v) || !slots_of(a[6], device, tokens, &slots)) return NULL;
   if (!require((a[7] == Py_None) == (a[8] == Py_None), "q and q_out come together") || !require((a[9] == Py_None) == (a[10] == Py_None), "positions and freqs come together") ||
@@ -737,8 +744,8 @@ static PyObject* py_cache_read(PyObject* self, PyObject* const* a, Py_ssize_t n)
   void* stream;
   int type;
   memset(&d, 0, sizeof(d));
-  if (!fixed_args(n, 9, "cache_read") || !to_i64(a[7], &device) || !type_16(a[5], "k", &type) || !fill_cache(a, type, device, &c)) return NULL;
-  if (!rows_of(a[5], type, device, -1, c.heads, c.D, "k", d.k_strides, &k)) return NULL;
+  if (!fixed_args(n, 9, "cache_read") || !to_i64(a[7], &device) || !type_16(a[5], "k", &k, &type) || !fill_cache(a, type, device, &c)) return NULL;
+  if (!rows_described(&k, type, device, -1, c.heads, c.D, "k", d.k_strides)) return NULL;
   const int64_t tokens = k.g.size[0];
   if (!rows_of(a[6], type, device, tokens, c.heads, c.D, "v", d.v_strides, &v) || !slots_of(a[4], device, tokens, &slots) || !stream_on(a[8], device, &stream)) return NULL;
   d.tokens = (int32_t)tokens;
@@ -754,10 +761,10 @@ static int fill_attention(PyObject* const* a, int64_t device, comfuse_paged_atte
   int64_t window, max_length;
   double alpha, softcap;
   memset(d, 0, sizeof(*d));
-  if (!type_16(a[0], "q", type) || !fill_cache(a + 1, *type, device, c) || !describe(a[0], q)) return 0;
+  if (!type_16(a[0], "q", q, type) || !fill_cache(a + 1, *type, device, c)) return 0;
   const int dims = q->g.n == 3 ? 3 : 4;  // [sequences, heads, D]: one new token each
   const int64_t three[3] = {-1, -1, c->D}, four[4] = {-1, -1, -1, c->D};
-  if (!tensor(a[0], *type, 0, device, dims, dims == 3 ? three : four, "q", q) || !no_negative_strides(q, "q")) return 0;
+  if (!shaped(q, *type, 0, device, dims, dims == 3 ? three : four, "q") || !no_negative_strides(q, "q")) return 0;
   const int64_t batch = q->g.size[0], width[2] = {batch, -1};
   if (!tensor(a[5], -1, WIDE_I32, device, 2, width, "page_table", table) || !no_negative_strides(table, "page_table")) return 0;
   if (a[6] == Py_None) alpha = 0.;
@@ -801,7 +808,10 @@ static PyObject* py_paged_attention(PyObject* self, PyObject* const* a, Py_ssize
     void* p;
     if (!describe(a[14], &ws)) return NULL;
     if (ws.device != device) return refuse("workspace", "is not on the current device"), NULL;
-    if (!dense(&ws, "workspace") || !workspace_of(a[14], &p, &ws_bytes)) return NULL;
+    if (!dense(&ws, "workspace")) return NULL;
+    ws_bytes = (size_t)ws.bytes;
+    for (int i = 0; i < ws.g.n; ++i) ws_bytes *= (size_t)ws.g.size[i];
+    if (!ws.bytes && !workspace_of(a[14], &p, &ws_bytes)) return NULL;
   }
   if (!stream_on(a[16], device, &stream)) return NULL;
   d.out_strides[0] = out.g.stride[0];

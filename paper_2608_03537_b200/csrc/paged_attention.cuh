@@ -59,7 +59,7 @@ struct Form {
   static constexpr int kQueryStep = 8 * kRows + (Q8 ? 8 : 0);     // words of a step of all rows (8 bits: steps of a row on other banks)
   static constexpr int kQuery = DH / (Q8 ? 32 : 16) * kQueryStep * 4 * (Q8 ? kDigits : 1);
   static constexpr int kSmall = 256 + 4 * 32 * kKeyWarps + kRows * (8 * kKeyWarps + 24);
-  static constexpr int kCtasPerSm = DH == 256 || (DH == 128 && RW > 1) ? 1 : 2;
+  static constexpr int kCtasPerSm = DH == 256 || (RW > 1 && (DH == 128 || Q8)) ? 1 : 2;
   static constexpr int kSmem = kCtasPerSm == 2 ? 113 * 1024 : 226 * 1024;  // what a CTA may take
   static constexpr int kMostStages = (kSmem - kJoin - kQuery - kSmall) / (kStage * kKeyWarps);
   static constexpr int kStages = kMostStages < 8 ? kMostStages : 8;
@@ -1024,32 +1024,40 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttention
     first = blockIdx.x;
     cut = behind < line.total && at.at > F::kSetUp && item + F::kSetUp >= line.begin(blockIdx.x);
   }
-  griddep_wait();
   const int r = blockIdx.y, row = (at.hr % p.row_blocks) * F::kRows + r;
-  if (!cut || row >= p.rows) return;
-  const int n = static_cast<int>(line.owner(item + F::kSetUp + units - 1) - first) + 1;  // parts
+  const bool mine = cut && row < p.rows;
+  const int n = mine ? static_cast<int>(line.owner(item + F::kSetUp + units - 1) - first) + 1 : 0;  // parts
   const int slot = item <= line.begin(first) ? 0 : 1;  // (a share that begins in front of the item has some of another's first)
   const float* first_part = p.part + first * part_floats(F::kRows, DH) + (slot * F::kRows + r) * (DH + 4);
   const float* next_part = p.part + (first + 1) * part_floats(F::kRows, DH) + r * (DH + 4);
   auto part = [&](int i) { return i == 0 ? first_part : next_part + (i - 1) * part_floats(F::kRows, DH); };
+  const int stripe = tid / kAcross, col = (tid % kAcross) * 4;
+  const int head = at.hr / p.row_blocks, token = p.groups.of(row), h = head * p.group + row - token * p.group;
+  char* out = p.out + at.b * p.out_batch + token * p.out_token + h * p.out_head;
+  float* lse = p.lse ? p.lse + (static_cast<long long>(at.b) * p.tokens + token) * p.heads * p.group + h : nullptr;
+  griddep_wait();
+  if (!mine) return;
 
   // the first parts of this thread's stripe are on their way while the weights are worked out
   constexpr int kEarly = 4;
-  const int stripe = tid / kAcross, col = (tid % kAcross) * 4;
   float4 early[kEarly];
 #pragma unroll
   for (int i = 0; i < kEarly; ++i) early[i] = stripe + i * kStripes < n ? *reinterpret_cast<const float4*>(part(stripe + i * kStripes) + col) : make_float4(0.f, 0.f, 0.f, 0.f);
-  float m = -INFINITY, l = 0.f;
-  for (int i = lane; i < n; i += 32) m = fmaxf(m, part(i)[DH]);
+  float2 stats = lane < n ? *reinterpret_cast<const float2*>(part(lane) + DH) : make_float2(-INFINITY, 0.f);  // (of the first 32: more are read again)
+  float m = stats.x;
+  for (int i = lane + 32; i < n; i += 32) m = fmaxf(m, part(i)[DH]);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+  float l = 0.f;
   for (int i = lane; i < n; i += 32) {
-    const float pm = part(i)[DH], w = pm == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : ex2_approx(pm - m);
-    l += part(i)[DH + 1] * w;
+    if (i >= 32) stats = *reinterpret_cast<const float2*>(part(i) + DH);
+    const float w = stats.x == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : ex2_approx(stats.x - m);
+    l = fmaf(stats.y, w, l);
     if (tid < 32) s_weight[i] = w;
   }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
   __syncthreads();
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](const float4& x, float w) {
@@ -1058,7 +1066,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttention
 #pragma unroll
   for (int i = 0; i < kEarly; ++i)
     if (stripe + i * kStripes < n) add(early[i], s_weight[stripe + i * kStripes]);
-#pragma unroll 4
+#pragma unroll 8
   for (int i = stripe + kEarly * kStripes; i < n; i += kStripes) add(*reinterpret_cast<const float4*>(part(i) + col), s_weight[i]);
   s_sum[stripe][tid % kAcross] = v;
   __syncthreads();
@@ -1068,15 +1076,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttention
     const float4 x = s_sum[i][tid];
     v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
   }
-  const int head = at.hr / p.row_blocks, token = p.groups.of(row), h = head * p.group + row - token * p.group;
-  char* out = p.out + at.b * p.out_batch + token * p.out_token + h * p.out_head;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
   const float y[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
   uint32_t packed[2];
   Elem<DT>::pack(y, packed);
   if (col < p.D && COMFUSE_IN_BOUNDS(col + 4 <= p.D && row < p.rows && at.b < p.batch, p.status)) st_8(out + 2 * col, packed);
-  if (p.lse && tid == 0 && COMFUSE_IN_BOUNDS(at.b < p.batch && token < p.tokens, p.status))
-    p.lse[(static_cast<long long>(at.b) * p.tokens + token) * p.heads * p.group + h] = log_sum(m, l);
+  if (lse && tid == 0 && COMFUSE_IN_BOUNDS(at.b < p.batch && token < p.tokens, p.status)) *lse = log_sum(m, l);
 }
 
 // ------------------------------------------------------------------------------------------------ launches

@@ -239,7 +239,7 @@ def test_structures_are_those_of_the_header(tmp_path):
     assert got == want
 
 
-STORE = re.compile(r"\b(?:st_16|st_8|store_piece<\w+>|Elem<\w+>::put)\(|(?:c\.scale|p\.lse|part)\[[^\n]*?\] =|\*reinterpret_cast<uint32_t\*>\(to\) =")
+STORE = re.compile(r"\b(?:st_16|st_8|store_piece<\w+>|Elem<\w+>::put)\(|(?:c\.scale|p\.lse|part)\[[^\n]*?\] =|\*reinterpret_cast<uint32_t\*>\(to\) =|\*lse =")
 STORES = {"kv_cache.cu": 12, "paged_attention.cuh": 10}
 
 
