@@ -219,7 +219,7 @@ PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, b
   };
   double best = start + 2.9 + std::max(1.0, static_cast<double>(items) * (static_cast<double>(units) * mean + f.set_up) / static_cast<double>(slots)) * unit_us(std::min(slots, items * units));
   for (int c = 1; c <= 16 && (c == 1 || c <= units); c *= 2) {
-    const int64_t ctas = items * c, fit = f.ctas_per_sm * (c == 16 ? 112 : c == 8 ? 128 : 148), waves = (ctas + fit - 1) / fit;
+    const int64_t ctas = items * c, fit = f.ctas_per_sm * (c == 16 ? 112 : c == 8 ? 120 : 148), waves = (ctas + fit - 1) / fit;
     const double us = static_cast<double>(waves) * (start + static_cast<double>((units + c - 1) / c) * unit_us(std::min(ctas, fit)) * (waves == 1 ? 1.0 : mean)) + (c > 1 ? 1.2 : 0.0);
     if (us < best && ctas <= 0x7FFFFFFF) plan.cluster = c, best = us;
   }

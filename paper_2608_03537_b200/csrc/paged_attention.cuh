@@ -8,8 +8,9 @@
 //   * The call's work is a line of units of some positions (sequence by sequence, key head by key head), cut into equal shares, one for each of the CTAs that fit on the
 //     GPU: whatever the lengths, all finish together.  A CTA finds its share from the lengths themselves.  An item (sequence, key head) that lies in one share is
 //     finished there; one that is cut leaves a partial sum, maximum and weighted values for each share, and a second kernel joins them, in order.
-//   * Calls of few positions, whose time is latency, take clusters instead: each item is one cluster's, its units in equal parts the CTAs', which read one another's results through
-//     distributed shared memory.  One kernel, no shares to find, no partial results in memory.
+//   * Calls of few positions, whose time is latency, take clusters instead: each item is one cluster's, its units in equal parts the CTAs', which send one another their results through
+//     distributed shared memory, each those of some outputs.  One kernel, no shares to find, no partial results in memory.  (Results that are read from the others instead of sent by them: 1000
+//     positions 6.7 us; a read takes 200 ns.)
 //   * A unit is a block of 16 or 32 positions for each of the CTA's key warps.  A key warp is on its own: it fetches its blocks by 16-byte asynchronous copies, several blocks ahead and
 //     across the ends of items, into a ring of its own, and keeps a running maximum, sum and weighted values; no barrier but at the end of an item, where they are joined.  Where there are
 //     more rows of queries than a warp holds, several warps share a ring and its fetching, each with rows of its own, and meet once a block.
@@ -198,15 +199,8 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
 }
 // 1 / x for x = 2^n, |n| < 127; anything for 0
 __device__ __forceinline__ float reciprocal_of_power(float x) { return __uint_as_float(0x7F000000u - __float_as_uint(x)); }
-__device__ __forceinline__ float2 ld_cluster_f32x2(uint32_t at) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
-  return v;
-}
-__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t at) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
-  return v;
+__device__ __forceinline__ void st_cluster_f32x4(uint32_t at, const float* v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
 }
 // log of a sum whose terms were divided by 2^m; nothing: -inf
 __device__ __forceinline__ float log_sum(float m, float l) {
@@ -243,7 +237,6 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
     unsigned valid[F::kKeyWarps][8];                               // of the blocks in the ring: positions that are there
   };
   static_assert(sizeof(Small) <= F::kSmall, "room for what is small");
-  static_assert(F::kRows * (DH + 4) * 4 <= S * F::kStage * F::kKeyWarps, "a cluster's CTA keeps its results where its rings were");
   Small& sm = *reinterpret_cast<Small*>(reinterpret_cast<char*>(s_query) + F::kQuery);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int kw = RW == 1 ? warp : warp / RW, rw = RW == 1 ? 0 : warp % RW;  // which ring, which rows
@@ -578,7 +571,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         }
       }
     }
-    float ks[G][2], vs[G][2];
+    [[maybe_unused]] float ks[G][2], vs[G][2];
     if constexpr (Q8) {
       const float* scales = reinterpret_cast<const float*>(ring + stage * F::kStage + 2 * F::kSide);
 #pragma unroll
@@ -662,7 +655,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
       for (int n = 0; n < TN; ++n)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          float m = -INFINITY, most = 0.f;
+          float m = -INFINITY;
+          [[maybe_unused]] float most = 0.f;
 #pragma unroll
           for (int h = 0; h < G; ++h)
 #pragma unroll
@@ -699,7 +693,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         }
     }
     // weights, as the second product's operand
-    uint32_t w[G][TN][2], rest[G][TN][2];
+    uint32_t w[G][TN][2];
+    [[maybe_unused]] uint32_t rest[G][TN][2];
 #pragma unroll
     for (int n = 0; n < TN; ++n) {
       const float inv[2] = {reciprocal_of_power(unit_v[n][0]), reciprocal_of_power(unit_v[n][1])};
@@ -819,7 +814,14 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
   // ---- the end of an item, or of the share: the rings' results are joined; whole items are finished, cut ones kept
   // A thread adds up kMine columns of every kJoinColumns, of one of the 8 RW rows that a tile of each row warp makes.
   constexpr int kMine = 8 * RW * F::kJoinColumns / F::kThreads, kAcross = F::kJoinColumns / kMine;
-  // `part`: where the rows of a cut item go (a cluster: into its own shared memory).
+  // `parts`: where the rows of a cut item go.  A cluster: pieces of four columns to the CTAs in turn, statistics to all.
+  struct Sent {
+    float2 stats[CLUSTER ? 16 : 1][F::kRows];       // by sender
+    float4 values[CLUSTER ? F::kRows * DH / 4 + 16 : 1];  // by sender, its pieces for this CTA
+  };
+  static_assert(sizeof(Sent) <= S * F::kStage * F::kKeyWarps, "what a cluster's CTAs send lies where the rings were");
+  Sent& sent = *reinterpret_cast<Sent*>(smem);
+  int here = 0, sent_each = 0;  // rows, pieces of a sender
   auto end_item = [&](bool whole, float* parts) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -858,6 +860,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
       if (there && tid % kAcross == 0) {
         if (whole) {
           if (p.lse && COMFUSE_IN_BOUNDS(sm.lse[row] < p.batch * p.tokens * p.heads * p.group, p.status)) p.lse[sm.lse[row]] = log_sum(m, l);
+        } else if constexpr (CLUSTER) {
+          for (int k = 0; k < p.cluster; ++k) st_cluster_f32x2(map_to_cta(smem_u32(&sent.stats[rank][row]), k), m, l);
         } else if (COMFUSE_IN_BOUNDS(row < F::kRows, p.status)) {
           part[DH] = m;
           part[DH + 1] = l;
@@ -900,6 +904,14 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
             else if constexpr (kMine == 4) st_8(to, y);
             else *reinterpret_cast<uint32_t*>(to) = y[0];
           }
+        } else if constexpr (CLUSTER) {
+#pragma unroll
+          for (int j = 0; j < kMine; j += 4) {
+            const int piece = (row * DH + at + j) / 4, to = piece % p.cluster;
+            const uint32_t where = map_to_cta(smem_u32(&sent.values[rank * sent_each + piece / p.cluster]), to);
+            if constexpr (kMine >= 4) st_cluster_f32x4(where, v + j);
+            else st_cluster_f32x2(where + (at & 2) * 4, v[0], v[1]);
+          }
         } else if (COMFUSE_IN_BOUNDS(row < F::kRows, p.status)) {
 #pragma unroll
           for (int j = 0; j < kMine; j += 2) *reinterpret_cast<float2*>(part + at + j) = make_float2(v[j], v[j + 1]);
@@ -935,25 +947,23 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         end_item(true, nullptr);
         break;
       }
-      // The cluster's results: each CTA's in its own shared memory (the rings are done with), read by all for some of the outputs each.
       cp_async_wait<0>();
-      __syncthreads();
-      float* mine = reinterpret_cast<float*>(smem);
-      end_item(false, mine);
-      cluster_sync_all();
-      const uint32_t mine_u32 = smem_u32(mine);
-      const int head = p.row_blocks == 1 ? hr : hr / p.row_blocks, row0 = (hr - head * p.row_blocks) * F::kRows, here = min(F::kRows, p.rows - row0);
-      for (int i = rank + p.cluster * tid; i < here * (DH / 4); i += p.cluster * F::kThreads) {
-        const int r = i / (DH / 4), col = (i % (DH / 4)) * 4;
-        const uint32_t stats = mine_u32 + (r * (DH + 4) + DH) * 4, values = mine_u32 + (r * (DH + 4) + col) * 4;
-        float m = -INFINITY;
-        for (int k = 0; k < p.cluster; ++k) m = fmaxf(m, ld_cluster_f32x2(map_to_cta(stats, k)).x);
-        float l = 0.f;
+      const int head = p.row_blocks == 1 ? hr : hr / p.row_blocks;
+      here = min(F::kRows, p.rows - (hr - head * p.row_blocks) * F::kRows);
+      sent_each = (here * (DH / 4) + p.cluster - 1) / p.cluster;
+      cluster_sync_all();  // every CTA's rings are done with
+      end_item(false, nullptr);
+      cluster_sync_all();  // (behind it nobody writes into another CTA's shared memory)
+      for (int i = tid; i < sent_each; i += F::kThreads) {
+        const int piece = i * p.cluster + rank, r = piece / (DH / 4), col = (piece % (DH / 4)) * 4;
+        if (r >= here) continue;
+        float m = -INFINITY, l = 0.f;
+        for (int k = 0; k < p.cluster; ++k) m = fmaxf(m, sent.stats[k][r].x);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int k = 0; k < p.cluster; ++k) {
-          const float2 s = ld_cluster_f32x2(map_to_cta(stats, k));
-          const float4 x = ld_cluster_f32x4(map_to_cta(values, k));
+          const float2 s = sent.stats[k][r];
+          const float4 x = sent.values[k * sent_each + i];
           const float w = s.x == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : ex2_approx(s.x - m);
           l = fmaf(s.y, w, l);
           v.x = fmaf(x.x, w, v.x); v.y = fmaf(x.y, w, v.y); v.z = fmaf(x.z, w, v.z); v.w = fmaf(x.w, w, v.w);
@@ -965,7 +975,6 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
         if (col < p.D && COMFUSE_IN_BOUNDS(col + 4 <= p.D && r < here, p.status)) st_8(p.out + sm.out[r] + 2 * col, packed);
         if (p.lse && col == 0 && COMFUSE_IN_BOUNDS(sm.lse[r] < p.batch * p.tokens * p.heads * p.group, p.status)) p.lse[sm.lse[r]] = log_sum(m, l);
       }
-      cluster_sync_all();  // (nobody reads another CTA's shared memory behind it)
       break;
     }
     if (unit == seq.units || n + 1 == count) {
