@@ -214,12 +214,12 @@ PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, b
   const int di = DH == 64 ? 0 : DH == 128 ? 1 : 2, ri = plan.rows == 8 ? 0 : plan.rows == 16 ? 1 : plan.rows == 32 ? 2 : 3;
   const double start = kStart[quantized][di][ri], unit = kUnit[quantized][di][ri], mean = batch > 1 ? 0.75 : 1.0;
   auto unit_us = [&](int64_t ctas) {
-    const double n = static_cast<double>(std::min(ctas, slots));
+    const double n = static_cast<double>(ctas);
     return std::max(unit * (1.0 + 0.25 * std::max(0.0, n / 148 - 1.0)), f.unit_bytes * n / 6e6);
   };
   double best = start + 2.9 + std::max(1.0, static_cast<double>(items) * (static_cast<double>(units) * mean + f.set_up) / static_cast<double>(slots)) * unit_us(std::min(slots, items * units));
   for (int c = 1; c <= 16 && (c == 1 || c <= units); c *= 2) {
-    const int64_t ctas = items * c, fit = f.ctas_per_sm * (c == 16 ? 112 : c == 8 ? 120 : 148), waves = (ctas + fit - 1) / fit;
+    const int64_t ctas = items * c, fit = f.cluster_ctas_per_sm * (c == 16 ? 112 : c == 8 ? 120 : 148), waves = (ctas + fit - 1) / fit;
     const double us = static_cast<double>(waves) * (start + static_cast<double>((units + c - 1) / c) * unit_us(std::min(ctas, fit)) * (waves == 1 ? 1.0 : mean)) + (c > 1 ? 1.2 : 0.0);
     if (us < best && ctas <= 0x7FFFFFFF) plan.cluster = c, best = us;
   }

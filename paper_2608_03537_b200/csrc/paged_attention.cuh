@@ -41,7 +41,7 @@ constexpr float kSlack = 8.f;  // log2 of what a weight may exceed 1 by
 constexpr int kDigits = 3;     // of a query, 8 bits
 
 // Sizes of an instance: D up to DH, NT tiles of eight queries a warp, RW warps with rows of their own to a ring.
-template <bool Q8, int DH, int NT, int RW>
+template <bool Q8, int DH, int NT, int RW, bool CLUSTER>
 struct Form {
   static constexpr int kRowBytes = DH * (Q8 ? 1 : 2);
   static constexpr int kPieces = kRowBytes / 16;                  // of a row
@@ -60,8 +60,9 @@ struct Form {
   static constexpr int kQueryStep = 8 * kRows + (Q8 ? 8 : 0);     // words of a step of all rows (8 bits: steps of a row on other banks)
   static constexpr int kQuery = DH / (Q8 ? 32 : 16) * kQueryStep * 4 * (Q8 ? kDigits : 1);
   static constexpr int kSmall = 256 + 4 * 32 * kKeyWarps + kRows * (8 * kKeyWarps + 24);
-  static constexpr int kCtasPerSm = DH == 256 || (RW > 1 && (DH == 128 || Q8)) ? 1 : 2;
-  static constexpr int kSmem = kCtasPerSm == 2 ? 113 * 1024 : 226 * 1024;  // what a CTA may take
+  static constexpr int kCtasPerSm = DH == 256 || (RW > 1 && (DH == 128 || Q8)) ? 1 : CLUSTER && DH == 64 && NT == 1 ? 3 : 2;
+  // (Three CTAs an SM with rings of two blocks: 24 x 16 items of 512 positions, D = 64, 12.7 us where two take 17.8; one sequence of 131072 by shares 58 us instead of 48.)
+  static constexpr int kSmem = kCtasPerSm == 3 ? 75 * 1024 : kCtasPerSm == 2 ? 113 * 1024 : 226 * 1024;  // what a CTA may take
   static constexpr int kMostStages = (kSmem - kJoin - kQuery - kSmall) / (kStage * kKeyWarps);
   static constexpr int kStages = kMostStages < 8 ? kMostStages : 8;
   static constexpr int kBytes = kStages * kStage * kKeyWarps + kJoin + kQuery + kSmall;
@@ -215,8 +216,8 @@ __device__ __forceinline__ int place_of(int r, int c) {
 
 // ------------------------------------------------------------------------------------------------ the kernel
 template <int DT, bool Q8, int DH, int NT, int RW, bool CLUSTER>
-__global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, NT, RW>::kCtasPerSm) attention_kernel(const PagedAttentionParams p) {
-  using F = Form<Q8, DH, NT, RW>;
+__global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<Q8, DH, NT, RW, CLUSTER>::kCtasPerSm) attention_kernel(const PagedAttentionParams p) {
+  using F = Form<Q8, DH, NT, RW, CLUSTER>;
   constexpr bool kBf16 = DT == COMFUSE_DTYPE_BF16;  // of queries and outputs
   constexpr bool kMmaBf16 = kBf16 && !Q8;           // of the second product: 8-bit codes are exact in fp16
   // A weight in 16 bits is off by half a step of its type, which behind a sum over like terms is as much as the output's own rounding.  So the weights go in twice, rounded and what
@@ -1002,7 +1003,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW>::kThreads, Form<Q8, DH, N
 constexpr int kJoinThreads = 256;
 template <int DT, bool Q8, int DH, int NT, int RW>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttentionParams p, const int by_item) {
-  using F = Form<Q8, DH, NT, RW>;
+  using F = Form<Q8, DH, NT, RW, false>;
   constexpr int kAcross = DH / 4, kStripes = kJoinThreads / kAcross;  // threads of a row, four columns each; every kStripes-th part is one stripe's
   constexpr int kMost = 296;                                          // parts
   __shared__ float s_weight[kMost];
@@ -1108,7 +1109,7 @@ cudaError_t make_ready(const void* kernel, int bytes, bool clusters, std::atomic
 
 template <int DT, bool Q8, int DH, int NT, int RW, bool CLUSTER>
 cudaError_t launch_instance(const PagedAttentionPlan& plan, const PagedAttentionParams& p, cudaStream_t stream) {
-  using F = Form<Q8, DH, NT, RW>;
+  using F = Form<Q8, DH, NT, RW, CLUSTER>;
   static std::atomic<unsigned long long> ready{0};
   const auto kernel = attention_kernel<DT, Q8, DH, NT, RW, CLUSTER>;
   cudaError_t e = make_ready(reinterpret_cast<const void*>(kernel), F::kBytes, CLUSTER, &ready);
@@ -1165,12 +1166,12 @@ cudaError_t launch_type(const PagedAttentionPlan& plan, const PagedAttentionPara
 
 // What a plan needs to know of the instance that runs it.
 struct FormFacts {
-  int unit, block, ctas_per_sm, set_up, unit_bytes;
+  int unit, block, ctas_per_sm, cluster_ctas_per_sm, set_up, unit_bytes;
 };
 template <bool Q8, int DH, int NT, int RW>
 constexpr FormFacts facts_of() {
-  using F = Form<Q8, DH, NT, RW>;
-  return {F::kUnit, F::kBlock, F::kCtasPerSm, F::kSetUp, F::kStage * F::kKeyWarps};
+  using F = Form<Q8, DH, NT, RW, false>;
+  return {F::kUnit, F::kBlock, F::kCtasPerSm, Form<Q8, DH, NT, RW, true>::kCtasPerSm, F::kSetUp, F::kStage * F::kKeyWarps};
 }
 template <bool Q8, int DH>
 FormFacts facts(int rows) {
