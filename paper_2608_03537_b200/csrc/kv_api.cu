@@ -206,22 +206,25 @@ PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, b
   const int64_t slots = 148 * f.ctas_per_sm;
   // Items by clusters, or equal shares and a second kernel?  By estimated times (us): a CTA's start and end, and a unit alone, as measured on one sequence of 100 .. 16000 positions (rows: 16, 8 bits;
   // D up to 64, 128, 256; columns: 8, 16, 32, 64 query rows); where CTAs share SMs a unit takes a quarter longer, where they take all of HBM its bytes at 6 TB/s.  A second kernel costs 2.9, a
-  // cluster's joining 1.2; clusters of 8 and 16 leave some SMs idle.  Of a batch's lengths only the largest is known: three quarters of it are taken for the mean.  Over 210 calls of 1 .. 64
-  // sequences of 100 .. 16000 positions the choice is 3 % slower than the best of the six would be, in the geometric mean; shares alone 15 %.
-  static constexpr float kStart[2][3][4] = {{{3.1f, 4.0f, 4.1f, 4.5f}, {3.4f, 4.8f, 4.9f, 5.1f}, {4.4f, 6.4f, 6.4f, 6.9f}}, {{4.3f, 5.6f, 6.6f, 7.8f}, {4.3f, 6.1f, 6.4f, 6.7f}, {5.2f, 7.6f, 7.7f, 9.2f}}};
-  static constexpr float kUnit[2][3][4] = {{{0.82f, 0.99f, 1.57f, 1.56f}, {0.82f, 0.95f, 1.40f, 1.42f}, {1.11f, 1.40f, 2.15f, 2.20f}},
-                                           {{0.84f, 1.21f, 2.00f, 1.90f}, {0.99f, 1.55f, 1.40f, 1.38f}, {0.96f, 1.81f, 2.34f, 2.33f}}};
+  // cluster's joining 1.2; clusters of 8 and 16 leave some SMs idle, and clusters that do not fit at once are not taken.  Of a batch's lengths only the largest is known: 0.6 of it is
+  // taken for the mean.  Over 300 calls of 1 .. 64 sequences of 100 .. 16000 positions the choice is 1.5 % slower than the best of the six would be, in the geometric mean; shares alone 15 %.
+  static constexpr float kStart[2][3][4] = {{{3.1f, 3.9f, 4.1f, 4.3f}, {3.0f, 4.4f, 5.4f, 5.7f}, {4.2f, 6.0f, 6.3f, 6.5f}}, {{4.5f, 6.2f, 6.4f, 6.8f}, {4.8f, 6.9f, 7.7f, 6.5f}, {5.4f, 8.2f, 8.5f, 10.5f}}};
+  static constexpr float kUnit[2][3][4] = {{{0.82f, 0.98f, 1.30f, 1.47f}, {0.86f, 0.96f, 1.03f, 1.06f}, {1.12f, 1.25f, 1.63f, 1.96f}},
+                                           {{0.85f, 1.08f, 1.34f, 1.36f}, {1.03f, 1.41f, 1.22f, 1.26f}, {0.97f, 1.59f, 2.03f, 2.10f}}};
+  constexpr double kLaunch = 2.5;  // of the start: once, however many rounds of CTAs there are
   const int di = DH == 64 ? 0 : DH == 128 ? 1 : 2, ri = plan.rows == 8 ? 0 : plan.rows == 16 ? 1 : plan.rows == 32 ? 2 : 3;
-  const double start = kStart[quantized][di][ri], unit = kUnit[quantized][di][ri], mean = batch > 1 ? 0.75 : 1.0;
+  const double start = kStart[quantized][di][ri], unit = kUnit[quantized][di][ri], mean = batch > 1 ? 0.6 : 1.0;
   auto unit_us = [&](int64_t ctas) {
     const double n = static_cast<double>(ctas);
     return std::max(unit * (1.0 + 0.25 * std::max(0.0, n / 148 - 1.0)), f.unit_bytes * n / 6e6);
   };
-  double best = start + 2.9 + std::max(1.0, static_cast<double>(items) * (static_cast<double>(units) * mean + f.set_up) / static_cast<double>(slots)) * unit_us(std::min(slots, items * units));
-  for (int c = 1; c <= 16 && (c == 1 || c <= units); c *= 2) {
-    const int64_t ctas = items * c, fit = f.cluster_ctas_per_sm * (c == 16 ? 112 : c == 8 ? 120 : 148), waves = (ctas + fit - 1) / fit;
-    const double us = static_cast<double>(waves) * (start + static_cast<double>((units + c - 1) / c) * unit_us(std::min(ctas, fit)) * (waves == 1 ? 1.0 : mean)) + (c > 1 ? 1.2 : 0.0);
-    if (us < best && ctas <= 0x7FFFFFFF) plan.cluster = c, best = us;
+  double best = start + 2.9 + std::max(1.0, static_cast<double>(items) * (static_cast<double>(units) * mean + 2 * f.set_up) / static_cast<double>(slots)) * unit_us(std::min(slots, items * units));
+  for (int c = 1; c <= 16; c *= 2) {
+    const int64_t ctas = items * c, fit = f.cluster_ctas_per_sm * (c == 16 ? 112 : c == 8 ? 120 : 148), rounds = (ctas + fit - 1) / fit;
+    if ((c > 1 && (c > units || rounds > 1)) || ctas > 0x7FFFFFFF) break;
+    const double each = static_cast<double>((units + c - 1) / c) * unit_us(std::min(ctas, fit)) * (rounds == 1 ? 1.0 : mean);
+    const double us = kLaunch + static_cast<double>(rounds) * (start - kLaunch + each) + (c > 1 ? 1.2 : 0.0);
+    if (us < best) plan.cluster = c, best = us;
   }
   if (forced_cluster() >= 0 && items * 16 <= 0x7FFFFFFF) plan.cluster = forced_cluster();
   if (plan.cluster > 0) {
