@@ -8,14 +8,21 @@
 
 namespace comfuse {
 
-// Division of 32-bit numbers by a divisor known on the host: the high half of n * ceil(2^64 / d) is n / d for every n < 2^32.
+// Division of numbers below 2^31 by a divisor known on the host: with l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1 the quotient is floor(n m / 2^(31 + l)), since
+// n m exceeds 2^(31 + l) n / d by at most n < 2^31, less than 2^(31 + l) / d.  m fits in 32 bits; d = 1 stands apart.
 struct Divisor {
-  unsigned long long inverse;  // 0: d = 1
-  unsigned d;
+  unsigned m, shift, d;
   Divisor() = default;
-  explicit Divisor(unsigned by) : inverse(by > 1 ? ~0ull / by + 1 : 0), d(by) {}
+  explicit Divisor(unsigned by) : m(0), shift(0), d(by) {
+    if (by < 2) return;
+    unsigned l = 1;
+    while ((1ull << l) < by) ++l;
+    m = static_cast<unsigned>((1ull << (31 + l)) / by + 1);
+    shift = l - 1;
+  }
+  unsigned divide(unsigned n) const { return m ? static_cast<unsigned>((static_cast<unsigned long long>(n) * m) >> 32) >> shift : n; }
 #ifdef __CUDACC__
-  __device__ __forceinline__ unsigned of(unsigned n) const { return inverse ? static_cast<unsigned>(__umul64hi(n, inverse)) : n; }
+  __device__ __forceinline__ unsigned of(unsigned n) const { return m ? __umulhi(n, m) >> shift : n; }
 #endif
 };
 

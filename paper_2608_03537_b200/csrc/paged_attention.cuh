@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
   const bool my_piece_there = my_piece * 16 < p.D * (Q8 ? 1 : 2);
   const uint32_t my_dst = ring_u32 + my_row * F::kRowBytes + place_of<F::kPieces>(my_row, my_piece) * 16;
   const bool whole_pages = p.page_size.d % F::kBlock == 0;  // a block lies in one page
+  const bool dense_rows = p.kc.row == F::kRowBytes && p.vc.row == F::kRowBytes;  // known distances
   const bool same_strides = p.kc.page == p.vc.page && p.kc.row == p.vc.row;
   // (the strides of pages and rows fit in 32 bits)
   auto offset = [](unsigned page, unsigned row, const CacheSide& c) {
@@ -357,15 +358,24 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
           const int first = f_line - my_pos + my_row;
           const char* k = f_k + offset(f_page, first, p.kc);
           const char* v = f_v + offset(f_page, first, p.vc);
-          const long long k_step = kRowStep * p.kc.row, v_step = kRowStep * p.vc.row;
           if (my_piece_there) {
+            if (dense_rows) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-              const uint32_t to = (F::kPieces >= 8 ? dst ^ ((i * kRowStep & 7) << 4) : dst) + i * kRowStep * F::kRowBytes;
-              cp_async_16(to, k, true);
-              cp_async_16(to + F::kSide, v, true);
-              k += k_step;
-              v += v_step;
+              for (int i = 0; i < kLoads; ++i) {
+                const uint32_t to = (F::kPieces >= 8 ? dst ^ ((i * kRowStep & 7) << 4) : dst) + i * kRowStep * F::kRowBytes;
+                cp_async_16(to, k + i * kRowStep * F::kRowBytes, true);
+                cp_async_16(to + F::kSide, v + i * kRowStep * F::kRowBytes, true);
+              }
+            } else {
+              const long long k_step = kRowStep * p.kc.row, v_step = kRowStep * p.vc.row;
+#pragma unroll
+              for (int i = 0; i < kLoads; ++i) {
+                const uint32_t to = (F::kPieces >= 8 ? dst ^ ((i * kRowStep & 7) << 4) : dst) + i * kRowStep * F::kRowBytes;
+                cp_async_16(to, k, true);
+                cp_async_16(to + F::kSide, v, true);
+                k += k_step;
+                v += v_step;
+              }
             }
           }
         } else {
