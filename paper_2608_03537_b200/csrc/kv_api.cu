@@ -157,6 +157,8 @@ comfuse_status_t check_attention(const comfuse_paged_attention_desc_t* d, const 
   const int64_t d_ = c->D;
   CHECK_STRIDES(d->q_strides, 2, d->batch, d->tokens, d->q_heads);
   CHECK_STRIDES(d->out_strides, 2, d->batch, d->tokens, d->q_heads);
+  if (q == out && ((d->batch > 1 && d->q_strides[0] != d->out_strides[0]) || (d->tokens > 1 && d->q_strides[1] != d->out_strides[1]) || (d->q_heads > 1 && d->q_strides[2] != d->out_strides[2])))
+    return COMFUSE_ERR_INVALID_ARG;
   return aligned(q, 16) && aligned(out, 16) && aligned(table, 4) && aligned(lengths, 4) && aligned(slopes, 4) && aligned(lse, 4) ? COMFUSE_OK : COMFUSE_ERR_ALIGNMENT;
 }
 

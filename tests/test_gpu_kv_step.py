@@ -110,3 +110,59 @@ def test_a_prefix_read_back_for_attention_over_it(cuda_device):
     cf.paged_attention(q[:, -1], c.k, c.v, table, torch.tensor([n], dtype=torch.int32, device=cuda_device), out, workspace=ws, **c.scales())
     # values up to about 4: rounded to bf16 on the way (2^-9), weights to bf16 (2^-9), outputs twice (2^-9 of at most 1); averages of 256 of them
     assert (O[:, -1].float() - out[0].float()).abs().max() <= 4 * 4 * 2.0 ** -9
+
+
+CHILD = r"""
+import threading
+import torch
+import paper_2608_03537_b200 as cf
+from tests import test_gpu_kv_step as steps
+
+dev = torch.device("cuda:0")
+torch.cuda.set_device(0)
+blocks = [steps._block(dev, 6, 8, 2, 64, q) for q in (False, True)]
+for b in blocks:
+    b["x"].add_(1)
+torch.cuda.synchronize()
+# the first calls of the process, captured
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    for b in blocks:
+        steps._step(b)
+for _ in range(5):
+    graph.replay()
+torch.cuda.synchronize()
+for b in blocks:
+    assert int(b["lengths"][0]) == 5
+    steps._check(b)
+# and from several threads, each on its own stream and block
+own = [steps._block(dev, 3 + i, 8, 2, 64, i % 2 == 1) for i in range(4)]
+torch.cuda.synchronize()
+errors = []
+def work(b):
+    try:
+        torch.cuda.set_device(0)
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                steps._step(b)
+            torch.cuda.current_stream().synchronize()
+    except BaseException as e:
+        errors.append(e)
+threads = [threading.Thread(target=work, args=(b,)) for b in own]
+[t.start() for t in threads]
+[t.join() for t in threads]
+assert not errors, errors
+for b in own:
+    steps._check(b)
+assert cf.last_device_status() == cf.OK
+print("steps ok")
+"""
+
+
+def test_captured_as_the_first_calls_of_a_process_and_from_several_threads(cuda_device):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", CHILD], cwd=root, env=dict(os.environ, PYTHONPATH=root), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "steps ok" in r.stdout, r.stdout + r.stderr[-3000:]

@@ -53,6 +53,7 @@ class Call:
         ws = P.guarded((max(16, n),), torch.uint8, 255, q.device)
         args = dict(alpha=self.alpha, softcap=self.cap, slopes=self.slopes, lse=lse, workspace=ws, **more)
         args.update(kw)
+        out = args.pop("out", out)
         assert cf.paged_attention(q, c.k, c.v, self.device_table, self.device_lengths, out, **args) is out
         torch.cuda.synchronize()
         P.check_canaries({"out": self.out, "lse": self.lse, "workspace": ws})
@@ -104,6 +105,56 @@ def test_layouts(layout, name, quantized, cuda_device):
         c = Call([200, 33, 70], 1, 8, 4, 128, page, name, quantized, cuda_device, seed=page, layout=layout, spare=3, dims=3)
         c.run()
         c.check()
+
+
+@pytest.mark.parametrize("quantized", [False, True])
+@pytest.mark.parametrize("page", [16, 20])
+def test_keys_and_values_laid_out_differently(page, quantized, cuda_device):
+    """Keys [pages, heads, page, D], values [pages, page, heads, D], scales with strides of their own."""
+    c = Call([300, 41, 128], 2, 6, 3, 64, page, "f16", quantized, cuda_device, seed=8)
+    c.run()
+    first = c.out.clone()
+    c.cache.v = c.cache.v.transpose(1, 2).contiguous().transpose(1, 2)
+    if quantized:
+        c.cache.ks = c.cache.ks.transpose(0, 2).contiguous().transpose(0, 2)
+    for t in (c.cache.v, c.cache.ks):
+        if t is not None:
+            t._base_tensor = t
+    c.cache.check_canaries = lambda label="": None
+    c.run()
+    c.check()
+    assert torch.equal(first, c.out)
+
+
+@pytest.mark.parametrize("quantized", [False, True])
+@pytest.mark.parametrize("D", [8, 16, 40, 72, 136, 176, 248])
+def test_unusual_widths(D, quantized, cuda_device):
+    if quantized and D % 16:
+        return
+    c = Call([300, 0, 77, 1], 2, 12, 2, D, 16, "bf16", quantized, cuda_device, seed=D, slopes=True)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("quantized", [False, True])
+@pytest.mark.parametrize("T,Hq,H,D", [(1, 8, 2, 128), (4, 16, 2, 64), (7, 28, 2, 128), (3, 6, 3, 256)])
+def test_outputs_over_the_queries(T, Hq, H, D, quantized, cuda_device):
+    c = Call([2000, 0, 300, 45, 1000], T, Hq, H, D, 16, "bf16", quantized, cuda_device, seed=T)
+    c.run()
+    first, own = c.out.clone(), c.q.clone()
+    c.run(out=c.q)
+    assert torch.equal(c.q, first)
+    c.q.copy_(own)
+    c.check()
+
+
+def test_many_sequences(cuda_device):
+    """More sequences than a CTA has threads, most of them short, some empty."""
+    r = np.random.RandomState(2)
+    lengths = np.where(r.rand(1500) < 0.1, 0, np.ceil(2.0 ** r.uniform(0, 7, 1500))).astype(np.int64)
+    c = Call(lengths, 1, 2, 1, 64, 16, "bf16", False, cuda_device, seed=6)
+    c.run()
+    c.check()
 
 
 @pytest.mark.parametrize("name,quantized", TYPES)

@@ -151,7 +151,8 @@ def test_cache_write_and_read_refuse():
 
 def test_attention_refuses():
     for kw in (dict(q=None), dict(table=None), dict(lengths=None), dict(out=None), dict(batch=0), dict(tokens=0), dict(q_heads=0), dict(q_heads=7), dict(table_width=0), dict(max_length=-1), dict(window=-1),
-               dict(alpha=float("inf")), dict(softcap=-1.0), dict(softcap=float("nan")), dict(table_stride=9), dict(q_strides=(1024, 512, 0)), dict(out_strides=(1024, 512, 56))):
+               dict(alpha=float("inf")), dict(softcap=-1.0), dict(softcap=float("nan")), dict(table_stride=9), dict(q_strides=(1024, 512, 0)), dict(out_strides=(1024, 512, 56)),
+               dict(out=FAKE, out_strides=(2048, 512, 64)), dict(out=FAKE, out_strides=(1024, 512, 128))):
         assert _attention(**kw) == cf.ERR_INVALID_ARG, kw
     long = dict(table_width=4096, table_stride=4096)   # room for sequences that are cut
     for kw in (dict(q=ODD), dict(out=ODD), dict(table=OFF4), dict(lengths=OFF4), dict(slopes=OFF4), dict(lse=OFF4), dict(long, workspace=ODD), dict(q_strides=(1028, 512, 64))):
