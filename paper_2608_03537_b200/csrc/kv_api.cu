@@ -202,29 +202,31 @@ PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, b
   const paged::FormFacts f = quantized ? paged::facts<true>(D, plan.rows) : paged::facts<false>(D, plan.rows);
   int64_t seen = max_length;  // positions of a sequence that may be visible, from the block of the first on
   if (window > 0) seen = std::min<int64_t>(seen, static_cast<int64_t>(window) + tokens - 1 + f.block - 1);
-  const int64_t units = std::max<int64_t>(1, (seen + f.unit - 1) / f.unit);
+  const int64_t units = std::max<int64_t>(1, (seen + f.unit - 1) / f.unit), cluster_units = std::max<int64_t>(1, (seen + f.cluster_unit - 1) / f.cluster_unit);
   const int64_t items = static_cast<int64_t>(batch) * heads * plan.row_blocks;
   if (items > 0x7FFFFFFF / (units + f.set_up)) return plan;  // (units are counted in 32 bits: no CTAs)
   const int64_t slots = 148 * f.ctas_per_sm;
   // Items by clusters, or equal shares and a second kernel?  By estimated times (us): a CTA's start and end, and a unit alone, as measured on one sequence of 100 .. 16000 positions (rows: 16, 8 bits;
   // D up to 64, 128, 256; columns: 8, 16, 32, 64 query rows); where CTAs share SMs a unit takes a quarter longer, where they take all of HBM its bytes at 6 TB/s.  A second kernel costs 2.9, a
   // cluster's joining 1.2; clusters of 8 and 16 leave some SMs idle, and clusters that do not fit at once are not taken.  Of a batch's lengths only the largest is known: 0.6 of it is
-  // taken for the mean.  Over 300 calls of 1 .. 64 sequences of 100 .. 16000 positions the choice is 1.5 % slower than the best of the six would be, in the geometric mean; shares alone 15 %.
-  static constexpr float kStart[2][3][4] = {{{3.1f, 3.9f, 4.1f, 4.3f}, {3.0f, 4.4f, 5.4f, 5.7f}, {4.2f, 6.0f, 6.3f, 6.5f}}, {{4.5f, 6.2f, 6.4f, 6.8f}, {4.8f, 6.9f, 7.7f, 6.5f}, {5.4f, 8.2f, 8.5f, 10.5f}}};
-  static constexpr float kUnit[2][3][4] = {{{0.82f, 0.98f, 1.30f, 1.47f}, {0.86f, 0.96f, 1.03f, 1.06f}, {1.12f, 1.25f, 1.63f, 1.96f}},
-                                           {{0.85f, 1.08f, 1.34f, 1.36f}, {1.03f, 1.41f, 1.22f, 1.26f}, {0.97f, 1.59f, 2.03f, 2.10f}}};
+  // taken for the mean.  Over 300 calls of 1 .. 64 sequences of 100 .. 16000 positions the choice is 1.4 % slower than the best of the six would be, in the geometric mean; shares alone 15 %.
+  static constexpr float kStart[2][3][4] = {{{3.1f, 3.9f, 4.1f, 4.4f}, {3.1f, 4.6f, 5.7f, 7.4f}, {4.4f, 6.3f, 6.6f, 6.6f}}, {{4.4f, 6.3f, 6.5f, 6.7f}, {4.9f, 6.9f, 6.9f, 6.9f}, {5.4f, 8.3f, 8.0f, 10.7f}}};
+  static constexpr float kUnit[2][3][4] = {{{0.79f, 0.97f, 1.27f, 1.39f}, {0.83f, 0.94f, 1.47f, 1.49f}, {1.08f, 1.22f, 1.57f, 1.90f}},
+                                           {{0.85f, 1.07f, 1.36f, 1.35f}, {1.01f, 1.37f, 1.90f, 2.00f}, {0.95f, 1.58f, 2.01f, 2.12f}}};
   constexpr double kLaunch = 2.5;  // of the start: once, however many rounds of CTAs there are
   const int di = DH == 64 ? 0 : DH == 128 ? 1 : 2, ri = plan.rows == 8 ? 0 : plan.rows == 16 ? 1 : plan.rows == 32 ? 2 : 3;
   const double start = kStart[quantized][di][ri], unit = kUnit[quantized][di][ri], mean = batch > 1 ? 0.6 : 1.0;
-  auto unit_us = [&](int64_t ctas) {
+  auto unit_us = [](double alone, int bytes, int64_t ctas) {
     const double n = static_cast<double>(ctas);
-    return std::max(unit * (1.0 + 0.25 * std::max(0.0, n / 148 - 1.0)), f.unit_bytes * n / 6e6);
+    return std::max(alone * (1.0 + 0.25 * std::max(0.0, n / 148 - 1.0)), bytes * n / 6e6);
   };
-  double best = start + 2.9 + std::max(1.0, static_cast<double>(items) * (static_cast<double>(units) * mean + 2 * f.set_up) / static_cast<double>(slots)) * unit_us(std::min(slots, items * units));
+  // (three rings instead of two do half as much again in a third more time)
+  const double share_unit = f.unit == f.cluster_unit ? unit : unit * 1.33;
+  double best = start + 2.9 + std::max(1.0, static_cast<double>(items) * (static_cast<double>(units) * mean + 2 * f.set_up) / static_cast<double>(slots)) * unit_us(share_unit, f.unit_bytes, std::min(slots, items * units));
   for (int c = 1; c <= 16; c *= 2) {
     const int64_t ctas = items * c, fit = f.cluster_ctas_per_sm * (c == 16 ? 112 : c == 8 ? 120 : 148), rounds = (ctas + fit - 1) / fit;
-    if ((c > 1 && (c > units || rounds > 1)) || ctas > 0x7FFFFFFF) break;
-    const double each = static_cast<double>((units + c - 1) / c) * unit_us(std::min(ctas, fit)) * (rounds == 1 ? 1.0 : mean);
+    if ((c > 1 && (c > cluster_units || rounds > 1)) || ctas > 0x7FFFFFFF) break;
+    const double each = static_cast<double>((cluster_units + c - 1) / c) * unit_us(unit, f.cluster_unit_bytes, std::min(ctas, fit)) * (rounds == 1 ? 1.0 : mean);
     const double us = kLaunch + static_cast<double>(rounds) * (start - kLaunch + each) + (c > 1 ? 1.2 : 0.0);
     if (us < best) plan.cluster = c, best = us;
   }

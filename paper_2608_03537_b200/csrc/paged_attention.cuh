@@ -50,10 +50,12 @@ template <bool Q8, int DH, int NT, int RW, bool CLUSTER>
 struct Form {
   static constexpr int kRowBytes = DH * (Q8 ? 1 : 2);
   static constexpr int kPieces = kRowBytes / 16;                  // of a row
-  // Groups of 16 positions in a block: two where rows are short (half the votes, waits and loop a position) and the registers hold both.
-  static constexpr int kGroups = kRowBytes <= 128 && !(Q8 && DH == 128 && RW > 1) ? 2 : 1;
+  // Groups of 16 positions in a block: two where the registers and the ring hold them (half the votes, meetings and loop a position; 64 rows over 80000 x 4 x 128, 16 bits: 97 us with one, 78 with two).
+  static constexpr int kGroups = kRowBytes <= 128 || (!Q8 && DH == 128 && RW > 1) ? 2 : 1;
   static constexpr int kBlock = 16 * kGroups;
-  static constexpr int kKeyWarps = RW == 4 ? 2 : 4;               // rings
+  // Rings.  64 rows: eight warps of 255 registers, or, where 168 are enough and the call is not one of latency, twelve (the same call: 78 and 69 us; 64 wide, 8 bits: 65 and 59; 128 wide and
+  // 8 bits would spill: 86 and 134; one sequence of 2000 in clusters, 64 wide, 8 bits: 12.3 and 13.8).
+  static constexpr int kKeyWarps = RW < 4 ? 4 : !CLUSTER && (Q8 ? DH == 64 : DH == 128) ? 3 : 2;
   static constexpr int kWarps = kKeyWarps * RW, kThreads = 32 * kWarps;
   static constexpr int kUnit = kBlock * kKeyWarps;
   static constexpr int kRows = 8 * NT * RW;                       // of queries
@@ -830,7 +832,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
 
   // ---- the end of an item, or of the share: the rings' results are joined; whole items are finished, cut ones kept
   // A thread adds up kMine columns of every kJoinColumns, of one of the 8 RW rows that a tile of each row warp makes.
-  constexpr int kMine = 8 * RW * F::kJoinColumns / F::kThreads, kAcross = F::kJoinColumns / kMine;
+  constexpr int kSumThreads = F::kThreads < 256 ? F::kThreads : 256;
+  constexpr int kMine = 8 * RW * F::kJoinColumns / kSumThreads, kAcross = F::kJoinColumns / kMine;
   // `parts`: where the rows of a cut item go.  A cluster: pieces of four columns to the CTAs in turn, statistics to all.
   struct Sent {
     float2 stats[CLUSTER ? 16 : 1][F::kRows];       // by sender
@@ -865,14 +868,14 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
         weight[j] = top[n][j] == -INFINITY && m == -INFINITY ? 1.f : ex2_approx(top[n][j] - m);
         if constexpr (Q8) weight[j] *= unit_v[n][j];
       }
-      const int r = tid / kAcross, col = (tid % kAcross) * kMine, row = n * 8 * RW + r;
+      const int r = min(tid / kAcross, 8 * RW - 1), col = (tid % kAcross) * kMine, row = n * 8 * RW + r;
       float m = sm.top[0][row], l = 0.f;
 #pragma unroll
       for (int w = 1; w < F::kKeyWarps; ++w) m = fmaxf(m, sm.top[w][row]);
 #pragma unroll
       for (int w = 0; w < F::kKeyWarps; ++w) l += sm.sum[w][row] * (sm.top[w][row] == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : ex2_approx(sm.top[w][row] - m));
       const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
-      const bool there = sm.out[row] >= 0;
+      const bool there = tid < kSumThreads && sm.out[row] >= 0;
       float* part = parts + row * (DH + 4);
       if (there && tid % kAcross == 0) {
         if (whole) {
@@ -1182,12 +1185,14 @@ cudaError_t launch_type(const PagedAttentionPlan& plan, const PagedAttentionPara
 
 // What a plan needs to know of the instance that runs it.
 struct FormFacts {
-  int unit, block, ctas_per_sm, cluster_ctas_per_sm, set_up, unit_bytes;
+  int unit, block, ctas_per_sm, set_up, unit_bytes;
+  int cluster_unit, cluster_ctas_per_sm, cluster_unit_bytes;
 };
 template <bool Q8, int DH, int NT, int RW>
 constexpr FormFacts facts_of() {
   using F = Form<Q8, DH, NT, RW, false>;
-  return {F::kUnit, F::kBlock, F::kCtasPerSm, Form<Q8, DH, NT, RW, true>::kCtasPerSm, F::kSetUp, F::kStage * F::kKeyWarps};
+  using C = Form<Q8, DH, NT, RW, true>;
+  return {F::kUnit, F::kBlock, F::kCtasPerSm, F::kSetUp, F::kStage * F::kKeyWarps, C::kUnit, C::kCtasPerSm, C::kStage * C::kKeyWarps};
 }
 template <bool Q8, int DH>
 FormFacts facts(int rows) {
