@@ -693,6 +693,7 @@ def paged_attention(q, k_cache, v_cache, page_table, lengths, out, *, alpha=None
 
     score = alpha * q.k (``alpha``: D ** -0.5 unless given), with ``softcap`` > 0 softcap * tanh(score / softcap), plus slopes[head] * (n - its own position) where ``slopes``
     (fp32 [q_heads]) are given.  ``lse`` (fp32, q's shape without D) receives log(sum(exp(score))).  A token that sees nothing has out 0 and lse -inf.
+    ``out`` may be ``q``.
 
     ``max_length``: no sequence is longer than this (else the table's width decides): fewer CTAs are started for less work.  ``workspace``: a CUDA tensor of
     paged_attention_workspace_size() bytes or more, of any content; calls that may overlap need one each."""
