@@ -9,6 +9,7 @@
 //
 // On one B200 (copies run at 6.5 TB/s): 16384 x 24 x 128 bf16 turned in 34.6 us = 5.8 TB/s; 8192 tokens, 32 heads of queries turned and 2 x 8 of keys and values written, 38 us = 5.3 TB/s; one
 // such token 2.0 us: launch and one round trip; 32768 x 8 x 128 read back from 8 bits 39 us = 5.2 TB/s.
+#include <cmath>
 #include <cstdio>
 
 #include "kv_params.h"
@@ -17,7 +18,9 @@
 namespace comfuse {
 namespace {
 
-constexpr int kThreads = 256;
+// Two warps a CTA: an SM takes the next one as soon as two are done (256 threads: 32768 x 8 x 128 read back in 38.6 us instead of 36.4, 16384 x 24 x 128 turned with pairs side by side in 39.3 instead
+// of 36.2, 777 x 12 x 64 fp32 in 3.7 instead of 3.1).
+constexpr int kThreads = 64;
 constexpr int kMostPairs = 256;  // (D <= 512)
 
 // How a row's pairs lie.  kHalvesWhole: (i, i + pairs), pairs a multiple of 8: a unit is a piece of the first half and its partner.  kAdjacent: (2i, 2i + 1): a unit is
@@ -147,9 +150,10 @@ int lanes_log2_of(int D, int pairs, int mode) {
   return n;
 }
 
-// Three CTAs an SM: 8192 tokens (above) 43.2 us with two, 38.7 with three, 41.8 with four, whose registers no longer hold two rows and the sines; fp32 rows are twice as large, and two CTAs hold them.
+// Warps an SM: 8192 tokens (above) 43.2 us with 16, 38.7 with 24, 41.8 with 32, whose registers no longer hold two rows and the sines; fp32 rows are twice as large, and 16 warps hold them.
+constexpr int warps_of(int dtype) { return dtype == COMFUSE_DTYPE_F32 ? 16 : 24; }
 template <int DT, bool CACHED, bool Q8, int MODE>
-__global__ void __launch_bounds__(kThreads, DT == COMFUSE_DTYPE_F32 ? 2 : 3) rotary_write_kernel(const RotaryWriteParams p, const int lanes_log2) {
+__global__ void __launch_bounds__(kThreads, warps_of(DT) * 32 / kThreads) rotary_write_kernel(const RotaryWriteParams p, const int lanes_log2) {
   __shared__ float2 s_angles[MODE == kNothing ? 1 : kThreads / 32][MODE == kNothing ? 1 : kMostPairs];
   griddep_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -376,9 +380,18 @@ cudaError_t launch_rotary_write(int dtype, bool cached, bool quantized, RotaryWr
   const int mode = !p.positions ? kNothing : p.adjacent ? kAdjacent : p.pairs % 8 == 0 ? kHalvesWhole : kHalves;
   if (mode == kNothing) p.pairs = 0;
   p.rows = p.q_heads + (cached ? 2 * p.kv_heads : 0);
-  // Warps of a token: one where there are tokens enough to fill the GPU, else as many as leave each lane two rows.
-  const int groups = 32 >> lanes_log2_of(p.D, p.pairs, mode);
-  while ((static_cast<long long>(p.tokens) << p.slices_log2) < 16ll * dev.sm_count && (2 * groups) << p.slices_log2 < p.rows) ++p.slices_log2;
+  // Warps of a token: by how many rounds of warps there are (the last one, which has the memory to itself, counts 0.7 and 0.3 of its share), and what a warp does in one: its sines and start, about as
+  // long as two rows a lane, and its rows, two a lane at a time (8192 tokens, 32 + 2 x 8 heads of 128: 36.8 us with one, 34.9 with two, 41 with four; 3000: 15.1 and 17.0; 2000: 12.3 and 11.7;
+  // 4096 of 256: 44.1 and 37.7).
+  const int groups = 32 >> lanes_log2_of(p.D, p.pairs, mode), at_once = dev.sm_count * warps_of(dtype);
+  double least = 0;
+  for (int n = 0; n == 0 || (2 * groups) << (n - 1) < p.rows; ++n) {
+    const double full = std::ldexp(static_cast<double>(p.tokens), n) / at_once, rounds = full <= 1 ? 1.0 : 0.7 * std::ceil(full) + 0.3 * full;
+    const double time = rounds * (1 + (p.rows + (2 * groups << n) - 1) / (2 * groups << n));
+    if (n > 0 && time >= least) continue;
+    least = time;
+    p.slices_log2 = n;
+  }
   const long long warps = static_cast<long long>(p.tokens) << p.slices_log2;
   const unsigned grid = static_cast<unsigned>((warps + kThreads / 32 - 1) / (kThreads / 32));
   if (verbose_enabled())
@@ -399,16 +412,16 @@ namespace {
 template <int DT, bool Q8>
 cudaError_t launch_read(CacheReadParams p, const DeviceInfo& dev, cudaStream_t stream) {
   const int lanes = lanes_log2_of(p.D, 0, kNothing), groups = kThreads >> lanes;
-  // Eight tokens a block where that leaves no group without one; four rows a lane where they still fill the GPU (32768 x 8 x 128 from 8 bits: 41 us with two, 38 with four, 43
-  // with eight; 500 x 6 x 64: 2.2 us with two, 3.2 with four).
+  // Eight tokens a block where that leaves no group without one; several rows a lane where they still fill the GPU, four only of 8 bits (32768 x 8 x 128 from 8 bits: 38.6 us with two, 36.2 with four;
+  // from 16 bits 43.9 and 46.2; 4000 x 8 x 128 from 8 bits 9.1 us with one, 6.7 with two, 8.4 with four).
   while (p.tokens_log2 < 3 && p.tokens % (2 << p.tokens_log2) == 0) ++p.tokens_log2;
   if (p.tokens >= 64) p.tokens_log2 = 3;
-  const long long blocks = (p.tokens + (1ll << p.tokens_log2) - 1) >> p.tokens_log2, rows = (blocks << p.tokens_log2) * p.rows.d;
-  const bool many = rows >= 8ll * 4 * groups * dev.sm_count;
-  const long long per = (many ? 4ll : 1ll) * groups;
-  const unsigned grid = static_cast<unsigned>((rows + per - 1) / per);
-  if (many) return launch(cache_read_kernel<DT, Q8, 4>, p, lanes, grid, stream);
-  return launch(cache_read_kernel<DT, Q8, 1>, p, lanes, grid, stream);
+  const long long blocks = (p.tokens + (1ll << p.tokens_log2) - 1) >> p.tokens_log2, rows = (blocks << p.tokens_log2) * p.rows.d, ctas = rows / groups;
+  const int per = Q8 && ctas >= 128ll * dev.sm_count ? 4 : ctas >= 16ll * dev.sm_count ? 2 : 1;
+  const unsigned grid = static_cast<unsigned>((rows + per * groups - 1) / (per * groups));
+  if constexpr (Q8)
+    if (per == 4) return launch(cache_read_kernel<DT, Q8, 4>, p, lanes, grid, stream);
+  return per == 2 ? launch(cache_read_kernel<DT, Q8, 2>, p, lanes, grid, stream) : launch(cache_read_kernel<DT, Q8, 1>, p, lanes, grid, stream);
 }
 }  // namespace
 
