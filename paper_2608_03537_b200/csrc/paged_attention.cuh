@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
       const bool mine = r < F::kRows && step < kQuerySteps;
       uint32_t* to = s_query + step * kStepWords + r * 8;
       if constexpr (Q8) {
-        // A multiple of 2^-21 of the power of two at or below the row's largest element, in three digits: exact for bf16 down to 2^-14 of that, for fp16 to 2^-11.
+        // A multiple of 2^-21 of the power of two at or below the row's largest element, below 2^22 of them, in three digits: exact for bf16 down to 2^-14 of that, for fp16 to 2^-11.
         uint32_t top = 0u;  // of the bits: infinities and NaNs are above every number
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -443,8 +443,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
 #pragma unroll
         for (int o = kQuerySteps / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         const bool odd = top >= 0x7F800000u;  // (such a row has no digits: NaN)
-        const uint32_t e = min(max(top & 0x7F800000u, 0x10000000u), 0x7E000000u);  // (2^-95: a row below that is zero beside any other)
-        const float up = reciprocal_of_power(__uint_as_float(e)) * 0x1p21f;
+        const uint32_t e = min(max(top & 0x7F800000u, 0x10000000u), 0x7F000000u);  // (2^-95: a row below that is zero beside any other; 2^127: the largest numbers')
+        const float up = __uint_as_float(0x89800000u - e);  // 2^21 / e, a normal number for all of them
         if (mine && step == 0) sm.factor[r] = odd ? __int_as_float(0x7FFFFFFF) : __uint_as_float(e) * 0x1p-21f;
         // elements 4w .. 4w + 3 of the step are word 2 (w mod 4) + w / 4 of its row: lane c's first four, and 16 further its second
         uint32_t digit[kDigits][8];
@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
   // normal number of fp16 down to 2^-20 of the largest.
   float unit_v[NT][2];
   float factor[NT][2];  // of a score
-  const SoftcapLog2 cap(p.alpha, p.softcap > 0.f ? p.softcap : 1.f);
+  const SoftcapLog2 cap(1.f, p.softcap > 0.f ? p.softcap : 1.f);
   auto begin_item = [&]() {
     if constexpr (RW > 1) {
       const int here = p.row_blocks == 1 ? p.rows : min(F::kRows, p.rows - (hr - hr / p.row_blocks * p.row_blocks) * F::kRows);
@@ -517,8 +517,9 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
       for (int k = 0; k < kSteps; ++k) o[k][n][0] = o[k][n][1] = o[k][n][2] = o[k][n][3] = 0.f;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        factor[n][j] = p.softcap > 0.f ? 1.f : p.alpha * kLog2e;
-        if constexpr (Q8) factor[n][j] *= sm.factor[row_of_mine + 8 * RW * n + j];
+        factor[n][j] = p.alpha;
+        if constexpr (Q8) factor[n][j] *= sm.factor[row_of_mine + 8 * RW * n + j];  // (together: a tiny alpha and a large query make an ordinary factor, of sums that fit)
+        if (p.softcap <= 0.f) factor[n][j] *= kLog2e;
       }
     }
     if constexpr (kHold) {
@@ -617,7 +618,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
 #pragma unroll
         for (int n = 0; n < TN; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[h][n][i] = cap(Q8 ? s[h][n][i] * (factor[n][i & 1] * ks[h][i >> 1]) : s[h][n][i]) - ref[n][i & 1];
+          for (int i = 0; i < 4; ++i) s[h][n][i] = cap(s[h][n][i] * (Q8 ? factor[n][i & 1] * ks[h][i >> 1] : factor[n][i & 1])) - ref[n][i & 1];
     } else {
 #pragma unroll
       for (int h = 0; h < G; ++h)

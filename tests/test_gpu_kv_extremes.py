@@ -1,0 +1,64 @@
+"""Paged attention where its number formats end, against the definition in 64 bits: queries near the largest number over an 8-bit cache.
+
+Bounds (u = 2^-24, half a step of fp32), beside what tests/kv.py derives:
+  queries over 8 bits  an element enters as a multiple of 2^-21 of a power of two that is at most its row's largest, max: off by at most 2^-22 max.  A score: 2^-22 |alpha| max sum|k|, and its
+                       factor (alpha, power of two, scale, log2 e) is rounded four times: 4 u of itself (inside 8 u peak).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_oracle as orc
+from tests import kv
+from tests.test_gpu_paged_attention import Call
+
+pytestmark = pytest.mark.gpu
+
+FORMS = [(1, 8, 2, 128), (3, 4, 1, 64), (5, 5, 1, 256), (8, 8, 1, 128)]   # new tokens, query heads, key heads, D: 4 .. 64 query rows
+MAX_BF16 = torch.finfo(torch.bfloat16).max
+
+
+def check(c):
+    """As Call.check, with the bound above."""
+    quantized, dtype = c.cache.quantized, c.out.dtype
+    q, keys = kv.f64(c.q), c.cache.values("k")
+    want, lse, weight = orc.attention(q, keys, c.cache.values("v"), c.table, c.lengths, c.alpha, c.cap, None if c.slopes is None else kv.f64(c.slopes), c.window)
+    ds = np.zeros_like(lse)
+    if quantized:
+        held = np.abs(np.nan_to_num(keys)).sum(-1).max()
+        ds += 2.0 ** -22 * abs(c.alpha) * np.abs(q).max(-1) * held
+    bound, lse_bound = kv.attention_bounds(want, lse, weight, int(c.lengths.max()), c.D, dtype, quantized, c.cap)
+    bound = bound + (1 + kv.half_step(dtype)) * 2 * ds[..., None] * weight[0]
+    got, got_lse, seen = kv.f64(c.out), kv.f64(c.lse), np.isfinite(lse)
+    assert np.isfinite(got).all() and np.array_equal(np.isfinite(got_lse), seen)
+    assert np.all(np.abs(got_lse - lse)[seen] <= (lse_bound + ds)[seen])
+    worst = np.max(np.abs(got - want) / bound)
+    assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+@pytest.mark.parametrize("T,Hq,H,D", FORMS)
+@pytest.mark.parametrize("largest", [2.0 ** 125, 2.0 ** 126, 1.9921875 * 2.0 ** 126, 2.0 ** 127, 1.5 * 2.0 ** 127, MAX_BF16])
+def test_large_queries_over_8_bits(largest, T, Hq, H, D, cap, cuda_device):
+    """A row's largest elements, of both signs, up to the type's largest number; alpha brings the scores back."""
+    c = Call([300, 45, 64], T, Hq, H, D, 16, "bf16", True, cuda_device, seed=D, alpha=2.0 ** -126, cap=cap)
+    x = kv.f64(c.q)
+    x /= np.abs(x).max(-1, keepdims=True)
+    x[..., 7::16], x[..., 3::16] = 1, -1
+    c.q.copy_(torch.from_numpy((x * largest).astype(np.float32)).to(cuda_device))   # (exact: the rounding to bf16 is the copy's)
+    assert c.q.abs().max() == largest
+    for side in "kv":   # codes up to 127 with scales of about 2^-7
+        scale = c.cache.ks if side == "k" else c.cache.vs
+        scale.mul_(2.0 ** torch.round(-torch.log2(scale) - 7))
+    c.run()
+    check(c)
+
+
+def test_an_outlying_query_element_over_8_bits(cuda_device):
+    """One element 2^15 times as large as the others meets keys that are zero there."""
+    for name in ("bf16", "f16"):
+        c = Call([300, 45], 1, 8, 2, 128, 16, name, True, cuda_device, seed=3)
+        c.q[..., 5] = 2.0 ** 15
+        c.cache.k[..., 5] = 0
+        c.run()
+        check(c)

@@ -1,0 +1,17 @@
+"""The tests of the paged attention's number formats once more on forms that a call can take (the switch is read once, so each form runs in a process of its own)."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.mark.parametrize("cluster", [0, 1, 4, 16])
+def test_form(cluster, cuda_device):
+    r = subprocess.run([sys.executable, "-m", "pytest", os.path.join(ROOT, "tests", "test_gpu_kv_extremes.py"), "-x", "-q", "-m", "gpu", "-p", "no:cacheprovider"], cwd=ROOT,
+                       env=dict(os.environ, COMFUSE_ATTENTION_CLUSTER=str(cluster), PYTHONPATH=ROOT), capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-3000:]
