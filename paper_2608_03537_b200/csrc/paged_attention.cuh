@@ -44,6 +44,10 @@ cudaError_t launch_f16_q8(const PagedAttentionPlan& plan, const PagedAttentionPa
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;  // log2 of what a weight may exceed 1 by
 constexpr int kDigits = 3;     // of a query, 8 bits
+// log2 of the weight at the running maximum.  fp16 over 16 bits: 2^7, so that with the slack weights stay below 2^15; fp16's steps end at 2^-24, so what both parts of a weight leave is at most
+// 2^-32 of the largest (with 1 a weight of e^-16 was off by 6 %, and from e^-17.5 on it was 0, in the product alone).  8 bits have units of their own, and bf16 has fp32's range.
+template <int DT, bool Q8>
+constexpr int kLiftOf = DT == COMFUSE_DTYPE_F16 && !Q8 ? 7 : 0;
 
 // Sizes of an instance: D up to DH, NT tiles of eight queries a warp, RW warps with rows of their own to a ring.
 template <bool Q8, int DH, int NT, int RW, bool CLUSTER>
@@ -211,10 +215,11 @@ __device__ __forceinline__ float reciprocal_of_power(float x) { return __uint_as
 __device__ __forceinline__ void st_cluster_f32x4(uint32_t at, const float* v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
 }
-// log of a sum whose terms were divided by 2^m; nothing: -inf
+// log of a sum whose terms were divided by 2^(m - LIFT); nothing: -inf
+template <int LIFT>
 __device__ __forceinline__ float log_sum(float m, float l) {
   if (m == -INFINITY) return l == 0.f ? -INFINITY : l;  // (else a NaN)
-  return m * 0.6931471805599453f + logf(l);
+  return m * 0.6931471805599453f + logf(l * (1.f / (1 << LIFT)));
 }
 // Piece c of row r lies at place c ^ (...): the eight rows that an ldmatrix reads at once are on eight different groups of banks.
 template <int PIECES>
@@ -231,6 +236,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
   // A weight in 16 bits is off by half a step of its type, which behind a sum over like terms is as much as the output's own rounding.  So the weights go in twice, rounded and what
   // the rounding left.  fp16 weights of bf16 outputs are eight times as fine as those and go in once.
   constexpr bool kTwice = !(Q8 && kBf16);
+  constexpr int kLift = kLiftOf<DT, Q8>;  // the sums carry it too, so it leaves at the division
   constexpr int kSteps = DH / 16, G = F::kGroups, S = F::kStages;
   static_assert(S >= 2 && S <= 8, "a ring of two blocks at least");
   extern __shared__ __align__(128) char smem[];
@@ -602,15 +608,15 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
           vs[h][i] = scales[F::kBlock + 16 * h + 8 * i + g];
         }
     }
-    // s: scores in the log2 domain less the running maximum (0 where there is none yet)
+    // s: scores in the log2 domain less the running maximum, raised by kLift (no maximum yet: the scores)
     float ref[TN][2], limit[TN][2];
 #pragma unroll
     for (int n = 0; n < TN; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const bool none = top[n][j] == -INFINITY;
-        ref[n][j] = none ? 0.f : top[n][j];
-        limit[n][j] = none ? -INFINITY : kSlack;
+        ref[n][j] = none ? 0.f : top[n][j] - kLift;
+        limit[n][j] = none ? -INFINITY : kSlack + kLift;
       }
     if (p.softcap > 0.f) {
 #pragma unroll
@@ -689,8 +695,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
           for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
           // (s is relative to ref: the maximum rises by m, where that is positive or there was none)
           const bool none = top[n][j] == -INFINITY;
-          const float rise = none ? m : fmaxf(m, 0.f), shift = rise == -INFINITY ? 0.f : rise;
-          const float less = none ? 1.f : ex2_approx(-shift);  // (without a maximum there is nothing yet to make less)
+          const float rise = none ? m : fmaxf(m - kLift, 0.f), shift = !none ? rise : rise == -INFINITY ? 0.f : rise - kLift;
+          const float less = none ? 1.f : ex2_approx(-rise);  // (without a maximum there is nothing yet to make less)
           top[n][j] = none ? rise : top[n][j] + rise;
           sum[n][j] *= less;
           float both = less;
@@ -880,7 +886,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
       float* part = parts + row * (DH + 4);
       if (there && tid % kAcross == 0) {
         if (whole) {
-          if (p.lse && COMFUSE_IN_BOUNDS(sm.lse[row] < p.batch * p.tokens * p.heads * p.group, p.status)) p.lse[sm.lse[row]] = log_sum(m, l);
+          if (p.lse && COMFUSE_IN_BOUNDS(sm.lse[row] < p.batch * p.tokens * p.heads * p.group, p.status)) p.lse[sm.lse[row]] = log_sum<kLiftOf<DT, Q8>>(m, l);
         } else if constexpr (CLUSTER) {
           for (int k = 0; k < p.cluster; ++k) st_cluster_f32x2(map_to_cta(smem_u32(&sent.stats[rank][row]), k), m, l);
         } else if (COMFUSE_IN_BOUNDS(row < F::kRows, p.status)) {
@@ -994,7 +1000,7 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
         uint32_t packed[2];
         Elem<DT>::pack(y, packed);
         if (col < p.D && COMFUSE_IN_BOUNDS(col + 4 <= p.D && r < here, p.status)) st_8(p.out + sm.out[r] + 2 * col, packed);
-        if (p.lse && col == 0 && COMFUSE_IN_BOUNDS(sm.lse[r] < p.batch * p.tokens * p.heads * p.group, p.status)) p.lse[sm.lse[r]] = log_sum(m, l);
+        if (p.lse && col == 0 && COMFUSE_IN_BOUNDS(sm.lse[r] < p.batch * p.tokens * p.heads * p.group, p.status)) p.lse[sm.lse[r]] = log_sum<kLiftOf<DT, Q8>>(m, l);
       }
       break;
     }
@@ -1110,7 +1116,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const PagedAttention
   uint32_t packed[2];
   Elem<DT>::pack(y, packed);
   if (col < p.D && COMFUSE_IN_BOUNDS(col + 4 <= p.D && row < p.rows && at.b < p.batch, p.status)) st_8(out + 2 * col, packed);
-  if (lse && tid == 0 && COMFUSE_IN_BOUNDS(at.b < p.batch && token < p.tokens, p.status)) *lse = log_sum(m, l);
+  if (lse && tid == 0 && COMFUSE_IN_BOUNDS(at.b < p.batch && token < p.tokens, p.status)) *lse = log_sum<kLiftOf<DT, Q8>>(m, l);
 }
 
 // ------------------------------------------------------------------------------------------------ launches

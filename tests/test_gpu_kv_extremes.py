@@ -1,16 +1,18 @@
-"""Paged attention where its number formats end, against the definition in 64 bits: queries near the largest number over an 8-bit cache.
+"""Paged attention where its number formats end, against the definition in 64 bits: queries near the largest number over an 8-bit cache, weights far below the largest one.
 
 Bounds (u = 2^-24, half a step of fp32), beside what tests/kv.py derives:
   queries over 8 bits  an element enters as a multiple of 2^-21 of a power of two that is at most its row's largest, max: off by at most 2^-22 max.  A score: 2^-22 |alpha| max sum|k|, and its
                        factor (alpha, power of two, scale, log2 e) is rounded four times: 4 u of itself (inside 8 u peak).
+  weights              over 8 bits as there; fp16 over 16 bits: the largest is held as 2^7, and fp16's steps end at 2^-24, so the two parts together are off by up to 2^-25: 2^-32 of the largest weight,
+                       2^-32 max|v| for each position.
 """
 import numpy as np
 import pytest
 import torch
 
 from oracle import kv_oracle as orc
-from tests import kv
-from tests.test_gpu_paged_attention import Call
+from tests import kv, parity as P
+from tests.test_gpu_paged_attention import TYPES, Call
 
 pytestmark = pytest.mark.gpu
 
@@ -19,7 +21,7 @@ MAX_BF16 = torch.finfo(torch.bfloat16).max
 
 
 def check(c):
-    """As Call.check, with the bound above."""
+    """As Call.check, with the bounds above."""
     quantized, dtype = c.cache.quantized, c.out.dtype
     q, keys = kv.f64(c.q), c.cache.values("k")
     want, lse, weight = orc.attention(q, keys, c.cache.values("v"), c.table, c.lengths, c.alpha, c.cap, None if c.slopes is None else kv.f64(c.slopes), c.window)
@@ -28,7 +30,8 @@ def check(c):
         held = np.abs(np.nan_to_num(keys)).sum(-1).max()
         ds += 2.0 ** -22 * abs(c.alpha) * np.abs(q).max(-1) * held
     bound, lse_bound = kv.attention_bounds(want, lse, weight, int(c.lengths.max()), c.D, dtype, quantized, c.cap)
-    bound = bound + (1 + kv.half_step(dtype)) * 2 * ds[..., None] * weight[0]
+    small = c.lengths.max() * 2.0 ** -32 * weight[3] if dtype == torch.float16 and not quantized else np.zeros_like(lse)
+    bound = bound + (1 + kv.half_step(dtype)) * (2 * ds[..., None] * weight[0] + small[..., None])
     got, got_lse, seen = kv.f64(c.out), kv.f64(c.lse), np.isfinite(lse)
     assert np.isfinite(got).all() and np.array_equal(np.isfinite(got_lse), seen)
     assert np.all(np.abs(got_lse - lse)[seen] <= (lse_bound + ds)[seen])
@@ -62,3 +65,28 @@ def test_an_outlying_query_element_over_8_bits(cuda_device):
         c.cache.k[..., 5] = 0
         c.run()
         check(c)
+
+
+@pytest.mark.parametrize("name,quantized", TYPES)
+@pytest.mark.parametrize("T,Hq,H,D", FORMS)
+@pytest.mark.parametrize("gap", [10.0, 13.0, 15.0, 16.5, 18.0])
+def test_small_weights_behind_a_dominating_position(gap, T, Hq, H, D, name, quantized, cuda_device):
+    """The first position outweighs each other by e^gap, and its value is zero: thousands of small like weights are the output.  As many sequences as give a CTA whole ones, so that a
+    warp that holds the first position holds a quarter of the others or more; all of them on the same pages."""
+    n, B = 3000, 320
+    c = Call([n], T, Hq, H, D, 16, name, quantized, cuda_device, seed=1, alpha=1.0)
+    where = [torch.from_numpy(x).to(cuda_device) for x in (c.table[0, np.arange(n) // 16].astype(np.int64), np.arange(n) % 16)]
+    g = torch.Generator(device=cuda_device).manual_seed(2)
+    keys, values = torch.zeros(n, H, D, device=cuda_device), 1 + 0.25 * torch.rand(n, H, D, device=cuda_device, generator=g)
+    keys[0, :, 0] = 1.0
+    values[0] = 0
+    c.cache.put("k", *where, keys)
+    c.cache.put("v", *where, values)
+    c.q = torch.zeros(B, T, Hq, D, dtype=c.q.dtype, device=cuda_device)
+    c.q[..., 0] = gap
+    c.out, c.lse = P.guarded((B, T, Hq, D), c.q.dtype, -77.0, cuda_device), P.guarded((B, T, Hq), torch.float32, -77.0, cuda_device)
+    c.device_table, c.device_lengths = c.device_table.repeat(B, 1), c.device_lengths.repeat(B)
+    c.run()
+    some = [0, 1, B // 2, B - 1]
+    c.q, c.out, c.lse, c.table, c.lengths = c.q[some], c.out[some], c.lse[some], c.table.repeat(4, 0), c.lengths.repeat(4)
+    check(c)
