@@ -1,5 +1,6 @@
 // C entry points of the key-value cache: argument checks, choice of the form.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdlib>
 
@@ -344,7 +345,9 @@ comfuse_status_t comfuse_paged_attention(const comfuse_paged_attention_desc_t* d
   fill_cache(*cache, &p.kc, &p.vc);
   p.table = table; p.table_stride = d.table_stride; p.lengths = lengths;
   p.slopes = slopes; p.lse = lse;
-  p.alpha = d.alpha; p.softcap = d.softcap;
+  p.alpha = d.alpha; p.alpha_log2 = d.alpha * paged::kLog2e;
+  p.cap = std::min(d.softcap * paged::kLog2e, FLT_MAX);  // (caps near the largest number and below the normal ones stay finite)
+  p.per_cap = p.cap > 0.f ? std::min(1.f / p.cap, FLT_MAX) : 0.f;
   p.part = static_cast<float*>(workspace);
   p.ctas = plan.ctas;
   p.cluster = plan.cluster;

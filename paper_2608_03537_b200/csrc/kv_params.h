@@ -87,7 +87,8 @@ struct PagedAttentionParams {
   const int* lengths;
   const float* slopes;
   float* lse;
-  float alpha, softcap;
+  float alpha, alpha_log2;              // alpha log2 e
+  float cap, per_cap;                   // in the log2 domain, and 1 / cap; 0: no soft-cap
   float* part;                          // partial results, see paged_attention.cuh
   int ctas, cluster;                    // cluster: CTAs of an item (0: shares)
   unsigned int* status;

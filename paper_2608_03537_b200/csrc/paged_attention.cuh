@@ -215,6 +215,17 @@ __device__ __forceinline__ float reciprocal_of_power(float x) { return __uint_as
 __device__ __forceinline__ void st_cluster_f32x4(uint32_t at, const float* v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
 }
+// cap * tanh(x / cap), x, cap and the result in the log2 domain.  cap - 2 cap / (1 + e^(2x / cap)) is exact to 2^-21 of itself where x is not small beside the cap, but its error is one of the cap; so
+// below 0.6 of it x times a polynomial in (x / cap)^2 takes its place (coefficients fitted to tanh(y) / y, 2^-22), which for caps far above x, up to the largest number, is x.
+constexpr float kCapNear = 0.6f;
+__device__ __forceinline__ float softcap_near(float x, float per_cap) {
+  const float y = x * per_cap, t = y * y;
+  return fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.015612628310918808f, -0.05221180245280266f), 0.13313116133213043f), -0.33332598209381104f), 1.f) * x;
+}
+__device__ __forceinline__ float softcap_any(float x, float cap, float per_cap) {
+  const float far = fmaf(-2.f * cap, rcp_approx(1.f + ex2_approx(x * per_cap * (2.f * kLog2e))), cap);
+  return fabsf(x * per_cap) < kCapNear ? softcap_near(x, per_cap) : far;
+}
 // log of a sum whose terms were divided by 2^(m - LIFT); nothing: -inf
 template <int LIFT>
 __device__ __forceinline__ float log_sum(float m, float l) {
@@ -508,7 +519,6 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
   // normal number of fp16 down to 2^-20 of the largest.
   float unit_v[NT][2];
   float factor[NT][2];  // of a score
-  const SoftcapLog2 cap(1.f, p.softcap > 0.f ? p.softcap : 1.f);
   auto begin_item = [&]() {
     if constexpr (RW > 1) {
       const int here = p.row_blocks == 1 ? p.rows : min(F::kRows, p.rows - (hr - hr / p.row_blocks * p.row_blocks) * F::kRows);
@@ -523,9 +533,8 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
       for (int k = 0; k < kSteps; ++k) o[k][n][0] = o[k][n][1] = o[k][n][2] = o[k][n][3] = 0.f;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        factor[n][j] = p.alpha;
-        if constexpr (Q8) factor[n][j] *= sm.factor[row_of_mine + 8 * RW * n + j];  // (together: a tiny alpha and a large query make an ordinary factor, of sums that fit)
-        if (p.softcap <= 0.f) factor[n][j] *= kLog2e;
+        // (alpha and the query's together first: a tiny alpha and a large query make an ordinary factor)
+        factor[n][j] = Q8 ? p.alpha * sm.factor[row_of_mine + 8 * RW * n + j] * kLog2e : p.alpha_log2;
       }
     }
     if constexpr (kHold) {
@@ -618,13 +627,53 @@ __global__ void __launch_bounds__(Form<Q8, DH, NT, RW, CLUSTER>::kThreads, Form<
         ref[n][j] = none ? 0.f : top[n][j] - kLift;
         limit[n][j] = none ? -INFINITY : kSlack + kLift;
       }
-    if (p.softcap > 0.f) {
+    if (p.cap > 0.f) {
+      auto far_of = [&](int h, int n) {
+        bool far = false;
 #pragma unroll
-      for (int h = 0; h < G; ++h)
+        for (int i = 0; i < 4; ++i) {
+          s[h][n][i] *= Q8 ? factor[n][i & 1] * ks[h][i >> 1] : factor[n][i & 1];
+          far |= fabsf(s[h][n][i] * p.per_cap) >= kCapNear;
+        }
+        return far;
+      };
+      auto capped_any = [&](int h, int n) {
 #pragma unroll
-        for (int n = 0; n < TN; ++n)
+        for (int i = 0; i < 4; ++i) s[h][n][i] = softcap_any(s[h][n][i], p.cap, p.per_cap) - ref[n][i & 1];
+      };
+      auto capped_near = [&](int h, int n) {  // (most blocks of most calls: no exponentials)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[h][n][i] = cap(s[h][n][i] * (Q8 ? factor[n][i & 1] * ks[h][i >> 1] : factor[n][i & 1])) - ref[n][i & 1];
+        for (int i = 0; i < 4; ++i) s[h][n][i] = softcap_near(s[h][n][i], p.per_cap) - ref[n][i & 1];
+      };
+      // One look at all of the block's scores (five new tokens of 8 sequences, D = 256: 34.3 us, with one a tile 35.4), or, where 168 registers or fewer would not hold what lies between (64 rows
+      // of 128 over 20000 positions, 8 heads: 48.5 us instead of 53.1), at a tile's.
+      if constexpr (F::kThreads * F::kCtasPerSm > 256) {
+#pragma unroll
+        for (int h = 0; h < G; ++h)
+#pragma unroll
+          for (int n = 0; n < TN; ++n) {
+            if (__any_sync(0xFFFFFFFFu, far_of(h, n))) capped_any(h, n);
+            else capped_near(h, n);
+          }
+      } else {
+        bool far = false;
+#pragma unroll
+        for (int h = 0; h < G; ++h)
+#pragma unroll
+          for (int n = 0; n < TN; ++n) far |= far_of(h, n);
+        const bool any = __any_sync(0xFFFFFFFFu, far);
+        if (any) {
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int n = 0; n < TN; ++n) capped_any(h, n);
+        } else {
+#pragma unroll
+          for (int h = 0; h < G; ++h)
+#pragma unroll
+            for (int n = 0; n < TN; ++n) capped_near(h, n);
+        }
+      }
     } else {
 #pragma unroll
       for (int h = 0; h < G; ++h)

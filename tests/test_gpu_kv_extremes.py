@@ -1,10 +1,11 @@
-"""Paged attention where its number formats end, against the definition in 64 bits: queries near the largest number over an 8-bit cache, weights far below the largest one.
+"""Paged attention where its number formats end, against the definition in 64 bits: queries near the largest number over an 8-bit cache, weights far below the largest one, soft-caps of any size.
 
 Bounds (u = 2^-24, half a step of fp32), beside what tests/kv.py derives:
   queries over 8 bits  an element enters as a multiple of 2^-21 of a power of two that is at most its row's largest, max: off by at most 2^-22 max.  A score: 2^-22 |alpha| max sum|k|, and its
                        factor (alpha, power of two, scale, log2 e) is rounded four times: 4 u of itself (inside 8 u peak).
   weights              over 8 bits as there; fp16 over 16 bits: the largest is held as 2^7, and fp16's steps end at 2^-24, so the two parts together are off by up to 2^-25: 2^-32 of the largest weight,
                        2^-32 max|v| for each position.
+  soft-cap             relative to the score: 16 u (both of its branches are below 2^-21 = 8 u of it, and its argument is rounded three times).
 """
 import numpy as np
 import pytest
@@ -21,7 +22,7 @@ MAX_BF16 = torch.finfo(torch.bfloat16).max
 
 
 def check(c):
-    """As Call.check, with the bounds above."""
+    """As Call.check, with the bounds above (the soft-cap's in place of one that is relative to the cap)."""
     quantized, dtype = c.cache.quantized, c.out.dtype
     q, keys = kv.f64(c.q), c.cache.values("k")
     want, lse, weight = orc.attention(q, keys, c.cache.values("v"), c.table, c.lengths, c.alpha, c.cap, None if c.slopes is None else kv.f64(c.slopes), c.window)
@@ -29,7 +30,9 @@ def check(c):
     if quantized:
         held = np.abs(np.nan_to_num(keys)).sum(-1).max()
         ds += 2.0 ** -22 * abs(c.alpha) * np.abs(q).max(-1) * held
-    bound, lse_bound = kv.attention_bounds(want, lse, weight, int(c.lengths.max()), c.D, dtype, quantized, c.cap)
+    if c.cap:
+        ds += 16 * kv.U * weight[1]
+    bound, lse_bound = kv.attention_bounds(want, lse, weight, int(c.lengths.max()), c.D, dtype, quantized)
     small = c.lengths.max() * 2.0 ** -32 * weight[3] if dtype == torch.float16 and not quantized else np.zeros_like(lse)
     bound = bound + (1 + kv.half_step(dtype)) * (2 * ds[..., None] * weight[0] + small[..., None])
     got, got_lse, seen = kv.f64(c.out), kv.f64(c.lse), np.isfinite(lse)
@@ -89,4 +92,13 @@ def test_small_weights_behind_a_dominating_position(gap, T, Hq, H, D, name, quan
     c.run()
     some = [0, 1, B // 2, B - 1]
     c.q, c.out, c.lse, c.table, c.lengths = c.q[some], c.out[some], c.lse[some], c.table.repeat(4, 0), c.lengths.repeat(4)
+    check(c)
+
+
+@pytest.mark.parametrize("name,quantized", TYPES)
+@pytest.mark.parametrize("T,Hq,H,D", FORMS[:2] + FORMS[3:])
+@pytest.mark.parametrize("cap", [1e-40, 1e-30, 0.5, 6.0, 30.0, 3000.0, 1e5, 1e7, 1e8, 1e20, 3e38])
+def test_caps_of_all_sizes(cap, T, Hq, H, D, name, quantized, cuda_device):
+    c = Call([400, 0, 33, 129], T, Hq, H, D, 24, name, quantized, cuda_device, seed=D, cap=cap, scale=3.0, slopes=T == 3)
+    c.run()
     check(c)
