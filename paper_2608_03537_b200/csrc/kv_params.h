@@ -20,10 +20,14 @@ struct Divisor {
     m = static_cast<unsigned>((1ull << (31 + l)) / by + 1);
     shift = l - 1;
   }
-  unsigned divide(unsigned n) const { return m ? static_cast<unsigned>((static_cast<unsigned long long>(n) * m) >> 32) >> shift : n; }
-#ifdef __CUDACC__
-  __device__ __forceinline__ unsigned of(unsigned n) const { return m ? __umulhi(n, m) >> shift : n; }
+  __host__ __device__ __forceinline__ unsigned of(unsigned n) const {
+#ifdef __CUDA_ARCH__
+    const unsigned upper = __umulhi(n, m);
+#else
+    const unsigned upper = static_cast<unsigned>((static_cast<unsigned long long>(n) * m) >> 32);
 #endif
+    return m ? upper >> shift : n;
+  }
 };
 
 // Where a cached row lies: base + page * page_stride + head * head_stride + row * row_stride.
