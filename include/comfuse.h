@@ -571,11 +571,13 @@ typedef struct {
  *   score[n] = cap(alpha * q[b, i, h] . k[n]) + slopes[h] * (n - m)   for max(0, m - window + 1) <= n <= m, and nothing for other positions
  *   out[b, i, h] = sum_n softmax(score)[n] v[n],   lse[b, i, h] = log sum_n exp(score[n])
  * Positions on pages outside the cache (a table entry < 0 or >= pages) count as not there.  Where nothing is left out is 0 and lse -inf.  What other
- * positions hold, infinities and NaN too, changes nothing.  slopes (fp32 [q_heads]) and lse (fp32 [batch, tokens, q_heads], dense) may be NULL.
- * q and out are 16-bit, of the cache's dtype.  Scores, statistics and sums are fp32; the weights enter the second product in 16 bits twice (the rounded
- * weight and what the rounding left), or over an 8-bit cache and bf16 outputs once, as fp16; over an 8-bit cache a position may add an error of 2^-31 of the
- * largest value that its row sees, and an element of a query is off by at most 2^-22 of the largest of its row (not at all from 2^-14 of that on for bf16,
- * 2^-11 for fp16); over 16 bits of fp16 a position may add one of 2^-32 of the largest value.  out may be q itself (same strides); otherwise they do not overlap.
+ * positions hold, infinities and NaN too, changes nothing; what is seen and is not finite makes the outputs that it reaches infinite or NaN.
+ * slopes (fp32 [q_heads]) and lse (fp32 [batch, tokens, q_heads], dense) may be NULL.
+ * q and out are 16-bit, of the cache's dtype.  Scores (soft-caps of any size too), statistics and sums are fp32; the weights enter the second product in 16
+ * bits twice (the rounded weight and what the rounding left), or over an 8-bit cache and bf16 outputs once, as fp16.  Where fp16's range ends a position may
+ * add an error of 2^-31 (8-bit cache) or 2^-32 (16 bits of fp16) of the largest value that its row sees.  Over an 8-bit cache an element of a query is off by
+ * at most 2^-22 of the largest of its row (not at all from 2^-14 of that on for bf16, 2^-11 for fp16).
+ * out may be q itself (same strides); otherwise they do not overlap.
  * Workspace: comfuse_paged_attention_workspace_size() bytes (a function of the sizes alone, never above 32 MiB), 16-byte aligned, of any content;
  * calls that may overlap need one each.  Results do not depend on the order in which parts finish. */
 comfuse_status_t comfuse_paged_attention_workspace_size(const comfuse_paged_attention_desc_t* desc, const comfuse_kv_cache_t* cache, size_t* bytes);

@@ -210,7 +210,9 @@ PagedAttentionPlan paged_attention_plan(int batch, int rows, int heads, int D, b
   // Items by clusters, or equal shares and a second kernel?  By estimated times (us): a CTA's start and end, and a unit alone, as measured on one sequence of 100 .. 16000 positions (rows: 16, 8 bits;
   // D up to 64, 128, 256; columns: 8, 16, 32, 64 query rows); where CTAs share SMs a unit takes a quarter longer, where they take all of HBM its bytes at 6 TB/s.  A second kernel costs 2.9, a
   // cluster's joining 1.2; clusters of 8 and 16 leave some SMs idle, and clusters that do not fit at once are not taken.  Of a batch's lengths only the largest is known: 0.6 of it is
-  // taken for the mean.  Over 300 calls of 1 .. 64 sequences of 100 .. 16000 positions the choice is 1.4 % slower than the best of the six would be, in the geometric mean; shares alone 15 %.
+  // taken for the mean.  Over 300 calls of 1 .. 64 sequences of 100 .. 16000 positions, lengths spread below the longest, the choice is 1.4 % slower than the best of the six would be, in the geometric
+  // mean; shares alone 15 %.  Over 120 calls of 2 .. 64 sequences of 200 .. 4000 positions it is 1.6 % slower, and where all are equally long 1.4 % (the worst 27 and 29 %); over 30 that see
+  // windows of 512, 3.6 and 3.2 % (19 %).
   static constexpr float kStart[2][3][4] = {{{3.1f, 3.9f, 4.1f, 4.4f}, {3.1f, 4.6f, 5.7f, 7.4f}, {4.4f, 6.3f, 6.6f, 6.6f}}, {{4.4f, 6.3f, 6.5f, 6.7f}, {4.9f, 6.9f, 6.9f, 6.9f}, {5.4f, 8.3f, 8.0f, 10.7f}}};
   static constexpr float kUnit[2][3][4] = {{{0.79f, 0.97f, 1.27f, 1.39f}, {0.83f, 0.94f, 1.47f, 1.49f}, {1.08f, 1.22f, 1.57f, 1.90f}},
                                            {{0.85f, 1.07f, 1.36f, 1.35f}, {1.01f, 1.37f, 1.90f, 2.00f}, {0.95f, 1.58f, 2.01f, 2.12f}}};

@@ -7,8 +7,9 @@
 // heads: a warp computes the sines and cosines of its token once, two pairs a lane, and each lane keeps those of its unit while it turns row after row.  Where there are few tokens
 // several warps share one, each with its own sines.
 //
-// On one B200 (copies run at 6.5 TB/s): 16384 x 24 x 128 bf16 turned in 33.5 us = 6.0 TB/s; 8192 tokens, 32 heads of queries turned and 2 x 8 of keys and values written, 35 us = 5.8 TB/s; one
-// such token 2.1 us: launch and one round trip; 32768 x 8 x 128 read back from 8 bits 36 us = 5.6 TB/s.
+// On one B200 (copies run at 6.5 TB/s), replayed as a graph: 16384 x 24 x 128 bf16 turned in 33.5 us = 6.0 TB/s, fp32 in 65.3 = 6.2, with pairs side by side in 81; 8192 tokens, 32 heads of queries
+// turned and 2 x 8 of keys and values written, 35 us = 5.8 TB/s, into 8 bits 42.5 = 4.4; one such token 2.1 us: launch and one round trip; 32768 x 8 x 128 read back from 8 bits 36.5 us =
+// 5.6 TB/s, from 16 bits 43.7 = 6.1.  Called one by one the short ones take what the host takes (one token 4.3 to 4.7 us), and the read-back from 8 bits 38.6.
 #include <cmath>
 #include <cstdio>
 
@@ -18,7 +19,7 @@
 namespace comfuse {
 namespace {
 
-// Two warps a CTA: an SM takes the next one as soon as two are done (256 threads: 32768 x 8 x 128 read back in 38.6 us instead of 36.4, 16384 x 24 x 128 turned with pairs side by side in 39.3 instead
+// Two warps a CTA: an SM takes the next one as soon as two are done (256 threads, all as graphs: 32768 x 8 x 128 read back in 38.6 us instead of 36.4, 16384 x 24 x 128 turned with pairs side by side in 39.3 instead
 // of 36.2, 777 x 12 x 64 fp32 in 3.7 instead of 3.1).
 constexpr int kThreads = 64;
 constexpr int kMostPairs = 256;  // (D <= 512)
@@ -412,7 +413,7 @@ namespace {
 template <int DT, bool Q8>
 cudaError_t launch_read(CacheReadParams p, const DeviceInfo& dev, cudaStream_t stream) {
   const int lanes = lanes_log2_of(p.D, 0, kNothing), groups = kThreads >> lanes;
-  // Eight tokens a block where that leaves no group without one; several rows a lane where they still fill the GPU, four only of 8 bits (32768 x 8 x 128 from 8 bits: 38.6 us with two, 36.2 with four;
+  // Eight tokens a block where that leaves no group without one; several rows a lane where they still fill the GPU, four only of 8 bits (as graphs: 32768 x 8 x 128 from 8 bits 38.6 us with two, 36.4 with four;
   // from 16 bits 43.9 and 46.2; 4000 x 8 x 128 from 8 bits 9.1 us with one, 6.7 with two, 8.4 with four).
   while (p.tokens_log2 < 3 && p.tokens % (2 << p.tokens_log2) == 0) ++p.tokens_log2;
   if (p.tokens >= 64) p.tokens_log2 = 3;

@@ -21,10 +21,11 @@
 //     The key's scale is a factor of its score, the value's scale one of its weight.  The values' codes become fp16 by five instructions for each four.
 //   * The maximum is renewed only when a score is more than 8 (a factor of 256) above it: a vote instead of a reduction in most blocks.
 //
-// On one B200 (copies run at 6.5 TB/s): one sequence of 131072 positions, 8 key heads of 128 for 32 of queries, bf16, 92 us = 5.9 TB/s; 64 sequences of up to 16384 positions over 8 bits, 8 heads of
-// 128 for 64, 180 us = 6.0 TB/s on a cold GPU and 198 under its power limit, which is then what bounds it; 1000 positions 6.2 us, most of them start and end; 24 sequences that see 512 positions, 16
-// heads of 64, 13 us = 3.6 TB/s; eight sequences of up to 5000 positions with five new tokens each, 2 heads of 256 for 16, 33 us = 1.3 TB/s: 40 rows of 256 fill the registers with eight warps an SM,
-// whose chain from block to block (copies seen, first product, exponentials, second product) is the time; 64 rows of 128 over 80000 positions, 4 heads, 70 us = 2.3 TB/s by twelve warps.
+// On one B200 (copies run at 6.5 TB/s), replayed as a graph: one sequence of 131072 positions, 8 key heads of 128 for 32 of queries, bf16, 92 us = 5.9 TB/s; 64 sequences of up to 16384 positions over
+// 8 bits, 8 heads of 128 for 64, 179 us = 6.0 TB/s on a cold GPU and 199 under its power limit, which is then what bounds it; 1000 positions 6.6 us, most of them start and end; 24 sequences that see
+// 512 positions, 16 heads of 64, 13.3 us = 3.5 TB/s; eight sequences of up to 5000 positions with five new tokens each, 2 heads of 256 for 16, 33.9 us = 1.3 TB/s (8 bits: 41): 40 rows of 256 fill
+// the registers with eight warps an SM, whose chain from block to block (copies seen, first product, exponentials, second product) is the time; 64 rows of 128 over 80000 positions, 4 heads, 73 us =
+// 2.2 TB/s by twelve warps (8 bits: 87; rows of 256: 146 and 178).  Called one by one these take as long, but for the short ones' half a microsecond.
 #pragma once
 
 #include <cstdio>
